@@ -1,0 +1,490 @@
+"""Operators on a key/value cache held in 4 bits: rows quantised as they are written, rows read back, and the tree-masked
+multi-stream attention that reads the codes.
+
+Format.  The d values of one head's key (or value) at one slot are stored as codes c in 0..15 with one scale s and one zero
+point z of their own: a value stands for s * (c - z).  With lo = min(0, min x), hi = max(0, max x):
+    s = (hi - lo) / 15 rounded up to bf16 (2**-120 if that is larger),   z = round(-lo / s),   c = min(15, max(0, round(x / s) + z)),
+round() going to the nearest whole number and from the middle away from zero.  x and s have 8 significant bits each, so x / s is
+either exactly in the middle or at least 2**-13 of itself away from it.
+Layout.  Codes uint8 [layers][slots][heads][d / 2]: of every 8 values 8w .. 8w + 7, value 8w + 2i lies at bits 4i and value
+8w + 2i + 1 at bits 16 + 4i of the little-endian 32-bit word w.  Scales and zero points int32 [layers][slots][heads] (any strides;
+here a head's slots lie next to each other): bits 0..15 the scale as bf16, bits 16..19 the zero point.
+
+Kinds
+  attend  one layer's attention: the rows of a draft tree's nodes (and of their speculative streams) see the 4-bit prefix, their
+          ancestors and themselves; a tree of one node is plain decoding
+  write   rows enter the cache (a prompt, or the accepted path of a verified draft, in all layers at once) and are read back
+  read    a run of slots is read back as bf16
+"""
+import math
+import random
+
+import torch
+
+own = False
+
+ORDER = [0, 2, 4, 6, 1, 3, 5, 7]           # nibble n of a word holds value ORDER[n] of its 8
+PATH_STRIDE = 64
+
+
+def _attend(name, batch, heads, dim, length, nodes, gamma=0, lse=False, head_major=False):
+    return dict(name=name, op="attend", batch=batch, heads=heads, dim=dim, len_lo=length[0], len_hi=length[1], nodes=nodes,
+                gamma=gamma, lse=lse, head_major=head_major)
+
+
+def _write(name, layers, batch, heads, dim, rows, held, path=False):
+    return dict(name=name, op="write", layers=layers, batch=batch, heads=heads, dim=dim, rows_lo=rows[0], rows_hi=rows[1],
+                held=held, path=path)
+
+
+def _read(name, layers, batch, heads, dim, rows, held):
+    return dict(name=name, op="read", layers=layers, batch=batch, heads=heads, dim=dim, rows_lo=rows[0], rows_hi=rows[1], held=held)
+
+
+def listed():
+    return [
+        # one user decoding token by token with a 7B-class model: a call of a few microseconds
+        _attend("attend token 7b", 1, 32, 128, (2048, 2048), 1),
+        # one user, 1.3B-class model, a plain layer under a draft of 16 nodes
+        _attend("attend 1.3b", 1, 32, 64, (512, 512), 16),
+        # one user, 2.7B-class model, a multi-stream layer: 32 nodes and three streams are 128 rows of 80
+        _attend("attend 2.7b streams", 1, 32, 80, (1024, 1024), 32, 3),
+        # one user, 7B-class model: a plain layer, and a multi-stream layer of 320 rows
+        _attend("attend 7b", 1, 32, 128, (2048, 2048), 64),
+        _attend("attend 7b streams", 1, 32, 128, (2048, 2048), 64, 4),
+        # sixteen users at once, each at another length, log-sum-exps wanted
+        _attend("attend 7b ragged x16", 16, 32, 128, (512, 4096), 64, 0, True),
+        # plain decoding of a full batch, from fresh prompts to long ones: bound by reading the cache
+        _attend("attend token x64", 64, 32, 128, (1, 8191), 1),
+        # one user far into a long text, a draft that is a chain of five, head-major cache
+        _attend("attend long chain", 1, 32, 128, (100001, 100001), 5, 0, False, True),
+        # the accepted path of a verified draft enters all layers of a 7B-class model
+        _write("write path 7b", 32, 1, 32, 128, (5, 5), 2048, True),
+        # prompts of four users, ragged, into eight layers
+        _write("write prompts", 8, 4, 32, 128, (512, 4096), 3),
+        # reading back one layer of one user, and an odd run of a 2.7B-class model's layers
+        _read("read 7b", 1, 1, 32, 128, (2048, 2048), 0),
+        _read("read 2.7b odd", 32, 2, 32, 80, (1, 1301), 37),
+    ]
+
+
+def draw(rng):
+    def log_int(lo, hi):
+        return max(lo, min(hi, int(round(math.exp(rng.uniform(math.log(lo), math.log(hi + 1)))))))
+
+    limit = max(work(c)["bytes"] for c in listed() if c["op"] == "attend")
+    flops = max(work(c)["flops"] for c in listed())
+    moved = max(work(c)["bytes"] for c in listed() if c["op"] != "attend")
+    while True:
+        op = rng.choice(["attend", "attend", "attend", "write", "read"])
+        heads, dim = rng.choice([2, 8, 13, 16, 32, 40]), rng.choice([64, 80, 128])
+        batch = log_int(1, 64)
+        if op == "attend":
+            hi = log_int(1, 100001)
+            lo = rng.choice([hi, rng.randint(0, hi), rng.randint(0, hi)])
+            case = _attend("", batch, heads, dim, (lo, hi), log_int(1, 64), rng.choice([0, 0, 0, 1, 2, 3, 4]), rng.random() < 0.5,
+                           rng.random() < 0.3)
+            cost = work(case)
+            if cost["bytes"] <= limit and cost["flops"] <= flops:
+                break
+        else:
+            hi = log_int(1, 4096)
+            lo = rng.randint(0, hi)
+            layers, held = log_int(1, 32), rng.randint(0, 5000)
+            if op == "write" and rng.random() < 0.5:
+                hi = min(hi, 9)
+                case = _write("", layers, batch, heads, dim, (1, hi), held, True)
+            else:
+                case = (_write if op == "write" else _read)("", layers, batch, heads, dim, (lo, hi), held)
+            if 0 < work(case)["bytes"] <= moved:
+                break
+    del case["name"]
+    return case
+
+
+def _spread(case, lo, hi):
+    """Per sequence a whole number between lo and hi: the case's own, whatever the seed of its values."""
+    rng = random.Random("%d %d %d %d" % (case["batch"], case["heads"], lo, hi))
+    return [rng.randint(lo, hi) for _ in range(case["batch"])]
+
+
+def work(case):
+    H, d = case["heads"], case["dim"]
+    held = 2 * (d // 2 + 4)                                  # bytes of a slot and head: codes, scale and zero point of K and V
+    if case["op"] == "attend":
+        B, T, g = case["batch"], case["nodes"], case["gamma"]
+        n = sum(_spread(case, case["len_lo"], case["len_hi"]))
+        rows = B * T * (1 + g)
+        nbytes = n * H * held + B * T * (1 + g) * H * d * 4 + rows * H * (4 * d + (4 if case["lse"] else 0))
+        return {"bytes": nbytes, "flops": 4 * d * H * T * (1 + g) * (n + B)}
+    n = case["layers"] * sum(_spread(case, case["rows_lo"], case["rows_hi"])) * H
+    if case["op"] == "write":
+        return {"bytes": n * (2 * 2 * d + held + 2 * 2 * d), "flops": n * 2 * d * 6}
+    return {"bytes": n * (held + 2 * 2 * d), "flops": n * 2 * d * 2}
+
+
+# ---- inputs -------------------------------------------------------------------------------------------------------------
+def _values(shape, gen, scale=1.0):
+    """Keys or values as a model's projections give them: normal, some channels of a head far larger than the others."""
+    x = torch.randn(shape, generator=gen, device="cuda", dtype=torch.float32)
+    channel = torch.randn(shape[-2:], generator=gen, device="cuda", dtype=torch.float32)
+    return (x * (0.5 + 0.5 * channel.abs()) * scale + 0.3 * channel).to(torch.bfloat16)
+
+
+def _quantise(x):
+    """bf16 [..., d] -> codes (whole numbers 0..15), scale and zero point [...], all in 64 bits."""
+    x = x.double()
+    lo, hi = x.amin(-1).clamp(max=0.0), x.amax(-1).clamp(min=0.0)
+    m, e = torch.frexp((hi - lo) / 15.0)                    # m in [1/2, 1): eight bits of it are a bf16 significand
+    # (the quotient is rounded; where it is a bf16 times 1 + 2**-53 or so the product with 15 decides)
+    s = torch.ldexp(torch.ceil(m * 256.0), e - 8)
+    below = torch.ldexp(torch.ceil(m * 256.0) - 1.0, e - 8)
+    s = torch.where(below * 15.0 >= hi - lo, below, s)
+    s = s.clamp(min=2.0 ** -120)
+
+    def nearest(v):
+        return torch.sign(v) * torch.floor(v.abs() + 0.5)
+
+    z = nearest(-lo / s)
+    c = (nearest(x / s[..., None]) + z[..., None]).clamp(0.0, 15.0)
+    return c, s, z
+
+
+def _pack(c, s, z):
+    """Codes, scales and zero points in the cache's layout."""
+    n = c.to(torch.uint8).unflatten(-1, (-1, 8))[..., ORDER]
+    codes = (n[..., 0::2] | (n[..., 1::2] << 4)).flatten(-2)
+    scale = s.to(torch.bfloat16).view(torch.int16).to(torch.int32) & 0xFFFF
+    return codes, scale | (z.to(torch.int32) << 16)
+
+
+def _unpack(codes, params):
+    """Values that the cache's bytes stand for, in 32 bits."""
+    n = torch.stack((codes & 15, codes >> 4), -1).flatten(-2).unflatten(-1, (-1, 8))
+    back = [ORDER.index(i) for i in range(8)]
+    c = n[..., back].flatten(-2).float()
+    s = (params << 16).view(torch.float32)
+    z = (params >> 16).float()
+    return s[..., None] * (c - z[..., None])
+
+
+def _empty_cache(layers, slots, heads, dim, head_major=False):
+    if head_major:
+        codes = torch.zeros((layers, heads, slots, dim // 2), dtype=torch.uint8, device="cuda").transpose(1, 2)
+    else:
+        codes = torch.zeros((layers, slots, heads, dim // 2), dtype=torch.uint8, device="cuda")
+    params = torch.zeros((layers, heads, slots), dtype=torch.int32, device="cuda").transpose(1, 2)
+    return codes, params
+
+
+def _filled_cache(layers, slots, heads, dim, gen, head_major=False):
+    codes, params = _empty_cache(layers, slots, heads, dim, head_major)
+    step = max(1, (1 << 25) // (heads * dim))
+    for layer in range(layers):
+        for s0 in range(0, slots, step):
+            n = min(step, slots - s0)
+            codes[layer, s0:s0 + n], params[layer, s0:s0 + n] = _pack(*_quantise(_values((n, heads, dim), gen)))
+    return codes, params
+
+
+def _tree(rng, nodes):
+    """Parents of a random draft tree of depth four at most (a chain where there are no more than five nodes)."""
+    if nodes <= 5:
+        return list(range(-1, nodes - 1))
+    parent, depth, children = [-1], [0], [0]
+    for i in range(1, nodes):
+        u = rng.choice([v for v in range(i) if depth[v] < 4 and children[v] < 4])
+        children[u] += 1
+        parent.append(u)
+        depth.append(depth[u] + 1)
+        children.append(0)
+    return parent
+
+
+def prepare(case, seed):
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    rng = random.Random(seed)
+    B, H, d = case["batch"], case["heads"], case["dim"]
+    st = dict(case=case)
+    if case["op"] == "attend":
+        T, g = case["nodes"], case["gamma"]
+        lens = _spread(case, case["len_lo"], case["len_hi"])
+        caps = [(n + T + 63) // 64 * 64 for n in lens]
+        starts = [sum(caps[:b]) for b in range(B)]
+        st["k"] = _filled_cache(1, sum(caps), H, d, gen, case["head_major"])
+        st["v"] = _filled_cache(1, sum(caps), H, d, gen, case["head_major"])
+        st["lens"], st["starts"] = lens, starts
+        st["parents"] = [_tree(rng, T) for _ in range(B)]
+        for name in ("q_main", "k_tree", "v_tree"):
+            st[name] = _values((B, T, H, d), gen)
+        for name in ("q_spec", "k_spec", "v_spec"):
+            st[name] = _values((B, T, g, H, d), gen) if g else None
+        st["scale"] = 1.0 / math.sqrt(d)
+    else:
+        layers, held = case["layers"], case["held"]
+        rows = _spread(case, case["rows_lo"], case["rows_hi"])
+        most = max(1, max(rows))
+        caps = [held + n + 3 for n in rows]
+        starts = [sum(caps[:b]) for b in range(B)]
+        st["rows"], st["starts"], st["most"] = rows, starts, most
+        st["held"] = torch.full((B,), held, dtype=torch.int32, device="cuda")
+        st["n_rows"] = torch.tensor(rows, dtype=torch.int32, device="cuda")
+        st["path"] = None
+        if case["op"] == "write":
+            st["k"], st["v"] = _empty_cache(layers, sum(caps), H, d), _empty_cache(layers, sum(caps), H, d)
+            source = 64 if case["path"] else most
+            st["k_rows"] = _values((layers, B, source, H, d), gen)
+            st["v_rows"] = _values((layers, B, source, H, d), gen)
+            if case["path"]:
+                st["paths"] = [[0] + sorted(rng.sample(range(1, 64), n - 1)) for n in rows]
+                st["path"] = torch.tensor([p + [-1] * (PATH_STRIDE - len(p)) for p in st["paths"]], dtype=torch.int32, device="cuda")
+        else:
+            st["k"], st["v"] = _filled_cache(layers, sum(caps), H, d, gen), _filled_cache(layers, sum(caps), H, d, gen)
+    if own:
+        _prepare_own(st)
+    torch.cuda.synchronize()
+    return st
+
+
+def _prepare_own(st):
+    from paper_2402_11131_b200 import api
+    case = st["case"]
+    B, H, d = case["batch"], case["heads"], case["dim"]
+    st["cache"] = api.make_kv4_cache(*st["k"], *st["v"])
+    st["kv_start"] = torch.tensor(st["starts"], dtype=torch.int64, device="cuda")
+    if case["op"] == "attend":
+        T, g = case["nodes"], case["gamma"]
+        st["kv_len"] = torch.tensor(st["lens"], dtype=torch.int32, device="cuda")
+        st["trees"] = api.trees_to_device([api.ss_tree_build(p, g) for p in st["parents"]])
+        st["o_main"] = torch.zeros((B, T, H, d), dtype=torch.bfloat16, device="cuda")
+        st["o_spec"] = torch.zeros((B, T, g, H, d), dtype=torch.bfloat16, device="cuda") if g else None
+        st["lse_main"] = torch.zeros((B, T, H), dtype=torch.float32, device="cuda") if case["lse"] else None
+        st["lse_spec"] = torch.zeros((B, T, g, H), dtype=torch.float32, device="cuda") if case["lse"] and g else None
+
+        def params(workspace):
+            return api.make_kv4_attn_params(
+                q_main=st["q_main"], o_main=st["o_main"], k_tree=st["k_tree"], v_tree=st["v_tree"], cache=st["cache"], layer=0,
+                kv_start=st["kv_start"], kv_len=st["kv_len"], trees=st["trees"], gamma=g, sm_scale=st["scale"],
+                q_spec=st["q_spec"], k_spec=st["k_spec"], v_spec=st["v_spec"], o_spec=st["o_spec"], lse_main=st["lse_main"],
+                lse_spec=st["lse_spec"], workspace=workspace)
+
+        st["workspace"] = api.workspace(api.ss_msa_attention_kv4_workspace_bytes(params(None)))
+        st["params"] = params(st["workspace"])
+    else:
+        st["kv_len_out"] = torch.zeros(B, dtype=torch.int32, device="cuda")
+        st["k_back"] = torch.zeros((case["layers"], B, st["most"], H, d), dtype=torch.bfloat16, device="cuda")
+        st["v_back"] = torch.zeros_like(st["k_back"])
+
+
+# ---- one pass -----------------------------------------------------------------------------------------------------------
+def run(st):
+    case = st["case"]
+    if own:
+        from paper_2402_11131_b200 import api
+        if case["op"] == "attend":
+            api.ss_msa_attention_kv4(st["params"])
+            return _outputs(st["o_main"], st["o_spec"], st["lse_main"], st["lse_spec"])
+        if case["op"] == "write":
+            api.ss_kv4_write(st["k_rows"], st["v_rows"], st["cache"], st["kv_start"], st["held"], st["n_rows"], st["path"], None,
+                             st["kv_len_out"])
+        api.ss_kv4_read(st["cache"], st["k_back"], st["v_back"], st["kv_start"], st["held"], st["n_rows"])
+        return [st["k_back"], st["v_back"]] + ([st["kv_len_out"]] if case["op"] == "write" else [])
+    return {"attend": _plain_attend, "write": _plain_write, "read": _plain_read}[case["op"]](st)
+
+
+def _outputs(*tensors):
+    return [t for t in tensors if t is not None]
+
+
+def _ancestors(parent):
+    """[T][T] truth values: node a is t or one of its ancestors."""
+    T = len(parent)
+    see = torch.zeros((T, T), dtype=torch.bool)
+    for t in range(T):
+        if t:
+            see[t] = see[parent[t]]
+        see[t, t] = True
+    return see
+
+
+def _plain_attend(st):
+    case = st["case"]
+    B, T, g, H, d = case["batch"], case["nodes"], case["gamma"], case["heads"], case["dim"]
+    o_main = torch.empty((B, T, H, d), dtype=torch.bfloat16, device="cuda")
+    o_spec = torch.empty((B, T, g, H, d), dtype=torch.bfloat16, device="cuda") if g else None
+    lse_main = torch.empty((B, T, H), dtype=torch.float32, device="cuda") if case["lse"] else None
+    lse_spec = torch.empty((B, T, g, H), dtype=torch.float32, device="cuda") if case["lse"] and g else None
+    for b in range(B):
+        s0, L = st["starts"][b], st["lens"][b]
+        see = _ancestors(st["parents"][b]).cuda()
+        k_held = _unpack(st["k"][0][0, s0:s0 + L], st["k"][1][0, s0:s0 + L])
+        v_held = _unpack(st["v"][0][0, s0:s0 + L], st["v"][1][0, s0:s0 + L])
+        k = torch.cat((k_held, st["k_tree"][b].float())).permute(1, 2, 0)            # [H][d][L + T]
+        v = torch.cat((v_held, st["v_tree"][b].float())).permute(1, 0, 2)            # [H][L + T][d]
+        hide = torch.cat((torch.zeros((T, L), dtype=torch.bool, device="cuda"), ~see), 1)
+
+        def scores(q):                                                             # [T][H][d] -> [H][T][L + T]
+            return (torch.matmul(q.float().permute(1, 0, 2), k) * st["scale"]).masked_fill(hide, -math.inf)
+
+        def finish(parts, values, out, lse):
+            top = torch.stack([p.amax(-1) for p in parts]).amax(0)
+            e = [torch.exp(p - top[..., None]) for p in parts]
+            total = sum(x.sum(-1) for x in e)
+            o = sum(torch.matmul(x, y) for x, y in zip(e, values)) / total[..., None]
+            out.copy_(o.permute(1, 0, 2).to(torch.bfloat16))
+            if lse is not None:
+                lse.copy_((top + torch.log(total)).permute(1, 0))
+
+        finish([scores(st["q_main"][b])], [v], o_main[b], None if lse_main is None else lse_main[b])
+        for j in range(g):
+            q = st["q_spec"][b, :, j]
+            ks, vs = st["k_spec"][b, :, :j + 1].float(), st["v_spec"][b, :, :j + 1].float()        # [T][j + 1][H][d]
+            near = (q.float()[:, None] * ks).sum(-1).permute(2, 0, 1) * st["scale"]               # [H][T][j + 1]
+            s = scores(q)
+            top = torch.maximum(s.amax(-1), near.amax(-1))
+            e, en = torch.exp(s - top[..., None]), torch.exp(near - top[..., None])
+            total = e.sum(-1) + en.sum(-1)
+            o = torch.matmul(e, v) + (en[..., None] * vs.permute(2, 0, 1, 3)).sum(2)
+            o_spec[b, :, j] = (o / total[..., None]).permute(1, 0, 2).to(torch.bfloat16)
+            if lse_spec is not None:
+                lse_spec[b, :, j] = (top + torch.log(total)).permute(1, 0)
+    return _outputs(o_main, o_spec, lse_main, lse_spec)
+
+
+def _plain_write(st):
+    case = st["case"]
+    B, H, d, layers = case["batch"], case["heads"], case["dim"], case["layers"]
+    out = []
+    for name, (codes, params) in (("k_rows", st["k"]), ("v_rows", st["v"])):
+        back = torch.zeros((layers, B, st["most"], H, d), dtype=torch.bfloat16, device="cuda")
+        for layer in range(layers):
+            for b in range(B):
+                n, at = st["rows"][b], st["starts"][b] + case["held"]
+                if n == 0:
+                    continue
+                rows = st[name][layer, b]
+                rows = rows[st["paths"][b]] if case["path"] else rows[:n]
+                codes[layer, at:at + n], params[layer, at:at + n] = _pack(*_quantise(rows))
+                back[layer, b, :n] = _unpack(codes[layer, at:at + n], params[layer, at:at + n]).to(torch.bfloat16)
+        out.append(back)
+    return out + [st["held"] + st["n_rows"]]
+
+
+def _plain_read(st):
+    case = st["case"]
+    out = []
+    for codes, params in (st["k"], st["v"]):
+        back = torch.zeros((case["layers"], case["batch"], st["most"], case["heads"], case["dim"]), dtype=torch.bfloat16, device="cuda")
+        for b, n in enumerate(st["rows"]):
+            at = st["starts"][b] + case["held"]
+            for layer in range(case["layers"]):
+                back[layer, b, :n] = _unpack(codes[layer, at:at + n], params[layer, at:at + n]).to(torch.bfloat16)
+        out.append(back)
+    return out
+
+
+# ---- the operators' definition in 64 bits ---------------------------------------------------------------------------------
+def _meaning(codes, params):
+    """What stored bytes stand for, value by value: shifts of the 32-bit words."""
+    words = codes.contiguous().view(torch.int32).to(torch.int64) & 0xFFFFFFFF
+    out = torch.empty((*words.shape, 8), dtype=torch.float64, device=codes.device)
+    p = params.to(torch.int64)
+    scale = (p & 0xFFFF).to(torch.int16).view(torch.bfloat16).double()
+    zero = (p >> 16) & 15
+    for i in range(8):
+        at = 4 * (i // 2) + 16 * (i % 2)
+        out[..., i] = ((words >> at) & 15) - zero[..., None]
+    return out.flatten(-2) * scale[..., None]
+
+
+def _stored(x):
+    """What rows stand for once they are stored: the smallest bf16 whose 15-fold covers the range, found by its bit pattern."""
+    x = x.double()
+    span_lo, span_hi = torch.minimum(x.amin(-1), x.new_zeros(())), torch.maximum(x.amax(-1), x.new_zeros(()))
+    span = span_hi - span_lo
+    bits = (span / 15.0).float().view(torch.int32) >> 16
+    s = torch.zeros_like(span)
+    for step in (1, 0, -1):
+        cand = ((bits + step).clamp(min=0) << 16).view(torch.float32).double()
+        s = torch.where((cand * 15.0 >= span) | (s == 0), cand, s)
+    s = torch.maximum(s, torch.full_like(s, 2.0 ** -120))
+    # twice the ratio, one added, halved and rounded down: the nearest whole number, the middle going up
+    def near(num, den):
+        return torch.floor((2.0 * num + den) / (2.0 * den))
+
+    z = near(-span_lo, s)
+    up, down = near(x.abs(), s[..., None]), -near(x.abs(), s[..., None])
+    c = torch.minimum(torch.maximum(torch.where(x < 0, down, up) + z[..., None], x.new_zeros(())), x.new_full((), 15.0))
+    return (c - z[..., None]) * s[..., None]
+
+
+def exact(case, seed):
+    global own
+    mine, own = own, False
+    try:
+        st = prepare(case, seed)
+    finally:
+        own = mine
+    B, H, d = case["batch"], case["heads"], case["dim"]
+    if case["op"] != "attend":
+        out = []
+        for name in ("k", "v"):
+            back = torch.zeros((case["layers"], B, st["most"], H, d), dtype=torch.float64, device="cuda")
+            for layer in range(case["layers"]):
+                for b in range(B):
+                    n, at = st["rows"][b], st["starts"][b] + case["held"]
+                    if n == 0:
+                        continue
+                    if case["op"] == "read":
+                        back[layer, b, :n] = _meaning(st[name][0][layer, at:at + n], st[name][1][layer, at:at + n])
+                    elif case["path"]:
+                        for i, node in enumerate(st["paths"][b]):
+                            back[layer, b, i] = _stored(st[name + "_rows"][layer, b, node])
+                    else:
+                        back[layer, b, :n] = _stored(st[name + "_rows"][layer, b, :n])
+            out.append(back)
+        return out + ([(st["held"] + st["n_rows"])] if case["op"] == "write" else [])
+
+    T, g = case["nodes"], case["gamma"]
+    o_main = torch.zeros((B, T, H, d), dtype=torch.float64, device="cuda")
+    o_spec = torch.zeros((B, T, g, H, d), dtype=torch.float64, device="cuda") if g else None
+    lse_main = torch.zeros((B, T, H), dtype=torch.float64, device="cuda") if case["lse"] else None
+    lse_spec = torch.zeros((B, T, g, H), dtype=torch.float64, device="cuda") if case["lse"] and g else None
+    for b in range(B):
+        s0, L, parent = st["starts"][b], st["lens"][b], st["parents"][b]
+        # one list of keys (prefix, nodes, streams) and one mask over all rows (nodes, then a node's streams)
+        rows, keys = T * (1 + g), L + T + T * g
+        see = torch.zeros((rows, keys), dtype=torch.bool)
+        see[:, :L] = True
+        for t in range(T):
+            mine_rows = [t] + [T + t * g + j for j in range(g)]
+            a = t
+            while a >= 0:
+                for r in mine_rows:
+                    see[r, L + a] = True
+                a = parent[a]
+            for j in range(g):
+                see[T + t * g + j, L + T + t * g:L + T + t * g + j + 1] = True
+        see = see.cuda()
+        for h0 in range(0, H, 4):
+            hs = slice(h0, min(H, h0 + 4))
+            k = [_meaning(st["k"][0][0, s0:s0 + L, hs], st["k"][1][0, s0:s0 + L, hs]), st["k_tree"][b, :, hs].double()]
+            v = [_meaning(st["v"][0][0, s0:s0 + L, hs], st["v"][1][0, s0:s0 + L, hs]), st["v_tree"][b, :, hs].double()]
+            q = [st["q_main"][b, :, hs].double()]
+            if g:
+                k.append(st["k_spec"][b, :, :, hs].double().flatten(0, 1))
+                v.append(st["v_spec"][b, :, :, hs].double().flatten(0, 1))
+                q.append(st["q_spec"][b, :, :, hs].double().flatten(0, 1))
+            k, v, q = torch.cat(k), torch.cat(v), torch.cat(q)
+            s = torch.einsum("rhd,khd->hrk", q, k) * st["scale"]
+            s = torch.where(see, s, torch.full_like(s, -math.inf))
+            lse = torch.logsumexp(s, -1)
+            o = torch.einsum("hrk,khd->rhd", torch.exp(s - lse[..., None]), v)
+            o_main[b, :, hs] = o[:T]
+            if g:
+                o_spec[b, :, :, hs] = o[T:].unflatten(0, (T, g))
+            if case["lse"]:
+                lse_main[b, :, hs] = lse.T[:T]
+                if g:
+                    lse_spec[b, :, :, hs] = lse.T[T:].unflatten(0, (T, g))
+    return _outputs(o_main, o_spec, lse_main, lse_spec)
