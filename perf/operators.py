@@ -250,7 +250,7 @@ def _prepare_own(st):
     from paper_2402_11131_b200 import api
     case = st["case"]
     B, H, d = case["batch"], case["heads"], case["dim"]
-    st["cache"] = api.make_kv4_cache(*st["k"], *st["v"])
+    st["cache"] = api.make_kvq_cache(*st["k"], *st["v"])
     st["kv_start"] = torch.tensor(st["starts"], dtype=torch.int64, device="cuda")
     if case["op"] == "attend":
         T, g = case["nodes"], case["gamma"]
@@ -262,13 +262,13 @@ def _prepare_own(st):
         st["lse_spec"] = torch.zeros((B, T, g, H), dtype=torch.float32, device="cuda") if case["lse"] and g else None
 
         def params(workspace):
-            return api.make_kv4_attn_params(
+            return api.make_kvq_attn_params(
                 q_main=st["q_main"], o_main=st["o_main"], k_tree=st["k_tree"], v_tree=st["v_tree"], cache=st["cache"], layer=0,
                 kv_start=st["kv_start"], kv_len=st["kv_len"], trees=st["trees"], gamma=g, sm_scale=st["scale"],
                 q_spec=st["q_spec"], k_spec=st["k_spec"], v_spec=st["v_spec"], o_spec=st["o_spec"], lse_main=st["lse_main"],
                 lse_spec=st["lse_spec"], workspace=workspace)
 
-        st["workspace"] = api.workspace(api.ss_msa_attention_kv4_workspace_bytes(params(None)))
+        st["workspace"] = api.workspace(api.ss_msa_attention_kvq_workspace_bytes(params(None)))
         st["params"] = params(st["workspace"])
     else:
         st["kv_len_out"] = torch.zeros(B, dtype=torch.int32, device="cuda")
@@ -282,12 +282,12 @@ def run(st):
     if own:
         from paper_2402_11131_b200 import api
         if case["op"] == "attend":
-            api.ss_msa_attention_kv4(st["params"])
+            api.ss_msa_attention_kvq(st["params"])
             return _outputs(st["o_main"], st["o_spec"], st["lse_main"], st["lse_spec"])
         if case["op"] == "write":
-            api.ss_kv4_write(st["k_rows"], st["v_rows"], st["cache"], st["kv_start"], st["held"], st["n_rows"], st["path"], None,
+            api.ss_kvq_write(st["k_rows"], st["v_rows"], st["cache"], st["kv_start"], st["held"], st["n_rows"], st["path"], None,
                              st["kv_len_out"])
-        api.ss_kv4_read(st["cache"], st["k_back"], st["v_back"], st["kv_start"], st["held"], st["n_rows"])
+        api.ss_kvq_read(st["cache"], st["k_back"], st["v_back"], st["kv_start"], st["held"], st["n_rows"])
         return [st["k_back"], st["v_back"]] + ([st["kv_len_out"]] if case["op"] == "write" else [])
     return {"attend": _plain_attend, "write": _plain_write, "read": _plain_read}[case["op"]](st)
 
