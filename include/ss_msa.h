@@ -14,6 +14,7 @@
  *   ss_tree_verify_soft / ss_tree_verify_sampled   soft matching, top-k sampling at T = 1  (App. A.2, App. B)
  *   ss_stream_insert   stream initialisation S = M + P_j                            (Eq. 3)
  *   ss_value_rotate    value-rotation stream variant                                (Eq. 7)
+ *   ss_kvq_write / ss_kvq_read / ss_msa_attention_kvq   a cache held in 4 bits: written, read back, attended over
  *   ss_status          read back the device status word
  *   ss_wait_selftest   diagnostic: a device-side wait that runs out reports SS_ERR_DEVICE_TIMEOUT
  *
@@ -311,6 +312,106 @@ typedef struct ss_cache_layout {
 int32_t ss_kv_compact(void* k_cache_all, void* v_cache_all, const ss_cache_layout* layout, int32_t batch,
                       const int64_t* kv_start, const int32_t* kv_len_in, const int32_t* accept_len,
                       const int32_t* accept_path, int32_t* kv_len_out, void* stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * A cache held in 4 bits: ss_kvq_write puts rows into it, ss_kvq_read takes them out as bf16, ss_msa_attention_kvq attends
+ * over the codes.  (The paper keeps its cache in 16 bits; the format is this library's.)
+ *
+ * The d values of one head's key (or value) at one slot are stored as codes c in 0..15 with one scale s (bf16) and one zero
+ * point z (0..15) of their own; a value stands for s * (c - z).  With lo = min(0, min x) and hi = max(0, max x)
+ *     s = (hi - lo) / 15 rounded up to bf16, or 2^-120 if that is larger;   z = round(-lo / s);
+ *     c = min(15, max(0, round(x / s) + z));        round: to the nearest whole number, from the middle away from zero.
+ * The quotients are those of the exact values, so codes and scales are defined bit by bit.  A value is off by at most s / 2
+ * (s where the code was clamped).  A row with a value that is not finite gets a NaN scale: it reads back as NaN throughout.
+ *
+ * Codes: head_dim / 2 bytes per head and slot.  Of every 8 values 8w .. 8w + 7, value 8w + 2i lies at bits 4i and value
+ * 8w + 2i + 1 at bits 16 + 4i of the little-endian 32-bit word w.  Scales and zero points: one 32-bit word per head and slot,
+ * bits 0..15 the scale, bits 16..19 the zero point, the rest zero.
+ * Layer l, slot s, head h of the codes lies at k_codes + l * layer_stride + s * slot_stride + h * head_stride (bytes: bases and
+ * strides are multiples of 16, of 8 where head_dim is 80), its word at k_params + the same with the param strides (in words).
+ * The attention reads a head's words slot after slot: param_slot_stride = 1 is the fast layout. */
+typedef struct ss_kvq_cache {
+    int32_t n_layers, n_heads, head_dim;
+    int32_t device;                  /* the device that holds the cache: a call with another current device is refused; -1: not checked */
+    void* k_codes;
+    void* v_codes;
+    uint32_t* k_params;
+    uint32_t* v_params;
+    int64_t layer_stride, slot_stride, head_stride;
+    int64_t param_layer_stride, param_slot_stride, param_head_stride;
+    int64_t total_slots;
+} ss_kvq_cache;
+
+/* bf16 rows outside the cache: layer l, sequence b, row r, head h at k + l * layer_stride + b * batch_stride + r * row_stride +
+ * h * head_stride (elements, multiples of 8; bases 16-byte aligned), head_dim values next to each other. */
+typedef struct ss_kvq_rows {
+    void* k;
+    void* v;
+    int64_t layer_stride, batch_stride, row_stride, head_stride;
+    int32_t batch, max_rows;
+} ss_kvq_rows;
+
+/* Writes rows into the cache, in every layer, and advances the lengths: row r < n_rows[b] of sequence b goes to slot
+ * kv_start[b] + kv_len_in[b] + r, and kv_len_out[b] = kv_len_in[b] + n_rows[b].  With a path, row r is rows[path[b][r]] (the
+ * accepted nodes of a draft: accept_len and accept_path of a verification call are n_rows and path; what ss_kv_compact does
+ * for a bf16 cache); without one it is rows[r] (a prompt).
+ *   n_rows int32 [batch] or NULL (max_rows each); at most max_rows without a path, SS_PATH_STRIDE with one, are taken
+ *   path int32 [batch][SS_PATH_STRIDE] or NULL; a row whose entry is not in [0, max_rows) is not written
+ *   kv_capacity int32 [batch] or NULL; kv_len_out int32 [batch] or NULL, may overlap kv_len_in
+ *   status   a workspace whose word 0 receives SS_ERR_CAPACITY, or NULL
+ * A sequence whose rows do not fit (kv_len + n_rows over its capacity, or slots outside the slab) is skipped and keeps its
+ * length.  Slots of other rows are not touched.  One launch, two where kv_len_out overlaps an input.
+ * Errors (nothing launched): SS_ERR_INVALID_ARG, SS_ERR_UNSUPPORTED (head_dim not in {64, 80, 128}), SS_ERR_CUDA. */
+int32_t ss_kvq_write(const ss_kvq_rows* rows, const ss_kvq_cache* cache, const int64_t* kv_start, const int32_t* kv_len_in,
+                     const int32_t* n_rows, const int32_t* path, const int32_t* kv_capacity, int32_t* kv_len_out, void* status,
+                     void* stream);
+
+/* Reads slots back: row r < n_rows[b] of sequence b receives the values of slot kv_start[b] + first[b] + r as bf16 (s * (c - z)
+ * rounded once), in every layer.  first int32 [batch] or NULL (0), n_rows int32 [batch] or NULL (max_rows).  Rows behind
+ * n_rows[b], and rows whose slot lies outside the slab, are left as they are. */
+int32_t ss_kvq_read(const ss_kvq_cache* cache, const ss_kvq_rows* rows, const int64_t* kv_start, const int32_t* first,
+                    const int32_t* n_rows, void* stream);
+
+/* ss_msa_attention over a prefix held in 4 bits (Eq. 1, Eq. 2).  Rows, masks, outputs and log-sum-exps are those of
+ * ss_msa_attention; only slots 0 .. kv_len[b] - 1 of the sequence's run are read from the cache (layer `layer` of it).  The K/V of
+ * the tree's nodes, which that call finds behind the prefix, are bf16 inputs here, as the streams' K/V are: what is rejected
+ * never enters the cache, and what is accepted is quantised once, by ss_kvq_write.  A tree of one node is plain decoding.
+ *   q_main, o_main, k_tree, v_tree        bf16 [batch][max_nodes][n_heads][head_dim]
+ *   q_spec, k_spec, v_spec, o_spec        bf16 [batch][max_nodes][gamma][n_heads][head_dim]
+ *   lse_main, lse_spec                    optional, as there
+ * Scores are s_k * sm_scale * <q, c - z>, the weights p * s_v meet V's (c - z) as bf16 (rounded once, as ss_msa_attention
+ * rounds p); sums, statistics and both products accumulate in fp32.
+ * The keys of all heads are dealt out evenly over the GPU, whatever the lengths; a head that several CTAs share leaves partial
+ * rows in the workspace, and the last of them to finish joins them in key order: results do not depend on the order of arrival,
+ * and no CTA waits for another.
+ * A sequence with kv_len[b] over its capacity, with slots outside the slab or without nodes is skipped (its outputs are not
+ * written); for the first two the status word is set to SS_ERR_CAPACITY.
+ * Errors (nothing launched): SS_ERR_INVALID_ARG, SS_ERR_UNSUPPORTED, SS_ERR_WORKSPACE, SS_ERR_CUDA. */
+typedef struct ss_kvq_attn_params {
+    int32_t batch, gamma, max_nodes, layer;
+    float sm_scale;
+    const void* q_main;
+    void* o_main;
+    const void* k_tree;
+    const void* v_tree;
+    const void* q_spec;
+    const void* k_spec;
+    const void* v_spec;
+    void* o_spec;
+    ss_kvq_cache cache;
+    const int64_t* kv_start;
+    const int32_t* kv_len;
+    const int32_t* kv_capacity;     /* may be NULL */
+    const ss_tree_desc* trees;
+    float* lse_main;
+    float* lse_spec;
+    void* workspace;
+    size_t workspace_bytes;
+} ss_kvq_attn_params;
+
+/* Bytes of workspace the call needs for these shapes, whatever the lengths and the slab. */
+size_t ss_msa_attention_kvq_workspace_bytes(const ss_kvq_attn_params* p);
+int32_t ss_msa_attention_kvq(const ss_kvq_attn_params* p, void* stream);
 
 /* Diagnostic of the bounded device-side waits.  Runs, as one warp, the step in which a CTA of a head split
  * two ways combines its share of the partial rows (the routine ss_msa_attention's kernels use), with no

@@ -32,13 +32,14 @@ _LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libss_msa.
 _lib = None
 _native = None          # the _pycall module: takes the tensors of the per-step calls apart (see native())
 _NATIVE_CALLS = ("ss_msa_attention", "ss_tree_verify", "ss_tree_verify_soft", "ss_tree_verify_sampled", "ss_tree_prune", "ss_next_draft",
-                 "ss_kv_compact", "ss_stream_insert", "ss_value_rotate")        # in the order of _pycall.setup
+                 "ss_kv_compact", "ss_stream_insert", "ss_value_rotate", "ss_msa_attention_kvq", "ss_kvq_write",
+                 "ss_kvq_read")                                                 # in the order of _pycall.setup
 
 # number of kernels each entry point enqueues per call (for launch accounting in the benchmark); ss_kv_compact enqueues a
-# second one where kv_len_out overlaps one of its inputs
+# second one where kv_len_out overlaps one of its inputs, as does ss_kvq_write
 LAUNCHES_PER_CALL = {"ss_msa_attention": 1, "ss_tree_verify": 1, "ss_kv_compact": 1, "ss_next_draft": 1,
                      "ss_tree_prune": 1, "ss_tree_verify_soft": 1, "ss_tree_verify_sampled": 1, "ss_stream_insert": 1,
-                     "ss_value_rotate": 1}
+                     "ss_value_rotate": 1, "ss_msa_attention_kvq": 1, "ss_kvq_write": 1, "ss_kvq_read": 1}
 
 
 class SsError(RuntimeError):
@@ -70,12 +71,31 @@ class CacheLayout(C.Structure):
                 ("layer_stride", C.c_int64), ("slot_stride", C.c_int64), ("head_stride", C.c_int64)]
 
 
+class KvqCache(C.Structure):
+    """A cache in 4 bits (ss_kvq_cache); make_kvq_cache and empty_kvq_cache keep its tensors with it."""
+    _fields_ = [("n_layers", C.c_int32), ("n_heads", C.c_int32), ("head_dim", C.c_int32), ("device", C.c_int32),
+                ("k_codes", C.c_void_p), ("v_codes", C.c_void_p), ("k_params", C.c_void_p), ("v_params", C.c_void_p),
+                ("layer_stride", C.c_int64), ("slot_stride", C.c_int64), ("head_stride", C.c_int64),
+                ("param_layer_stride", C.c_int64), ("param_slot_stride", C.c_int64), ("param_head_stride", C.c_int64),
+                ("total_slots", C.c_int64)]
+
+
+class KvqAttnParams(C.Structure):
+    _fields_ = [("batch", C.c_int32), ("gamma", C.c_int32), ("max_nodes", C.c_int32), ("layer", C.c_int32), ("sm_scale", C.c_float),
+                ("q_main", C.c_void_p), ("o_main", C.c_void_p), ("k_tree", C.c_void_p), ("v_tree", C.c_void_p),
+                ("q_spec", C.c_void_p), ("k_spec", C.c_void_p), ("v_spec", C.c_void_p), ("o_spec", C.c_void_p),
+                ("cache", KvqCache), ("kv_start", C.c_void_p), ("kv_len", C.c_void_p), ("kv_capacity", C.c_void_p),
+                ("trees", C.c_void_p), ("lse_main", C.c_void_p), ("lse_spec", C.c_void_p),
+                ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t)]
+
+
 EXPORTS = ("ss_tree_build", "ss_msa_attention_workspace_bytes", "ss_msa_attention",
            "ss_tree_verify_workspace_bytes", "ss_tree_verify", "ss_tree_verify_static", "ss_kv_compact", "ss_status",
            "ss_version", "ss_error_string",
            "ss_next_draft_workspace_bytes", "ss_next_draft", "ss_tree_prune_workspace_bytes", "ss_tree_prune",
            "ss_tree_verify_soft", "ss_tree_verify_sampled_workspace_bytes", "ss_tree_verify_sampled",
-           "ss_stream_insert", "ss_value_rotate", "ss_wait_selftest")
+           "ss_stream_insert", "ss_value_rotate", "ss_wait_selftest",
+           "ss_kvq_write", "ss_kvq_read", "ss_msa_attention_kvq_workspace_bytes", "ss_msa_attention_kvq")
 SS_MAX_TOPK = 8
 SS_VERIFY_STATIC_SCRATCH_BYTES = 1 << 20
 
@@ -122,6 +142,12 @@ def lib() -> C.CDLL:
         l.ss_stream_insert.argtypes = [vp, vp, vp, C.c_int64, i32, i32, vp]
         l.ss_value_rotate.restype = i32
         l.ss_value_rotate.argtypes = [vp, vp, C.c_int64, i32, i32, f32, vp]
+        l.ss_kvq_write.restype = l.ss_kvq_read.restype = l.ss_msa_attention_kvq.restype = i32
+        l.ss_kvq_write.argtypes = [vp, C.POINTER(KvqCache)] + [vp] * 8
+        l.ss_kvq_read.argtypes = [C.POINTER(KvqCache)] + [vp] * 5
+        l.ss_msa_attention_kvq_workspace_bytes.restype = C.c_size_t
+        l.ss_msa_attention_kvq_workspace_bytes.argtypes = [C.POINTER(KvqAttnParams)]
+        l.ss_msa_attention_kvq.argtypes = [C.POINTER(KvqAttnParams), vp]
         l.ss_wait_selftest.restype = C.c_int32
         l.ss_wait_selftest.argtypes = [C.c_void_p, C.c_size_t, C.c_void_p]
         l.ss_status.restype = C.c_int32
@@ -147,7 +173,7 @@ def native():
             torch.cuda.current_stream()                   # initialises CUDA if nothing has yet
         addresses = tuple(C.cast(getattr(lib(), name), C.c_void_p).value for name in _NATIVE_CALLS)
         _pycall.setup(SsError, torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice, AttnParams, CacheLayout, C.byref,
-                      C.ArgumentError, addresses)
+                      C.ArgumentError, addresses, KvqAttnParams, KvqCache)
         _native = _pycall
     return _native
 
@@ -322,6 +348,95 @@ def ss_kv_compact(k_all, v_all, layout: CacheLayout, kv_start, kv_len_in, accept
                   stream=None) -> None:
     """In-place gather of the accepted path's K/V in every layer (asynchronous on `stream`)."""
     (_native or native()).kv_compact(k_all, v_all, layout, kv_start, kv_len_in, accept_len, accept_path, kv_len_out, stream)
+
+
+# ---- a cache in 4 bits --------------------------------------------------------------------------
+def make_kvq_cache(k_codes: torch.Tensor, k_params: torch.Tensor, v_codes: torch.Tensor, v_params: torch.Tensor) -> KvqCache:
+    """Describes a cache in 4 bits: codes uint8 [n_layers][slots][H][d / 2] (d / 2 contiguous), scales and zero points int32
+    [n_layers][slots][H] (any strides; slots next to each other is the fast order); K and V laid out alike."""
+    for t, dtype, dims in ((k_codes, torch.uint8, 4), (v_codes, torch.uint8, 4), (k_params, torch.int32, 3), (v_params, torch.int32, 3)):
+        if t.dtype is not dtype or t.dim() != dims:
+            raise ValueError("codes are uint8 [n_layers][slots][H][d / 2], scales and zero points int32 [n_layers][slots][H]")
+    if (k_codes.shape != v_codes.shape or k_codes.stride() != v_codes.stride() or k_params.shape != v_params.shape
+            or k_params.stride() != v_params.stride() or k_codes.shape[:3] != k_params.shape or k_codes.stride(3) != 1):
+        raise ValueError("K and V are laid out alike, codes and their scales have the same layers, slots and heads, and a "
+                         "head's codes are contiguous")
+    if len({t.device for t in (k_codes, v_codes, k_params, v_params)}) != 1:
+        raise ValueError("the parts of a cache lie on one device")
+    c = KvqCache()
+    c.n_layers, c.total_slots, c.n_heads, c.head_dim = k_codes.shape[0], k_codes.shape[1], k_codes.shape[2], 2 * k_codes.shape[3]
+    c.device = k_codes.device.index if k_codes.is_cuda else -1
+    c.k_codes, c.v_codes, c.k_params, c.v_params = _ptr(k_codes), _ptr(v_codes), _ptr(k_params), _ptr(v_params)
+    c.layer_stride, c.slot_stride, c.head_stride = k_codes.stride()[:3]
+    c.param_layer_stride, c.param_slot_stride, c.param_head_stride = k_params.stride()
+    c.tensors = (k_codes, k_params, v_codes, v_params)
+    return c
+
+
+def empty_kvq_cache(n_layers: int, slots: int, n_heads: int, head_dim: int, device="cuda") -> KvqCache:
+    """A cache in 4 bits of its own memory: codes [n_layers][slots][H][d / 2], a head's scales and zero points slot after slot."""
+    codes = [torch.zeros((n_layers, slots, n_heads, head_dim // 2), dtype=torch.uint8, device=device) for _ in "kv"]
+    params = [torch.zeros((n_layers, n_heads, slots), dtype=torch.int32, device=device).transpose(1, 2) for _ in "kv"]
+    return make_kvq_cache(codes[0], params[0], codes[1], params[1])
+
+
+def _check_rows(k, v, cache):
+    if k.dtype is not torch.bfloat16 or v.dtype is not torch.bfloat16 or k.device != v.device:
+        raise ValueError("rows are bf16 tensors on one device")
+    if isinstance(cache, KvqCache) and cache.device >= 0 and k.get_device() != cache.device:
+        raise ValueError("rows and cache lie on one device")
+
+
+def ss_kvq_write(k_rows, v_rows, cache: KvqCache, kv_start, kv_len_in, n_rows=None, path=None, kv_capacity=None, kv_len_out=None,
+                 status=None, stream=None) -> None:
+    """Quantises rows into the cache, in every layer (asynchronous on `stream`).  k_rows, v_rows: bf16 [n_layers][B][rows][H][d] (d
+    contiguous); row r < n_rows[b] (int32 [B], None: all) goes to slot kv_start[b] + kv_len_in[b] + r, taken from row path[b][r]
+    where a path (int32 [B][SS_PATH_STRIDE], a verification's accept_path) is given; kv_len_out[b] = kv_len_in[b] + n_rows[b].
+    Sequences that do not fit are skipped; word 0 of `status` (a workspace) then says so."""
+    _check_rows(k_rows, v_rows, cache)
+    (_native or native()).kvq_write(k_rows, v_rows, cache, kv_start, kv_len_in, n_rows, path, kv_capacity, kv_len_out, status, stream)
+
+
+def ss_kvq_read(cache: KvqCache, k_rows, v_rows, kv_start, first=None, n_rows=None, stream=None) -> None:
+    """Rows of the cache as bf16, in every layer: k_rows[:, b, r] for r < n_rows[b] receives slot kv_start[b] + first[b] + r."""
+    _check_rows(k_rows, v_rows, cache)
+    (_native or native()).kvq_read(cache, k_rows, v_rows, kv_start, first, n_rows, stream)
+
+
+def make_kvq_attn_params(*, q_main, o_main, k_tree, v_tree, cache: KvqCache, kv_start, kv_len, trees, gamma, sm_scale, layer=0, q_spec=None,
+                         k_spec=None, v_spec=None, o_spec=None, kv_capacity=None, lse_main=None, lse_spec=None,
+                         workspace=None) -> KvqAttnParams:
+    """Fills ss_kvq_attn_params from tensors.  q_main, o_main, k_tree, v_tree: bf16 [B][Tmax][H][d]; *_spec: bf16
+    [B][Tmax][gamma][H][d]; contiguous, on the cache's device."""
+    B, Tmax, H, d = q_main.shape
+    if (H, d) != (cache.n_heads, cache.head_dim):
+        raise ValueError("the cache holds %d heads of %d, the queries have %d of %d" % (cache.n_heads, cache.head_dim, H, d))
+    main, spec = (B, Tmax, H, d), (B, Tmax, int(gamma), H, d)
+    for t, shape in ((q_main, main), (o_main, main), (k_tree, main), (v_tree, main), (q_spec, spec), (k_spec, spec), (v_spec, spec), (o_spec, spec)):
+        if t is not None and (t.dtype is not torch.bfloat16 or tuple(t.shape) != shape or not t.is_contiguous()):
+            raise ValueError("queries, outputs and the K/V of nodes and streams are contiguous bf16 tensors [B][Tmax][H][d] and [B][Tmax][gamma][H][d]")
+    for t, shape in ((lse_main, main[:-1]), (lse_spec, spec[:-1])):
+        if t is not None and (t.dtype is not torch.float32 or tuple(t.shape) != shape or not t.is_contiguous()):
+            raise ValueError("log-sum-exps are contiguous fp32 tensors [B][Tmax][H] and [B][Tmax][gamma][H]")
+    p = KvqAttnParams()
+    p.batch, p.gamma, p.max_nodes, p.layer, p.sm_scale = B, int(gamma), Tmax, int(layer), float(sm_scale)
+    p.q_main, p.o_main, p.k_tree, p.v_tree = _ptr(q_main), _ptr(o_main), _ptr(k_tree), _ptr(v_tree)
+    p.q_spec, p.k_spec, p.v_spec, p.o_spec = _ptr(q_spec), _ptr(k_spec), _ptr(v_spec), _ptr(o_spec)
+    p.cache = cache
+    p.kv_start, p.kv_len, p.kv_capacity, p.trees = _ptr(kv_start), _ptr(kv_len), _ptr(kv_capacity), _ptr(trees)
+    p.lse_main, p.lse_spec = _ptr(lse_main), _ptr(lse_spec)
+    p.workspace = _ptr(workspace)
+    p.workspace_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    return p
+
+
+def ss_msa_attention_kvq_workspace_bytes(p: KvqAttnParams) -> int:
+    return int(lib().ss_msa_attention_kvq_workspace_bytes(C.byref(p)))
+
+
+def ss_msa_attention_kvq(p: KvqAttnParams, stream: Optional[torch.cuda.Stream] = None) -> None:
+    """One layer of tree-masked multi-stream attention over a prefix in 4 bits (asynchronous on `stream`)."""
+    (_native or native()).msa_attention_kvq(p, stream)
 
 
 def ss_wait_selftest(workspace: torch.Tensor, stream=None) -> None:

@@ -2,6 +2,7 @@
 #pragma once
 #include <cuda_runtime.h>
 #include <stdint.h>
+#include <algorithm>
 
 #include "ss_msa.h"
 
@@ -26,6 +27,20 @@ inline int sm_count() {
         cached[dev] = n;
     }
     return cached[dev];
+}
+
+// A cache in 4 bits: what the host can see of it.
+inline int32_t kvq_check_cache(const ss_kvq_cache& c) {
+    if (!c.k_codes || !c.v_codes || !c.k_params || !c.v_params || c.n_layers < 1 || c.n_heads < 1 || c.total_slots < 0) return SS_ERR_INVALID_ARG;
+    if (c.head_dim != 64 && c.head_dim != 80 && c.head_dim != 128) return SS_ERR_UNSUPPORTED;
+    const uintptr_t unit = c.head_dim == 80 ? 7u : 15u;
+    if (((reinterpret_cast<uintptr_t>(c.k_codes) | reinterpret_cast<uintptr_t>(c.v_codes)) & unit) ||
+        ((reinterpret_cast<uintptr_t>(c.k_params) | reinterpret_cast<uintptr_t>(c.v_params)) & 3u))
+        return SS_ERR_INVALID_ARG;
+    if (static_cast<uintptr_t>(c.layer_stride | c.slot_stride | c.head_stride) & unit) return SS_ERR_UNSUPPORTED;
+    int dev = -1;
+    if (c.device >= 0 && (cudaGetDevice(&dev) != cudaSuccess || dev != c.device)) return SS_ERR_INVALID_ARG;
+    return SS_OK;
 }
 
 // Programmatic dependent launch.  A kernel launched with launch_after_previous may be scheduled while the

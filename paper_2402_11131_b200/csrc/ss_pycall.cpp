@@ -12,13 +12,15 @@
 
 namespace {
 
-PyObject *s_data_ptr, *s_shape, *s_nbytes, *s_cuda_stream;      // interned attribute names
+PyObject *s_data_ptr, *s_shape, *s_stride, *s_nbytes, *s_cuda_stream;      // interned attribute names
 PyObject *g_error, *g_raw_stream, *g_device;                    // SsError; torch's raw current stream and current device
-PyObject *g_attn_params, *g_cache_layout;                       // the ctypes structures of ss_attn_params and ss_cache_layout
+PyObject *g_attn_params, *g_cache_layout;                       // the ctypes structures of ss_attn_params and ss_cache_layout,
+PyObject *g_kvq_params, *g_kvq_cache;                           // of ss_kvq_attn_params and ss_kvq_cache
 // the entry points, in the order in which setup() takes them
 #define SS_FUNCTIONS(F)                                                                                                 \
     F(ss_msa_attention) F(ss_tree_verify) F(ss_tree_verify_soft) F(ss_tree_verify_sampled) F(ss_tree_prune)             \
-    F(ss_next_draft) F(ss_kv_compact) F(ss_stream_insert) F(ss_value_rotate)
+    F(ss_next_draft) F(ss_kv_compact) F(ss_stream_insert) F(ss_value_rotate)                                            \
+    F(ss_msa_attention_kvq) F(ss_kvq_write) F(ss_kvq_read)
 struct Functions {
 #define SS_MEMBER(name) decltype(&::name) name;
     SS_FUNCTIONS(SS_MEMBER)
@@ -51,6 +53,38 @@ struct Args {
             for (int k = 0; k < n; ++k) out[k] = PyLong_AsLongLong(PyTuple_GET_ITEM(s, k));
         }
         Py_XDECREF(s);
+    }
+    // the first n strides of argument i, in elements (after sizes(): the dimensions are known to be n)
+    void strides(int i, int n, long long* out) {
+        for (int k = 0; k < n; ++k) out[k] = 0;
+        if (!ok) return;
+        PyObject* s = PyObject_CallMethodNoArgs(a[i], s_stride);
+        ok = s && PyTuple_Check(s) && PyTuple_GET_SIZE(s) == n;
+        for (int k = 0; ok && k < n; ++k) out[k] = PyLong_AsLongLong(PyTuple_GET_ITEM(s, k));
+        if (!ok && !PyErr_Occurred()) PyErr_Format(PyExc_ValueError, "expected a tensor of %d dimensions", n);
+        Py_XDECREF(s);
+    }
+    // K and V rows [n_layers][batch][rows][n_heads][head_dim] of a cache in 4 bits
+    ss_kvq_rows rows(int k, int v, const ss_kvq_cache* cache) {
+        long long n[5], m[5], x[5], y[5];
+        ss_kvq_rows r = {};
+        sizes(k, 5, n);
+        sizes(v, 5, m);
+        strides(k, 5, x);
+        strides(v, 5, y);
+        r.k = ptr(k), r.v = ptr(v);
+        if (!ok) return r;
+        bool same = x[4] == 1 || n[4] <= 1;
+        for (int i = 0; i < 5; ++i) same = same && n[i] == m[i] && (x[i] == y[i] || n[i] <= 1);
+        if (!same || n[0] != cache->n_layers || n[3] != cache->n_heads || n[4] != cache->head_dim || n[1] > INT32_MAX || n[2] > INT32_MAX) {
+            PyErr_SetString(PyExc_ValueError, "expected rows [n_layers][batch][rows][n_heads][head_dim] of the cache's sizes, K and V laid out alike, "
+                                              "the last dimension contiguous");
+            ok = false;
+        }
+        // (a stride that is never used may have any value)
+        r.layer_stride = n[0] > 1 ? x[0] : 0, r.batch_stride = n[1] > 1 ? x[1] : 0, r.row_stride = n[2] > 1 ? x[2] : 0, r.head_stride = n[3] > 1 ? x[3] : 0;
+        r.batch = static_cast<int32_t>(n[1]), r.max_rows = static_cast<int32_t>(n[2]);
+        return r;
     }
     size_t nbytes(int i) {
         if (!ok) return 0;
@@ -255,9 +289,46 @@ SS_ENTRY(value_rotate, 4)
     return done("ss_value_rotate", st);
 }
 
+SS_ENTRY(msa_attention_kvq, 2)
+    Py_buffer view;
+    void* const s = a.stream(1);
+    const ss_kvq_attn_params* const p = a.structure<ss_kvq_attn_params>(0, g_kvq_params, &view);
+    SS_CALL(g_lib.ss_msa_attention_kvq(p, s))
+    PyBuffer_Release(&view);
+    return done("ss_msa_attention_kvq", st);
+}
+
+SS_ENTRY(kvq_write, 11)
+    Py_buffer view;
+    const int64_t* ks = a.as<int64_t>(3);
+    const int32_t *kl = a.as<int32_t>(4), *nr = a.as<int32_t>(5), *pa = a.as<int32_t>(6), *kc = a.as<int32_t>(7);
+    int32_t* ko = a.as<int32_t>(8);
+    void* const status = a.ptr(9);
+    void* const s = a.stream(10);
+    const ss_kvq_cache* const ca = a.structure<ss_kvq_cache>(2, g_kvq_cache, &view);
+    const ss_kvq_rows r = a.rows(0, 1, ca);
+    if (!a.ok && view.obj) PyBuffer_Release(&view);
+    SS_CALL(g_lib.ss_kvq_write(&r, ca, ks, kl, nr, pa, kc, ko, status, s))
+    PyBuffer_Release(&view);
+    return done("ss_kvq_write", st);
+}
+
+SS_ENTRY(kvq_read, 7)
+    Py_buffer view;
+    const int64_t* ks = a.as<int64_t>(3);
+    const int32_t *fi = a.as<int32_t>(4), *nr = a.as<int32_t>(5);
+    void* const s = a.stream(6);
+    const ss_kvq_cache* const ca = a.structure<ss_kvq_cache>(0, g_kvq_cache, &view);
+    const ss_kvq_rows r = a.rows(1, 2, ca);
+    if (!a.ok && view.obj) PyBuffer_Release(&view);
+    SS_CALL(g_lib.ss_kvq_read(ca, &r, ks, fi, nr, s))
+    PyBuffer_Release(&view);
+    return done("ss_kvq_read", st);
+}
+
 // setup(SsError, raw_stream(device) -> int, device() -> int, AttnParams, CacheLayout, ctypes.byref, ctypes.ArgumentError,
-//       addresses of SS_FUNCTIONS: a tuple of int)
-SS_ENTRY(setup, 8)
+//       addresses of SS_FUNCTIONS: a tuple of int, KvqAttnParams, KvqCache)
+SS_ENTRY(setup, 10)
     (void)a; (void)st;
     PyObject* const at = argv[7];
     Py_ssize_t n = 0;
@@ -268,15 +339,18 @@ SS_ENTRY(setup, 8)
     ++n;
     SS_FUNCTIONS(SS_TAKE)
     g_lib = lib;
-    PyObject** const kept[7] = {&g_error, &g_raw_stream, &g_device, &g_attn_params, &g_cache_layout, &g_byref, &g_argument_error};
-    for (int i = 0; i < 7; ++i) Py_XSETREF(*kept[i], Py_NewRef(argv[i]));
+    PyObject** const kept[10] = {&g_error, &g_raw_stream, &g_device, &g_attn_params, &g_cache_layout, &g_byref, &g_argument_error, nullptr, &g_kvq_params,
+                                 &g_kvq_cache};
+    for (int i = 0; i < 10; ++i)
+        if (kept[i]) Py_XSETREF(*kept[i], Py_NewRef(argv[i]));
     Py_RETURN_NONE;
 }
 
 #define SS_METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {SS_METHOD(setup), SS_METHOD(msa_attention), SS_METHOD(tree_verify), SS_METHOD(tree_verify_soft),
                          SS_METHOD(tree_verify_sampled), SS_METHOD(tree_prune), SS_METHOD(next_draft), SS_METHOD(kv_compact),
-                         SS_METHOD(stream_insert), SS_METHOD(value_rotate), {nullptr, nullptr, 0, nullptr}};
+                         SS_METHOD(stream_insert), SS_METHOD(value_rotate), SS_METHOD(msa_attention_kvq), SS_METHOD(kvq_write),
+                         SS_METHOD(kvq_read), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_pycall", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
@@ -284,6 +358,7 @@ PyModuleDef module = {PyModuleDef_HEAD_INIT, "_pycall", nullptr, -1, methods, nu
 PyMODINIT_FUNC PyInit__pycall() {
     s_data_ptr = PyUnicode_InternFromString("data_ptr");
     s_shape = PyUnicode_InternFromString("shape");
+    s_stride = PyUnicode_InternFromString("stride");
     s_nbytes = PyUnicode_InternFromString("nbytes");
     s_cuda_stream = PyUnicode_InternFromString("cuda_stream");
     return PyModule_Create(&module);
