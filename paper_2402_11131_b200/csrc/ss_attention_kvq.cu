@@ -23,14 +23,20 @@ struct alignas(16) KvqArgs {
 };
 
 // ---- work ---------------------------------------------------------------------------------------
-// A unit is a block of query rows of one head of one sequence; its keys are cut in chunks of 32: the cached slots, then the tree's
-// nodes and the stream keys of the block's own nodes.  All units' chunks, in order of sequence, head and block, are one line that
-// is cut into equal pieces, one per CTA: a CTA takes the end of a unit, whole units, and the beginning of another.  So every CTA
-// reads the same amount, whatever the lengths (which only the device knows).
+// A unit is a block of query rows of HW neighbouring heads of one sequence.  Its keys are cut in chunks of 32: the cached slots, then
+// the tree's nodes and the stream keys of the block's own nodes.  A CTA's eight warps take HW heads and 8 / HW chunks of each at a time,
+// a step.  All units' steps, in order of sequence, heads and block, are one line that is cut into equal pieces, one per CTA: a CTA
+// takes the end of a unit, whole units, and the beginning of another.  So every CTA reads the same amount, whatever the lengths (which
+// only the device knows).
+// HW: a CTA that reads eight neighbouring heads of a slot reads 512 bytes in a row where slots are the outer dimension of the cache
+// (one head's 64 bytes at a time kept DRAM at 2.4 TB/s), and its warps have nothing to join.  Where there are only a few
+// steps for each CTA, one head's keys over all warps leave fewer partial results to join.
 constexpr int kChunk = 32;
+constexpr int kWarps = 4, kWarpsLog2 = 2, kThreads = 32 * kWarps;
+constexpr int kStepsForHeads = 6;
 
 struct Seq {
-    int L, T, rows, blocks, chunks;                  // chunks of one unit: cached ones and those behind
+    int L, T, rows, blocks, chunks;                  // rows and blocks of rows per head, chunks of each: cached ones and those behind
     long long start;
 };
 
@@ -46,7 +52,7 @@ __host__ __device__ __forceinline__ int extra_chunks(int T, int gamma, int block
     return (T + stream + kChunk - 1) / kChunk;
 }
 
-// One sequence as the call gives it.  A sequence that cannot be run has no units.
+// One sequence as the call gives it.  A sequence that cannot be run has no blocks.
 template <int ROWS>
 __device__ __forceinline__ Seq load_seq(const KvqArgs& a, int b) {
     Seq s;
@@ -62,6 +68,24 @@ __device__ __forceinline__ Seq load_seq(const KvqArgs& a, int b) {
         s.chunks = prefix_chunks(s.L) + extra_chunks(s.T, a.gamma, ROWS);
     }
     return s;
+}
+
+// Heads per CTA (its log2) for `chunks` chunks and `blocks` blocks of one head: as many as eight where every CTA then has some steps,
+// at most an eighth of the warps have no head, and a unit is not cut in more than some ten pieces
+__device__ __forceinline__ int heads_log2(const KvqArgs& a, long long chunks, long long blocks) {
+    if (chunks * a.n_heads < static_cast<long long>(kStepsForHeads) * kWarps * gridDim.x) return 0;
+    int lg = kWarpsLog2;
+    while (lg > 0 && (8 * ((a.n_heads + (1 << lg) - 1) >> lg << lg) > 9 * a.n_heads || 10 * blocks * (a.n_heads >> lg) < gridDim.x)) --lg;
+    return lg;
+}
+
+__device__ __forceinline__ long long warp_sum(long long x) {
+    #pragma unroll 1
+    for (int i = 16; i > 0; i >>= 1) x += __shfl_xor_sync(0xffffffffu, x, i);
+    return x;
+}
+__device__ __forceinline__ long long divide(long long a, long long b) {
+    return (a >> 32) == 0 && (b >> 32) == 0 ? static_cast<long long>(static_cast<uint32_t>(a) / static_cast<uint32_t>(b)) : a / b;
 }
 
 // Row r of a unit's sequence: its node and stream (-1: main stream)
@@ -83,10 +107,9 @@ __device__ __forceinline__ long long row_offset(const KvqArgs& a, int hd, int b,
 // ---- small helpers ------------------------------------------------------------------------------
 __device__ __forceinline__ uint32_t smem_addr(const void* p) { return static_cast<uint32_t>(__cvta_generic_to_shared(p)); }
 template <int BYTES>
-__device__ __forceinline__ void copy_async(uint32_t dst, const void* src, bool real) {
-    const int n = real ? BYTES : 0;                  // (nothing is read where n is 0: the destination is filled with zeros)
-    if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
-    else asm volatile("cp.async.ca.shared.global [%0], [%1], %2, %3;" ::"r"(dst), "l"(src), "n"(BYTES), "r"(n) : "memory");
+__device__ __forceinline__ void copy_async(uint32_t dst, const void* src) {
+    if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+    else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(dst), "l"(src), "n"(BYTES) : "memory");
 }
 __device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
@@ -128,21 +151,30 @@ __device__ __forceinline__ void mma_bf16(float (&d)[4], uint32_t a0, uint32_t a1
         : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
-// Codes to bf16.  0x4300 is 128 in bf16, whose last mantissa bit is worth 1: a code or'd into it is 128 + c, and 128 + z subtracted
-// from that leaves c - z, exactly.
-__device__ __forceinline__ uint32_t with_magic(uint32_t x) {
+// Codes as fp16 operands without any arithmetic: a code in the last four mantissa bits of a half word is the subnormal number c 2^-24,
+// one in the four bits above them 16 c 2^-24, exactly, and MMAs take subnormal numbers at full value.  So a mask is all it takes, and a
+// shift by 8 for the other two codes of a half word; the powers of two, and the zero points, are dealt with where sums begin and end.
+__device__ __forceinline__ uint32_t low_codes(uint32_t w) { return w & 0x000f000fu; }
+__device__ __forceinline__ uint32_t high_codes(uint32_t w) { return w & 0x00f000f0u; }
+__device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t pack2_f16(float lo, float hi) {
     uint32_t r;
-    asm("lop3.b32 %0, %1, 0x000f000f, 0x43004300, 0xea;" : "=r"(r) : "r"(x));     // (x & mask) | magic
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
     return r;
 }
-__device__ __forceinline__ uint32_t sub_bf16x2(uint32_t a, uint32_t b) {
+__device__ __forceinline__ uint32_t times16_bf16x2(uint32_t x) {
     uint32_t r;
-    asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(x), "r"(0x41804180u));
     return r;
 }
-__device__ __forceinline__ uint32_t zero_pair(uint32_t word) { return with_magic(__byte_perm(word, 0u, 0x3232)); }          // one key's
-__device__ __forceinline__ uint32_t zero_pair(uint32_t a, uint32_t b) { return with_magic(__byte_perm(a, b, 0x7632)); }     // two keys'
+__device__ __forceinline__ uint32_t zero_pair(uint32_t a, uint32_t b) { return low_codes(__byte_perm(a, b, 0x7632)); }     // of two keys
 __device__ __forceinline__ float scale_of(uint32_t word) { return __uint_as_float(word << 16); }
+__device__ __forceinline__ float zero_over_16(uint32_t word) { return __uint_as_float(((word & 0xf0000u) << 3) | 0x3f800000u); }     // 1 + z / 16
+constexpr float kCode = 5.9604644775390625e-08f;                 // 2^-24: what a code counts in an MMA
 
 // ---- the kernel ---------------------------------------------------------------------------------
 // S^T = K Q^T and O^T = V^T P^T on mma.sync m16n8k16 with the keys (the dimensions) as the 16 rows of A and NG groups of 8 query
@@ -164,7 +196,7 @@ struct KvqGeometry {
     static constexpr int kCopy = D == 80 ? 8 : 16;               // bytes per asynchronous copy
     static constexpr int kCodeBytes = kChunk * kRowBytes;
     static constexpr int kStageBytes = 2 * kCodeBytes + 2 * kChunk * 4;
-    static constexpr int kStages = 3, kWarps = 8;
+    static constexpr int kStages = 4;
     static constexpr int kRingBytes = kStages * kStageBytes;
 };
 
@@ -173,34 +205,42 @@ struct KvqSmem {
     using G = KvqGeometry<D>;
     static constexpr int kRows = 8 * NG;
     static constexpr int kPad = D + 4;                           // floats per row of a warp's partial result
-    static constexpr int kRing = G::kWarps * G::kRingBytes;
-    static constexpr int kJoin = G::kWarps * kRows * kPad * 4;
-    static constexpr int kBytes = (kRing > kJoin ? kRing : kJoin) + G::kWarps * kRows * 8;
+    static constexpr int kRing = kWarps * G::kRingBytes;
+    static constexpr int kJoin = kWarps * kRows * kPad * 4;
+    static constexpr int kBytes = (kRing > kJoin ? kRing : kJoin) + kWarps * kRows * 8;
 };
 
-// floats of a CTA's partial result in the workspace: per row D sums, the reference and the sum of weights
-__host__ __device__ constexpr int partial_floats(int D, int rows) { return rows * (D + 4); }
+// floats of a CTA's partial result in the workspace: per head and row D sums, the reference and the sum of weights
+__host__ __device__ constexpr int partial_floats(int D, int rows) { return kWarps * rows * (D + 4); }
 
+// One warp's share.
+// Queries enter as fp16: x = q 2^-e, the row's largest |x| in [2^14, 2^15).  A bf16 has 8 significant bits, so x is exact down to 2^-28 of
+// the row's largest element (dimensions that meet codes counting 16 times as much are taken as x / 16), and off by at most 2^-36 of
+// that below.
+// Weights enter as fp16: p s_v 2^(6 - r), r the exponent of the largest V scale so far.  p is at most 2^8, so nothing overflows; a weight
+// keeps 11 bits down to 2^-20 of what the reference would weigh, and is off by at most 2^-31 2^r below.
+// o: sums of V's codes (tiles of odd number: 16 times that); zo: the same sum of zero points, which is what is to be subtracted.
 template <int D, int NG>
 struct WarpState {
-    float o[D / 16][NG][4];
+    float o[D / 16][NG][4], zo[NG][4];
     float ref[NG][2], sum[NG][2];
     uint32_t q[D / 16][NG][2];
+    float start[NG][2], factor[NG][2];               // of the lane's two rows: 16 sum(x) 2^-24; 2^24 2^e scale
+    float weight;                                    // 2^(6 - r)
+    float limit;                                     // V scales from here on raise r; 0: none seen yet
 };
 
-// Raises the references to the maxima of the scores t (rare: only when one exceeds its reference by more than 2^8)
+// Moves the references by `by` (log2 units)
 template <int D, int NG>
-__device__ __forceinline__ void raise_refs(WarpState<D, NG>& w, const float (&t)[2][NG][4]) {
+__device__ __forceinline__ void move_refs(WarpState<D, NG>& w, const float (&by)[NG][2]) {
     #pragma unroll
     for (int n = 0; n < NG; ++n) {
         #pragma unroll
         for (int e = 0; e < 2; ++e) {
-            float m = fmaxf(fmaxf(t[0][n][e], t[0][n][2 + e]), fmaxf(t[1][n][e], t[1][n][2 + e]));
-            #pragma unroll
-            for (int x = 4; x < 32; x <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, x));
-            const float old = w.ref[n][e], now = fmaxf(old, m), f = exp2_approx(old - now);
-            w.ref[n][e] = now;
+            const float f = exp2_approx(-by[n][e]);
+            w.ref[n][e] += by[n][e];
             w.sum[n][e] *= f;
+            w.zo[n][e] *= f;
             #pragma unroll
             for (int k = 0; k < D / 16; ++k) {
                 w.o[k][n][e] *= f;
@@ -210,54 +250,82 @@ __device__ __forceinline__ void raise_refs(WarpState<D, NG>& w, const float (&t)
     }
 }
 
-constexpr float kNoRef = -FLT_MAX / 2;               // below every score that counts; masked scores are -inf
-
-// Scores t (log2 units, masked ones -inf) of two tiles of 16 keys to P^T fragments; sv: V scales of the lane's keys
+// Raises r to the exponent of a V scale
 template <int D, int NG>
-__device__ __forceinline__ void softmax_chunk(WarpState<D, NG>& w, const float (&t)[2][NG][4], const float (&sv)[2][2], uint32_t (&p)[2][NG][2]) {
-    bool high = false;
+__device__ __forceinline__ void raise_scale(WarpState<D, NG>& w, float scale) {
+    const uint32_t r = min(max(__float_as_uint(scale) >> 23, 32u), 240u);
+    const float now = __uint_as_float((254u + 6u - r) << 23), f = now * __uint_as_float((254u << 23) - __float_as_uint(w.weight));   // (powers of two)
+    w.weight = now;
+    w.limit = __uint_as_float((r + 1u) << 23);
     #pragma unroll
     for (int n = 0; n < NG; ++n) {
         #pragma unroll
-        for (int e = 0; e < 2; ++e)
-            high |= fmaxf(fmaxf(t[0][n][e], t[0][n][2 + e]), fmaxf(t[1][n][e], t[1][n][2 + e])) > w.ref[n][e] + 8.f;
+        for (int i = 0; i < 4; ++i) {
+            w.zo[n][i] *= f;
+            #pragma unroll
+            for (int k = 0; k < D / 16; ++k) w.o[k][n][i] *= f;
+        }
     }
-    if (__any_sync(0xffffffffu, high)) raise_refs<D, NG>(w, t);
+}
+
+constexpr float kNoRef = -FLT_MAX / 2;               // reference of a partial result that has seen no key
+
+// Scores above their references (d, log2 units; -inf: not seen) of H tiles of 16 keys: where one is more than 8 above, references are
+// raised to the maxima and d lowered by as much.  A row that has seen no key so far takes the maximum whatever it is: so the first chunk
+// always comes here, by its V scales (no limit holds yet) or, `first`, because it is not a cached one.  `top`: the largest V scale.
+template <int D, int NG, int H>
+__device__ __forceinline__ void keep_in_range(WarpState<D, NG>& w, float (&d)[H][NG][4], float top, bool first) {
+    float most = d[0][0][0];
     #pragma unroll
-    for (int j = 0; j < 2; ++j) {
+    for (int j = 0; j < H; ++j) {
+        #pragma unroll
+        for (int n = 0; n < NG; ++n) most = fmaxf(fmaxf(fmaxf(most, d[j][n][0]), fmaxf(d[j][n][1], d[j][n][2])), d[j][n][3]);
+    }
+    if (__any_sync(0xffffffffu, most > 8.f || top >= w.limit || first)) {
+        float by[NG][2];
         #pragma unroll
         for (int n = 0; n < NG; ++n) {
-            float x[4];
             #pragma unroll
-            for (int i = 0; i < 4; ++i) x[i] = exp2_approx(t[j][n][i] - w.ref[n][i & 1]);
-            w.sum[n][0] += x[0] + x[2];
-            w.sum[n][1] += x[1] + x[3];
-            // (a weight of zero stays zero whatever the scale: what is masked may have any)
-            #pragma unroll
-            for (int i = 0; i < 4; ++i) x[i] = x[i] == 0.f ? 0.f : x[i] * sv[j][i >> 1];
-            p[j][n][0] = transpose_8x8(pack2_bf16(x[0], x[1]));
-            p[j][n][1] = transpose_8x8(pack2_bf16(x[2], x[3]));
+            for (int e = 0; e < 2; ++e) {
+                float m = -INFINITY, seen = w.sum[n][e];
+                #pragma unroll
+                for (int j = 0; j < H; ++j) m = fmaxf(m, fmaxf(d[j][n][e], d[j][n][2 + e]));
+                #pragma unroll
+                for (int x = 4; x < 32; x <<= 1) {
+                    m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, x));
+                    seen += __shfl_xor_sync(0xffffffffu, seen, x);
+                }
+                m = seen == 0.f ? (m == -INFINITY ? 0.f : m) : fmaxf(m, 0.f);
+                by[n][e] = m;
+                #pragma unroll
+                for (int j = 0; j < H; ++j) d[j][n][e] -= m, d[j][n][2 + e] -= m;
+            }
         }
+        move_refs<D, NG>(w, by);
+        #pragma unroll
+        for (int x = 16; x > 0; x >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
+        if (top >= w.limit) raise_scale<D, NG>(w, top);
     }
 }
 
 __device__ __forceinline__ int key_of(int g) { return 4 * (g & 1) + (g >> 1); }
 
-// One chunk of 32 cached slots, of which the first `valid` count
+// One chunk of 32 cached slots, of which the first `valid` count: lane offsets kl (codes of K), vl (of V), pl (words of its keys), zl
 template <int D, int NG>
-__device__ __forceinline__ void prefix_chunk(WarpState<D, NG>& w, uint32_t stage, int valid, float scale, int g, int c) {
+__device__ __forceinline__ void prefix_chunk(WarpState<D, NG>& w, uint32_t stage, int valid, uint32_t kl, uint32_t vl, uint32_t pl, uint32_t zl, int g, int c) {
     using G = KvqGeometry<D>;
-    const uint32_t ks = stage, vs = stage + G::kCodeBytes, kp = stage + 2 * G::kCodeBytes, vp = kp + 4 * kChunk;
-    float t[2][NG][4], sv[2][2];
+    constexpr uint32_t kWordsOfV = 4 * kChunk;
+    uint32_t pa[2], pb[2];
+    float d[2][NG][4];
+    // Scores.  With X = sum(x), sum x (c - z) = sum x c + 16 X - (1 + z / 16) 16 X: the second term is what the accumulators start
+    // from, and 1 + z / 16 is the zero point or'd into a float.
     #pragma unroll
     for (int j = 0; j < 2; ++j) {
-        const int key = 16 * j + key_of(g);
-        const uint32_t pa = lds32(kp + 4 * key), pb = lds32(kp + 4 * key + 32);
-        sv[j][0] = scale_of(lds32(vp + 4 * key));
-        sv[j][1] = scale_of(lds32(vp + 4 * key + 32));
-        const uint32_t za = zero_pair(pa), zb = zero_pair(pb);
+        pa[j] = lds32(stage + pl + 64 * j), pb[j] = lds32(stage + pl + 64 * j + 32);
+        #pragma unroll
+        for (int n = 0; n < NG; ++n) d[j][n][0] = d[j][n][2] = w.start[n][0], d[j][n][1] = d[j][n][3] = w.start[n][1];
+        const uint32_t row = stage + kl + j * 16 * G::kRowBytes;
         uint32_t wa[4], wb[4];
-        const uint32_t row = ks + key * G::kRowBytes + c * (4 * G::kWordsK);
         if constexpr (G::kWordsK == 4) {
             const uint4 x = lds128(row), y = lds128(row + 8 * G::kRowBytes);
             wa[0] = x.x, wa[1] = x.y, wa[2] = x.z, wa[3] = x.w;
@@ -266,31 +334,36 @@ __device__ __forceinline__ void prefix_chunk(WarpState<D, NG>& w, uint32_t stage
             const uint2 x = lds64(row), y = lds64(row + 8 * G::kRowBytes);
             wa[0] = x.x, wa[1] = x.y, wb[0] = y.x, wb[1] = y.y;
         }
-        float acc[NG][4] = {};
         #pragma unroll
         for (int i = 0; i < G::kWordsK; ++i) {
             #pragma unroll
             for (int s = 0; s < 2; ++s) {
-                const uint32_t a0 = sub_bf16x2(with_magic(wa[i] >> (8 * s)), za), a2 = sub_bf16x2(with_magic(wa[i] >> (8 * s + 4)), za);
-                const uint32_t a1 = sub_bf16x2(with_magic(wb[i] >> (8 * s)), zb), a3 = sub_bf16x2(with_magic(wb[i] >> (8 * s + 4)), zb);
+                const uint32_t u = wa[i] >> (8 * s), v = wb[i] >> (8 * s);
                 #pragma unroll
-                for (int n = 0; n < NG; ++n) mma_bf16(acc[n], a0, a1, a2, a3, w.q[2 * i + s][n][0], w.q[2 * i + s][n][1]);
+                for (int n = 0; n < NG; ++n)
+                    mma_f16(d[j][n], low_codes(u), low_codes(v), high_codes(u), high_codes(v), w.q[2 * i + s][n][0], w.q[2 * i + s][n][1]);
             }
         }
         if constexpr (D == 80) {
-            const uint32_t tail = ks + key * G::kRowBytes + 32;
+            const uint32_t tail = stage + kl - c * (4 * G::kWordsK) + j * 16 * G::kRowBytes + 32;
             const uint2 x = lds64(tail), y = lds64(tail + 8 * G::kRowBytes);
-            const uint32_t a0 = sub_bf16x2(with_magic(x.x >> (4 * c)), za), a2 = sub_bf16x2(with_magic(x.y >> (4 * c)), za);
-            const uint32_t a1 = sub_bf16x2(with_magic(y.x >> (4 * c)), zb), a3 = sub_bf16x2(with_magic(y.y >> (4 * c)), zb);
             #pragma unroll
-            for (int n = 0; n < NG; ++n) mma_bf16(acc[n], a0, a1, a2, a3, w.q[4][n][0], w.q[4][n][1]);
+            for (int n = 0; n < NG; ++n)
+                mma_f16(d[j][n], low_codes(x.x >> (4 * c)), low_codes(y.x >> (4 * c)), low_codes(x.y >> (4 * c)), low_codes(y.y >> (4 * c)), w.q[4][n][0], w.q[4][n][1]);
         }
-        const float sa = scale_of(pa) * scale, sb = scale_of(pb) * scale;
+    }
+    #pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        const float sa = scale_of(pa[j]), sb = scale_of(pb[j]), za = zero_over_16(pa[j]), zb = zero_over_16(pb[j]);
         #pragma unroll
         for (int n = 0; n < NG; ++n) {
             #pragma unroll
-            for (int i = 0; i < 4; ++i) t[j][n][i] = acc[n][i] * (i < 2 ? sa : sb);
+            for (int i = 0; i < 4; ++i) {
+                const float u = fmaf(i < 2 ? za : zb, -w.start[n][i & 1], d[j][n][i]) * (i < 2 ? sa : sb);
+                d[j][n][i] = fmaf(u, w.factor[n][i & 1], -w.ref[n][i & 1]);
+            }
         }
+        pa[j] = lds32(stage + pl + kWordsOfV + 64 * j), pb[j] = lds32(stage + pl + kWordsOfV + 64 * j + 32);
     }
     if (valid < kChunk) {
         #pragma unroll
@@ -300,17 +373,29 @@ __device__ __forceinline__ void prefix_chunk(WarpState<D, NG>& w, uint32_t stage
             for (int n = 0; n < NG; ++n) {
                 #pragma unroll
                 for (int i = 0; i < 4; ++i)
-                    if (key + (i < 2 ? 0 : 8) >= valid) t[j][n][i] = -INFINITY;
+                    if (key + (i < 2 ? 0 : 8) >= valid) d[j][n][i] = -INFINITY;
             }
         }
     }
-    uint32_t p[2][NG][2];
-    softmax_chunk<D, NG>(w, t, sv, p);
+    keep_in_range<D, NG, 2>(w, d, fmaxf(fmaxf(scale_of(pa[0]), scale_of(pb[0])), fmaxf(scale_of(pa[1]), scale_of(pb[1]))), false);
     #pragma unroll
     for (int j = 0; j < 2; ++j) {
-        const uint32_t pz = vp + 4 * (16 * j + c);
+        uint32_t p[NG][2];
+        const float sa = scale_of(pa[j]) * w.weight, sb = scale_of(pb[j]) * w.weight;
+        #pragma unroll
+        for (int n = 0; n < NG; ++n) {
+            const float x0 = exp2_approx(d[j][n][0]), x1 = exp2_approx(d[j][n][1]), x2 = exp2_approx(d[j][n][2]), x3 = exp2_approx(d[j][n][3]);
+            w.sum[n][0] += x0 + x2;
+            w.sum[n][1] += x1 + x3;
+            p[n][0] = transpose_8x8(pack2_f16(x0 * sa, x1 * sa));
+            p[n][1] = transpose_8x8(pack2_f16(x2 * sb, x3 * sb));
+        }
+        // O^T += V^T P^T
+        const uint32_t pz = stage + zl + 64 * j;
         const uint32_t z01 = zero_pair(lds32(pz), lds32(pz + 16)), z23 = zero_pair(lds32(pz + 32), lds32(pz + 48));
-        const uint32_t row = vs + (16 * j + c) * G::kRowBytes + g * (4 * G::kWordsV);
+        #pragma unroll
+        for (int n = 0; n < NG; ++n) mma_f16(w.zo[n], z01, z01, z23, z23, p[n][0], p[n][1]);
+        const uint32_t row = stage + vl + j * 16 * G::kRowBytes;
         uint32_t v[4][2];
         #pragma unroll
         for (int k = 0; k < 4; ++k) {
@@ -327,10 +412,11 @@ __device__ __forceinline__ void prefix_chunk(WarpState<D, NG>& w, uint32_t stage
             const uint32_t l23 = __byte_perm(v[2][i], v[3][i], 0x5410), h23 = __byte_perm(v[2][i], v[3][i], 0x7632);
             #pragma unroll
             for (int s = 0; s < 4; ++s) {
-                const uint32_t a0 = sub_bf16x2(with_magic(l01 >> (4 * s)), z01), a1 = sub_bf16x2(with_magic(h01 >> (4 * s)), z01);
-                const uint32_t a2 = sub_bf16x2(with_magic(l23 >> (4 * s)), z23), a3 = sub_bf16x2(with_magic(h23 >> (4 * s)), z23);
+                const int sh = 8 * (s >> 1);
+                const auto codes = [&](uint32_t x) { return s & 1 ? high_codes(x >> sh) : low_codes(x >> sh); };
+                const uint32_t a0 = codes(l01), a1 = codes(h01), a2 = codes(l23), a3 = codes(h23);
                 #pragma unroll
-                for (int n = 0; n < NG; ++n) mma_bf16(w.o[4 * i + s][n], a0, a1, a2, a3, p[j][n][0], p[j][n][1]);
+                for (int n = 0; n < NG; ++n) mma_f16(w.o[4 * i + s][n], a0, a1, a2, a3, p[n][0], p[n][1]);
             }
         }
         if constexpr (D == 80) {
@@ -338,13 +424,11 @@ __device__ __forceinline__ void prefix_chunk(WarpState<D, NG>& w, uint32_t stage
             const int sh = 4 * (g >> 1) + 16 * (g & 1);
             uint2 x[4];
             #pragma unroll
-            for (int k = 0; k < 4; ++k) x[k] = lds64(vs + (16 * j + c + 4 * k) * G::kRowBytes + 32);
-            const uint32_t a0 = sub_bf16x2(with_magic((x[0].x >> sh & 0xfu) | (x[1].x >> sh) << 16), z01);
-            const uint32_t a1 = sub_bf16x2(with_magic((x[0].y >> sh & 0xfu) | (x[1].y >> sh) << 16), z01);
-            const uint32_t a2 = sub_bf16x2(with_magic((x[2].x >> sh & 0xfu) | (x[3].x >> sh) << 16), z23);
-            const uint32_t a3 = sub_bf16x2(with_magic((x[2].y >> sh & 0xfu) | (x[3].y >> sh) << 16), z23);
+            for (int k = 0; k < 4; ++k) x[k] = lds64(row - g * (4 * G::kWordsV) + 32 + 4 * k * G::kRowBytes);
+            const uint32_t a0 = low_codes((x[0].x >> sh & 0xfu) | (x[1].x >> sh) << 16), a1 = low_codes((x[0].y >> sh & 0xfu) | (x[1].y >> sh) << 16);
+            const uint32_t a2 = low_codes((x[2].x >> sh & 0xfu) | (x[3].x >> sh) << 16), a3 = low_codes((x[2].y >> sh & 0xfu) | (x[3].y >> sh) << 16);
             #pragma unroll
-            for (int n = 0; n < NG; ++n) mma_bf16(w.o[4][n], a0, a1, a2, a3, p[j][n][0], p[j][n][1]);
+            for (int n = 0; n < NG; ++n) mma_f16(w.o[4][n], a0, a1, a2, a3, p[n][0], p[n][1]);
         }
     }
 }
@@ -355,123 +439,175 @@ struct Extra {
     int row0, rows;                                  // of the block; rows of the sequence
 };
 
-__device__ __forceinline__ const __nv_bfloat16* extra_key(const KvqArgs& a, const Extra& x, int D, int b, int h, int e, bool value) {
-    if (e < x.T) return (value ? a.v_tree : a.k_tree) + row_offset(a, D, b, h, Row{e, -1});
-    const int s = e - x.T;
-    return (value ? a.v_spec : a.k_spec) + row_offset(a, D, b, h, Row{x.t0 + s / x.gamma, s % x.gamma});
+// Row r of a head's query rows, or null behind the last one
+template <int D>
+__device__ __forceinline__ const __nv_bfloat16* query_row(const KvqArgs& a, int T, int rows, int b, int h, int r) {
+    if (r >= rows || h >= a.n_heads) return nullptr;
+    const Row x = row_of(r, T, a.gamma);
+    return (x.j < 0 ? a.q_main : a.q_spec) + row_offset(a, D, b, h, x);
 }
 
-// One chunk of 32 keys behind the prefix, from `first` on
+// Where key e lies in k_tree / v_tree or k_spec / v_spec (elements)
+__device__ __forceinline__ long long extra_offset(const KvqArgs& a, const Extra& x, int D, int b, int h, int e) {
+    if (e < x.T) return row_offset(a, D, b, h, Row{e, -1});
+    const int s = e - x.T;
+    return row_offset(a, D, b, h, Row{x.t0 + s / x.gamma, s % x.gamma});
+}
+
+// Scores above their references of 16 keys behind the prefix, from `first` on; what a row does not see is -inf
 template <int D, int NG>
-__device__ __forceinline__ void extra_chunk(WarpState<D, NG>& w, const KvqArgs& a, const Extra& x, int b, int h, int first, int g, int c) {
+__device__ __forceinline__ void extra_scores(const WarpState<D, NG>& w, float (&acc)[NG][4], const KvqArgs& a, const Extra& x, int b, int h, int first, int g, int c) {
     using G = KvqGeometry<D>;
-    float t[2][NG][4];
-    const float one[2][2] = {{1.f, 1.f}, {1.f, 1.f}};
+    const int ea = first + key_of(g), eb = ea + 8;
+    const __nv_bfloat16* ka = (ea < x.T ? a.k_tree : a.k_spec) + (ea < x.count ? extra_offset(a, x, D, b, h, ea) : 0);
+    const __nv_bfloat16* kb = (eb < x.T ? a.k_tree : a.k_spec) + (eb < x.count ? extra_offset(a, x, D, b, h, eb) : 0);
+    const __nv_bfloat16* q[NG];                      // the rows of B: row g of every group
     #pragma unroll
-    for (int j = 0; j < 2; ++j) {
-        const int ea = first + 16 * j + key_of(g), eb = ea + 8;
-        const __nv_bfloat16* ka = ea < x.count ? extra_key(a, x, D, b, h, ea, false) : nullptr;
-        const __nv_bfloat16* kb = eb < x.count ? extra_key(a, x, D, b, h, eb, false) : nullptr;
-        float acc[NG][4] = {};
-        #pragma unroll
-        for (int i = 0; i < G::kWordsK; ++i) {
-            uint4 u = {}, v = {};
-            if (ka) u = *reinterpret_cast<const uint4*>(ka + c * (8 * G::kWordsK) + 8 * i);
-            if (kb) v = *reinterpret_cast<const uint4*>(kb + c * (8 * G::kWordsK) + 8 * i);
-            #pragma unroll
-            for (int n = 0; n < NG; ++n) {
-                mma_bf16(acc[n], u.x, v.x, u.y, v.y, w.q[2 * i][n][0], w.q[2 * i][n][1]);
-                mma_bf16(acc[n], u.z, v.z, u.w, v.w, w.q[2 * i + 1][n][0], w.q[2 * i + 1][n][1]);
-            }
-        }
-        if constexpr (D == 80) {
-            uint32_t u[4] = {};
-            if (ka) u[0] = *reinterpret_cast<const uint32_t*>(ka + 64 + 2 * c), u[2] = *reinterpret_cast<const uint32_t*>(ka + 72 + 2 * c);
-            if (kb) u[1] = *reinterpret_cast<const uint32_t*>(kb + 64 + 2 * c), u[3] = *reinterpret_cast<const uint32_t*>(kb + 72 + 2 * c);
-            #pragma unroll
-            for (int n = 0; n < NG; ++n) mma_bf16(acc[n], u[0], u[1], u[2], u[3], w.q[4][n][0], w.q[4][n][1]);
-        }
+    for (int n = 0; n < NG; ++n) q[n] = query_row<D>(a, x.T, x.rows, b, h, x.row0 + 8 * n + g);
+    #pragma unroll
+    for (int n = 0; n < NG; ++n) acc[n][0] = acc[n][1] = acc[n][2] = acc[n][3] = 0.f;
+    #pragma unroll
+    for (int i = 0; i < G::kWordsK; ++i) {
+        uint4 u = {}, v = {};
+        if (ea < x.count) u = *reinterpret_cast<const uint4*>(ka + c * (8 * G::kWordsK) + 8 * i);
+        if (eb < x.count) v = *reinterpret_cast<const uint4*>(kb + c * (8 * G::kWordsK) + 8 * i);
         #pragma unroll
         for (int n = 0; n < NG; ++n) {
-            #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                const int r = x.row0 + 8 * n + 2 * c + e;
-                unsigned long long see = 0;
-                int lo = 0, hi = 0;                  // stream keys the row sees
-                if (r < x.rows) {
-                    const Row q = row_of(r, x.T, x.gamma);
-                    see = a.trees[b].anc_mask[q.t];
-                    lo = x.T + (q.t - x.t0) * x.gamma;
-                    hi = q.j < 0 ? lo : lo + q.j + 1;
-                }
-                const bool sa = ea < x.T ? (see >> ea & 1ull) : (ea >= lo && ea < hi);
-                const bool sb = eb < x.T ? (see >> eb & 1ull) : (eb >= lo && eb < hi);
-                t[j][n][e] = sa ? acc[n][e] * a.scale : -INFINITY;
-                t[j][n][2 + e] = sb ? acc[n][2 + e] * a.scale : -INFINITY;
-            }
+            uint4 r = {};
+            if (q[n]) r = *reinterpret_cast<const uint4*>(q[n] + c * (8 * G::kWordsK) + 8 * i);
+            mma_bf16(acc[n], u.x, v.x, u.y, v.y, r.x, r.y);
+            mma_bf16(acc[n], u.z, v.z, u.w, v.w, r.z, r.w);
         }
     }
-    uint32_t p[2][NG][2];
-    softmax_chunk<D, NG>(w, t, one, p);
+    if constexpr (D == 80) {
+        uint32_t u[4] = {};
+        if (ea < x.count) u[0] = *reinterpret_cast<const uint32_t*>(ka + 64 + 2 * c), u[2] = *reinterpret_cast<const uint32_t*>(ka + 72 + 2 * c);
+        if (eb < x.count) u[1] = *reinterpret_cast<const uint32_t*>(kb + 64 + 2 * c), u[3] = *reinterpret_cast<const uint32_t*>(kb + 72 + 2 * c);
+        #pragma unroll
+        for (int n = 0; n < NG; ++n) {
+            uint32_t r0 = 0u, r1 = 0u;
+            if (q[n]) r0 = *reinterpret_cast<const uint32_t*>(q[n] + 64 + 2 * c), r1 = *reinterpret_cast<const uint32_t*>(q[n] + 72 + 2 * c);
+            mma_bf16(acc[n], u[0], u[1], u[2], u[3], r0, r1);
+        }
+    }
     #pragma unroll
-    for (int j = 0; j < 2; ++j) {
-        const __nv_bfloat16* vk[4];
+    for (int n = 0; n < NG; ++n) {
         #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const int e = first + 16 * j + c + 4 * k;
-            vk[k] = e < x.count ? extra_key(a, x, D, b, h, e, true) : nullptr;
-        }
-        #pragma unroll
-        for (int i = 0; i < G::kWordsV; ++i) {
-            uint4 v[4] = {};
-            #pragma unroll
-            for (int k = 0; k < 4; ++k)
-                if (vk[k]) v[k] = *reinterpret_cast<const uint4*>(vk[k] + g * (8 * G::kWordsV) + 8 * i);
-            const uint32_t v0[4] = {v[0].x, v[0].y, v[0].z, v[0].w}, v1[4] = {v[1].x, v[1].y, v[1].z, v[1].w};
-            const uint32_t v2[4] = {v[2].x, v[2].y, v[2].z, v[2].w}, v3[4] = {v[3].x, v[3].y, v[3].z, v[3].w};
-            #pragma unroll
-            for (int s = 0; s < 4; ++s) {
-                const uint32_t a0 = __byte_perm(v0[s], v1[s], 0x5410), a1 = __byte_perm(v0[s], v1[s], 0x7632);
-                const uint32_t a2 = __byte_perm(v2[s], v3[s], 0x5410), a3 = __byte_perm(v2[s], v3[s], 0x7632);
-                #pragma unroll
-                for (int n = 0; n < NG; ++n) mma_bf16(w.o[4 * i + s][n], a0, a1, a2, a3, p[j][n][0], p[j][n][1]);
+        for (int e = 0; e < 2; ++e) {
+            const int r = x.row0 + 8 * n + 2 * c + e;
+            unsigned long long see = 0;
+            int lo = 0, hi = 0;                      // stream keys the row sees
+            if (r < x.rows) {
+                const Row q = row_of(r, x.T, x.gamma);
+                see = a.trees[b].anc_mask[q.t];
+                lo = x.T + (q.t - x.t0) * x.gamma;
+                hi = q.j < 0 ? lo : lo + q.j + 1;
             }
-        }
-        if constexpr (D == 80) {
-            uint32_t lo[4] = {}, hi[4] = {};
-            #pragma unroll
-            for (int k = 0; k < 4; ++k)
-                if (vk[k]) {
-                    lo[k] = reinterpret_cast<const unsigned short*>(vk[k])[64 + g];
-                    hi[k] = reinterpret_cast<const unsigned short*>(vk[k])[72 + g];
-                }
-            #pragma unroll
-            for (int n = 0; n < NG; ++n)
-                mma_bf16(w.o[4][n], lo[0] | lo[1] << 16, hi[0] | hi[1] << 16, lo[2] | lo[3] << 16, hi[2] | hi[3] << 16, p[j][n][0], p[j][n][1]);
+            const bool sa = ea < x.T ? (see >> ea & 1ull) : (ea >= lo && ea < hi);
+            const bool sb = eb < x.T ? (see >> eb & 1ull) : (eb >= lo && eb < hi);
+            acc[n][e] = sa ? fmaf(acc[n][e], a.scale, -w.ref[n][e]) : -INFINITY;
+            acc[n][2 + e] = sb ? fmaf(acc[n][2 + e], a.scale, -w.ref[n][e]) : -INFINITY;
         }
     }
 }
 
-// Asynchronous copies of a chunk's codes, scales and zero points into a stage of the warp's ring.  Slots behind `last` read as zero.
-template <int D>
-__device__ __forceinline__ void load_chunk(const KvqArgs& a, const Seq& s, int h, int chunk, uint32_t stage, int lane) {
+// O^T += V^T P^T of 16 keys behind the prefix
+template <int D, int NG>
+__device__ __forceinline__ void extra_values(WarpState<D, NG>& w, const uint32_t (&p)[NG][2], const KvqArgs& a, const Extra& x, int b, int h, int first, int g, int c) {
     using G = KvqGeometry<D>;
-    constexpr int kPer = G::kRowBytes / G::kCopy;
-    const int key0 = chunk * kChunk;
-    const long long slot = s.start + key0;
+    const __nv_bfloat16* vk[4];
+    bool there[4];
     #pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-        const int item = i * 32 + lane, key = item / kPer, at = item - key * kPer;
-        const bool real = key0 + key < s.L;
-        const long long off = real ? (slot + key) * a.slot_stride + h * a.head_stride + at * G::kCopy : 0;
-        copy_async<G::kCopy>(stage + key * G::kRowBytes + at * G::kCopy, a.k_codes + off, real);
-        copy_async<G::kCopy>(stage + G::kCodeBytes + key * G::kRowBytes + at * G::kCopy, a.v_codes + off, real);
+    for (int k = 0; k < 4; ++k) {
+        const int e = first + c + 4 * k;
+        there[k] = e < x.count;
+        vk[k] = (e < x.T ? a.v_tree : a.v_spec) + (there[k] ? extra_offset(a, x, D, b, h, e) : 0);
     }
-    const bool real = key0 + lane < s.L;
-    const long long off = real ? (slot + lane) * a.p_slot + h * a.p_head : 0;
-    copy_async<4>(stage + 2 * G::kCodeBytes + 4 * lane, a.k_params + off, real);
-    copy_async<4>(stage + 2 * G::kCodeBytes + 4 * kChunk + 4 * lane, a.v_params + off, real);
+    #pragma unroll
+    for (int i = 0; i < G::kWordsV; ++i) {
+        uint4 v[4] = {};
+        #pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (there[k]) v[k] = *reinterpret_cast<const uint4*>(vk[k] + g * (8 * G::kWordsV) + 8 * i);
+        const uint32_t v0[4] = {v[0].x, v[0].y, v[0].z, v[0].w}, v1[4] = {v[1].x, v[1].y, v[1].z, v[1].w};
+        const uint32_t v2[4] = {v[2].x, v[2].y, v[2].z, v[2].w}, v3[4] = {v[3].x, v[3].y, v[3].z, v[3].w};
+        #pragma unroll
+        for (int s = 0; s < 4; ++s) {
+            uint32_t a0 = __byte_perm(v0[s], v1[s], 0x5410), a1 = __byte_perm(v0[s], v1[s], 0x7632);
+            uint32_t a2 = __byte_perm(v2[s], v3[s], 0x5410), a3 = __byte_perm(v2[s], v3[s], 0x7632);
+            if (s & 1) a0 = times16_bf16x2(a0), a1 = times16_bf16x2(a1), a2 = times16_bf16x2(a2), a3 = times16_bf16x2(a3);
+            #pragma unroll
+            for (int n = 0; n < NG; ++n) mma_bf16(w.o[4 * i + s][n], a0, a1, a2, a3, p[n][0], p[n][1]);
+        }
+    }
+    if constexpr (D == 80) {
+        uint32_t lo[4] = {}, hi[4] = {};
+        #pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (there[k]) {
+                lo[k] = reinterpret_cast<const unsigned short*>(vk[k])[64 + g];
+                hi[k] = reinterpret_cast<const unsigned short*>(vk[k])[72 + g];
+            }
+        #pragma unroll
+        for (int n = 0; n < NG; ++n)
+            mma_bf16(w.o[4][n], lo[0] | lo[1] << 16, hi[0] | hi[1] << 16, lo[2] | lo[3] << 16, hi[2] | hi[3] << 16, p[n][0], p[n][1]);
+    }
 }
+
+// Asynchronous copies of chunks' codes, scales and zero points into the stages of a warp's ring.  A lane copies the same column of
+// every (32 / lanes per row)-th row, from pointers that walk along with the warp's chunks; slots behind the last one are read as the
+// last one again (their weights are zero).
+template <int D>
+struct ChunkLoader {
+    using G = KvqGeometry<D>;
+    static constexpr int kPer = G::kRowBytes / G::kCopy;         // copies per row and per lane: 4, 5 or 2
+    static constexpr bool kEven = 32 % kPer == 0;
+    const unsigned char *k, *v;                                  // of the next chunk: the lane's first copy (80: key 0)
+    const uint32_t *kp, *vp;                                     // the lane's key
+    long long on, pon, row;                                      // bytes and words to the warp's next chunk; bytes to the lane's next row
+    int left, step;                                              // slots from the next chunk on; slots between this warp's chunks
+
+    __device__ __forceinline__ ChunkLoader(const KvqArgs& a, const Seq& s, int h, int chunk, int stride, int lane) {
+        const long long slot = s.start + static_cast<long long>(chunk) * kChunk;
+        const long long off = (slot + (kEven ? lane / kPer : 0)) * a.slot_stride + h * a.head_stride + (kEven ? lane % kPer * G::kCopy : 0);
+        const long long poff = (slot + lane) * a.p_slot + h * a.p_head;
+        k = a.k_codes + off, v = a.v_codes + off;
+        kp = a.k_params + poff, vp = a.v_params + poff;
+        left = s.L - chunk * kChunk;
+        step = stride * kChunk;
+        on = step * a.slot_stride, pon = step * a.p_slot, row = (32 / kPer) * a.slot_stride;
+    }
+    // the next chunk of this warp, if it is among the cached ones
+    __device__ __forceinline__ void next(const KvqArgs& a, uint32_t stage, int lane, bool wanted) {
+        if (wanted) {
+            const uint32_t dst = stage + lane * G::kCopy, pdst = stage + 2 * G::kCodeBytes + 4 * lane;
+            if (kEven && left >= kChunk) {
+                #pragma unroll
+                for (int i = 0; i < kPer; ++i) {
+                    copy_async<G::kCopy>(dst + i * 32 * G::kCopy, k + i * row);
+                    copy_async<G::kCopy>(dst + i * 32 * G::kCopy + G::kCodeBytes, v + i * row);
+                }
+                copy_async<4>(pdst, kp);
+                copy_async<4>(pdst + 4 * kChunk, vp);
+            } else {
+                const int last = left - 1;
+                #pragma unroll 1
+                for (int i = 0; i < kPer; ++i) {
+                    const int item = i * 32 + lane, key = item / kPer;
+                    const long long off = kEven ? (min(key, last) - lane / kPer) * a.slot_stride : min(key, last) * a.slot_stride + (item - key * kPer) * G::kCopy;
+                    copy_async<G::kCopy>(dst + i * 32 * G::kCopy, k + off);
+                    copy_async<G::kCopy>(dst + i * 32 * G::kCopy + G::kCodeBytes, v + off);
+                }
+                const long long poff = (min(lane, last) - lane) * a.p_slot;
+                copy_async<4>(pdst, kp + poff);
+                copy_async<4>(pdst + 4 * kChunk, vp + poff);
+            }
+            k += on, v += on, kp += pon, vp += pon;
+            left -= step;
+        }
+        copy_commit();
+    }
+};
 
 // Dimensions that lane (g, c) holds in tile k of O^T: rows g (returned) and g + 8 (the next dimension; 8 further in the last tile of 80)
 template <int D>
@@ -481,7 +617,7 @@ __device__ __forceinline__ int tile_dim(int k, int g) {
 }
 
 template <int D, int NG>
-__global__ void __launch_bounds__(256, NG == 1 ? 2 : 1) msa_attention_kvq_rows_kernel(const __grid_constant__ KvqArgs a) {
+__global__ void __launch_bounds__(kThreads, NG == 1 ? 3 : 2) msa_attention_kvq_rows_kernel(const __grid_constant__ KvqArgs a) {
     using G = KvqGeometry<D>;
     using S = KvqSmem<D, NG>;
     constexpr int ROWS = 8 * NG, PAD = S::kPad;
@@ -490,43 +626,56 @@ __global__ void __launch_bounds__(256, NG == 1 ? 2 : 1) msa_attention_kvq_rows_k
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, c = lane & 3;
     const uint32_t ring = smem_addr(smem) + warp * G::kRingBytes;
     float* const parts = reinterpret_cast<float*>(smem);                                      // [warp][row][PAD], in the rings' place
-    float2* const stats = reinterpret_cast<float2*>(smem + S::kBytes - G::kWarps * ROWS * 8);   // [warp][row]: reference, sum
+    float2* const stats = reinterpret_cast<float2*>(smem + S::kBytes - kWarps * ROWS * 8);   // [warp][row]: reference, sum
+    const uint32_t kl = key_of(g) * G::kRowBytes + c * (4 * G::kWordsK), vl = G::kCodeBytes + c * G::kRowBytes + g * (4 * G::kWordsV);
+    const uint32_t pl = 2 * G::kCodeBytes + 4 * key_of(g), zl = 2 * G::kCodeBytes + 4 * kChunk + 4 * c;
     wait_for_previous_kernel();
     release_next_kernel();
 
     // how long the line is, and this CTA's piece of it
-    long long total = 0;
+    long long chunks = 0, blocks = 0;                             // of all sequences, for one head
+    Seq mine;                                                     // the lane's sequence of the first 32
+    #pragma unroll 1
     for (int b0 = 0; b0 < a.batch; b0 += 32) {
-        long long mine = 0;
-        if (b0 + lane < a.batch) {
-            const Seq s = load_seq<ROWS>(a, b0 + lane);
-            mine = static_cast<long long>(s.chunks) * s.blocks * a.n_heads;
-        }
-        #pragma unroll
-        for (int x = 16; x > 0; x >>= 1) mine += __shfl_xor_sync(0xffffffffu, mine, x);
-        total += mine;
+        const Seq s = b0 + lane < a.batch ? load_seq<ROWS>(a, b0 + lane) : Seq{};
+        if (b0 == 0) mine = s;
+        chunks += warp_sum(static_cast<long long>(s.chunks) * s.blocks);
+        blocks += warp_sum(s.blocks);
     }
-    const long long ctas = min(static_cast<long long>(gridDim.x), (total + G::kWarps - 1) / G::kWarps);
+    const int lg = heads_log2(a, chunks, blocks);
+    const int HW = 1 << lg, KS = kWarps >> lg, groups = (a.n_heads + HW - 1) >> lg;
+    const auto steps_of = [&](const Seq& s) { return (s.chunks + KS - 1) >> (kWarpsLog2 - lg); };
+    const auto line_of = [&](const Seq& s) { return static_cast<long long>(steps_of(s)) * s.blocks * groups; };
+    long long total = 0;
+    #pragma unroll 1
+    for (int b0 = 0; b0 < a.batch; b0 += 32)
+        total += warp_sum(b0 + lane < a.batch ? line_of(b0 == 0 ? mine : load_seq<ROWS>(a, b0 + lane)) : 0);
+    long long ctas = min(static_cast<long long>(gridDim.x), total);
+    // one sequence with fewer units than CTAs: every unit in the same number of pieces, so that all heads' pieces read the same slots at
+    // the same time
+    int pieces = 0, whole_steps = 0;
+    if (a.batch == 1 && total > 0) {
+        const int units = __shfl_sync(0xffffffffu, mine.blocks, 0) * groups;
+        whole_steps = __shfl_sync(0xffffffffu, steps_of(mine), 0);
+        pieces = static_cast<int>(static_cast<uint32_t>(ctas) / static_cast<uint32_t>(units));
+        if (pieces > 0) ctas = static_cast<long long>(pieces) * units;
+    }
     if (static_cast<long long>(blockIdx.x) >= ctas) return;
-    const auto cut = [&](long long i) { return total * i / ctas; };
-    const auto owner = [&](long long pos) {                       // the CTA whose piece holds position pos
-        long long i = pos * ctas / total;
-        while (cut(i + 1) <= pos) ++i;
-        while (cut(i) > pos) --i;
-        return i;
+    const long long share = pieces > 0 ? whole_steps / pieces : divide(total, ctas), rest = (pieces > 0 ? whole_steps : total) - share * (pieces > 0 ? pieces : ctas);
+    const auto cut = [&](int i) {
+        const int u = pieces > 0 ? i / pieces : 0, k = i - u * pieces;
+        return static_cast<long long>(u) * whole_steps + k * share + min(static_cast<long long>(k), rest);
     };
-    long long pos = cut(blockIdx.x);
-    const long long end = cut(blockIdx.x + 1ll);
-    // the sequence that holds the piece's first chunk
+    const int me = static_cast<int>(blockIdx.x);
+    long long pos = cut(me);
+    const long long end = cut(me + 1);
+    // the sequence that holds the piece's first step
     long long base = 0;
     int b = 0;
+    #pragma unroll 1
     for (int b0 = 0; b0 < a.batch; b0 += 32) {
-        long long mine = 0;
-        if (b0 + lane < a.batch) {
-            const Seq s = load_seq<ROWS>(a, b0 + lane);
-            mine = static_cast<long long>(s.chunks) * s.blocks * a.n_heads;
-        }
-        long long upto = mine;
+        const long long own = b0 + lane < a.batch ? line_of(b0 == 0 ? mine : load_seq<ROWS>(a, b0 + lane)) : 0;
+        long long upto = own;
         #pragma unroll
         for (int x = 1; x < 32; x <<= 1) {
             const long long y = __shfl_up_sync(0xffffffffu, upto, x);
@@ -536,7 +685,7 @@ __global__ void __launch_bounds__(256, NG == 1 ? 2 : 1) msa_attention_kvq_rows_k
         if (here) {
             const int l = __ffs(here) - 1;
             b = b0 + l;
-            base += __shfl_sync(0xffffffffu, upto - mine, l);
+            base += __shfl_sync(0xffffffffu, upto - own, l);
             break;
         }
         base += __shfl_sync(0xffffffffu, upto, 31);
@@ -544,17 +693,21 @@ __global__ void __launch_bounds__(256, NG == 1 ? 2 : 1) msa_attention_kvq_rows_k
     Seq s = load_seq<ROWS>(a, b);
     int* const counters = reinterpret_cast<int*>(a.ws + kWsHeaderBytes);
     float* const partial = reinterpret_cast<float*>(a.ws + kWsHeaderBytes + (4ull * gridDim.x + 255) / 256 * 256);
+    const int my_head = warp & (HW - 1), slice = warp >> lg;
 
+    int steps = steps_of(s), units = s.blocks * groups;
+    int unit = static_cast<int>(divide(pos - base, steps));
     while (pos < end) {
-        while (pos >= base + static_cast<long long>(s.chunks) * s.blocks * a.n_heads) {
-            base += static_cast<long long>(s.chunks) * s.blocks * a.n_heads;
+        while (unit >= units) {                      // on to the next sequence that has units
+            base += static_cast<long long>(units) * steps;
             s = load_seq<ROWS>(a, ++b);
+            steps = steps_of(s), units = s.blocks * groups, unit = 0;
         }
-        const int unit = static_cast<int>((pos - base) / s.chunks);
-        const long long unit0 = base + static_cast<long long>(unit) * s.chunks;
-        const int from = static_cast<int>(pos - unit0), to = static_cast<int>(min(end - unit0, static_cast<long long>(s.chunks)));
-        const int h = unit / s.blocks, row0 = (unit - h * s.blocks) * ROWS;
-        const int P = prefix_chunks(s.L);
+        const long long unit0 = base + static_cast<long long>(unit) * steps;
+        const int from = static_cast<int>(pos - unit0), to = static_cast<int>(min(end - unit0, static_cast<long long>(steps)));
+        const int group = static_cast<int>(static_cast<uint32_t>(unit) / static_cast<uint32_t>(s.blocks)), row0 = (unit - group * s.blocks) * ROWS;
+        const int h0 = group << lg, h = h0 + my_head;
+        const int P = prefix_chunks(s.L), stop = h < a.n_heads ? min(to * KS, s.chunks) : 0;       // (a warp without a head has no chunks)
 
         WarpState<D, NG> w;
         #pragma unroll
@@ -567,59 +720,99 @@ __global__ void __launch_bounds__(256, NG == 1 ? 2 : 1) msa_attention_kvq_rows_k
         }
         #pragma unroll
         for (int n = 0; n < NG; ++n) {
-            w.ref[n][0] = w.ref[n][1] = kNoRef;
+            w.ref[n][0] = w.ref[n][1] = 0.f;
             w.sum[n][0] = w.sum[n][1] = 0.f;
+            w.zo[n][0] = w.zo[n][1] = w.zo[n][2] = w.zo[n][3] = 0.f;
         }
-        int fetch = from + warp;
-        #pragma unroll
-        for (int i = 0; i < G::kStages - 1; ++i, fetch += G::kWarps) {
-            if (fetch < min(to, P)) load_chunk<D>(a, s, h, fetch, ring + i * G::kStageBytes, lane);
-            copy_commit();
-        }
+        w.weight = 64.f, w.limit = 0.f;
+        const int held = min(stop, P);               // chunks of cached slots end here
+        ChunkLoader<D> loader(a, s, min(h, a.n_heads - 1), from * KS + slice, KS, lane);
+        int fetch = from * KS + slice;
+        #pragma unroll 1
+        for (int i = 0; i < G::kStages - 1; ++i, fetch += KS) loader.next(a, ring + i * G::kStageBytes, lane, fetch < held);
         // query rows: row g of every group, the dimensions that c holds
         #pragma unroll
         for (int n = 0; n < NG; ++n) {
-            const int r = row0 + 8 * n + g;
-            const __nv_bfloat16* q = nullptr;
-            if (r < s.rows) {
-                const Row x = row_of(r, s.T, a.gamma);
-                q = (x.j < 0 ? a.q_main : a.q_spec) + row_offset(a, D, b, h, x);
+            const __nv_bfloat16* q = query_row<D>(a, s.T, s.rows, b, h, row0 + 8 * n + g);
+            uint32_t v[D / 16][2] = {};
+            if (q) {
+                #pragma unroll
+                for (int i = 0; i < G::kWordsK; ++i) {
+                    const uint4 u = *reinterpret_cast<const uint4*>(q + c * (8 * G::kWordsK) + 8 * i);
+                    v[2 * i][0] = u.x, v[2 * i][1] = u.y, v[2 * i + 1][0] = u.z, v[2 * i + 1][1] = u.w;
+                }
+                if constexpr (D == 80) v[4][0] = *reinterpret_cast<const uint32_t*>(q + 64 + 2 * c), v[4][1] = *reinterpret_cast<const uint32_t*>(q + 72 + 2 * c);
             }
+            uint32_t top = 0u;                       // two largest magnitudes (as patterns of bf16 they are in order)
             #pragma unroll
-            for (int i = 0; i < G::kWordsK; ++i) {
-                uint4 v = {};
-                if (q) v = *reinterpret_cast<const uint4*>(q + c * (8 * G::kWordsK) + 8 * i);
-                w.q[2 * i][n][0] = v.x, w.q[2 * i][n][1] = v.y, w.q[2 * i + 1][n][0] = v.z, w.q[2 * i + 1][n][1] = v.w;
+            for (int i = 0; i < D / 16; ++i) top = __vmaxu2(top, __vmaxu2(v[i][0] & 0x7fff7fffu, v[i][1] & 0x7fff7fffu));
+            top = __vmaxu2(top, __shfl_xor_sync(0xffffffffu, top, 1));
+            top = __vmaxu2(top, __shfl_xor_sync(0xffffffffu, top, 2));
+            // 2^e with the largest |q| 2^-e in [2^14, 2^15), kept where 2^e and 2^-e are normal numbers
+            const uint32_t eb = min(max(max(top & 0xffffu, top >> 16) >> 7, 24u), 247u) - 14u;
+            const float up = __uint_as_float(eb << 23), down = __uint_as_float((254u - eb) << 23);
+            float total = 0.f;
+            #pragma unroll
+            for (int i = 0; i < D / 16; ++i) {
+                #pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    const float x = __uint_as_float(v[i][k] << 16) * down, y = __uint_as_float(v[i][k] & 0xffff0000u) * down;
+                    const float f = k && i < 2 * G::kWordsK ? 0.0625f : 1.f;         // (these meet high codes)
+                    w.q[i][n][k] = pack2_f16(x * f, y * f);
+                    total += x + y;
+                }
             }
-            if constexpr (D == 80) {
-                w.q[4][n][0] = q ? *reinterpret_cast<const uint32_t*>(q + 64 + 2 * c) : 0u;
-                w.q[4][n][1] = q ? *reinterpret_cast<const uint32_t*>(q + 72 + 2 * c) : 0u;
+            total += __shfl_xor_sync(0xffffffffu, total, 1);
+            total += __shfl_xor_sync(0xffffffffu, total, 2);
+            // a row's sum and factor go to the lanes that hold its scores: rows 2c and 2c + 1 of the group
+            #pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                w.start[n][e] = __shfl_sync(0xffffffffu, total, 4 * (2 * c + e)) * (16.f * kCode);
+                w.factor[n][e] = __shfl_sync(0xffffffffu, up, 4 * (2 * c + e)) * (a.scale * (1.f / kCode));
             }
         }
-        int stage = 0;
-        for (int k = from + warp; k < to; k += G::kWarps) {
+        uint32_t stage = ring;
+        int k = from * KS + slice;
+        #pragma unroll 1
+        for (; k < held; k += KS) {
             copy_wait<G::kStages - 2>();
             __syncwarp();
-            {
-                int slot = stage + G::kStages - 1;
-                if (slot >= G::kStages) slot -= G::kStages;
-                if (fetch < min(to, P)) load_chunk<D>(a, s, h, fetch, ring + slot * G::kStageBytes, lane);
-                copy_commit();
-                fetch += G::kWarps;
+            loader.next(a, stage == ring ? stage + (G::kStages - 1) * G::kStageBytes : stage - G::kStageBytes, lane, fetch < held);
+            fetch += KS;
+            prefix_chunk<D, NG>(w, stage, s.L - k * kChunk, kl, vl, pl, zl, g, c);
+            stage = stage == ring + (G::kStages - 1) * G::kStageBytes ? ring : stage + G::kStageBytes;
+        }
+        if (k < stop) {
+            Extra x;
+            x.T = s.T, x.gamma = max(a.gamma, 1), x.row0 = row0, x.rows = s.rows, x.t0 = 0, x.count = s.T;
+            const int last = min(row0 + ROWS, s.rows) - 1;
+            if (last >= s.T) {                       // the block has stream rows: the streams of their nodes
+                x.t0 = row0 < s.T ? 0 : (row0 - s.T) / a.gamma;
+                x.count = s.T + ((last - s.T) / a.gamma - x.t0 + 1) * a.gamma;
             }
-            if (k < P) {
-                prefix_chunk<D, NG>(w, ring + stage * G::kStageBytes, min(kChunk, s.L - k * kChunk), a.scale, g, c);
-            } else {
-                Extra x;
-                x.T = s.T, x.gamma = max(a.gamma, 1), x.row0 = row0, x.rows = s.rows, x.t0 = 0, x.count = s.T;
-                const int last = min(row0 + ROWS, s.rows) - 1;
-                if (last >= s.T) {                   // the block has stream rows: the streams of their nodes
-                    x.t0 = row0 < s.T ? 0 : (row0 - s.T) / a.gamma;
-                    x.count = s.T + ((last - s.T) / a.gamma - x.t0 + 1) * a.gamma;
+            if (w.weight > 64.f) raise_scale<D, NG>(w, 1.f);             // (V in bf16 may be large: r is at least 0)
+            #pragma unroll 1
+            for (; k < stop; k += KS) {
+                #pragma unroll 1
+                for (int j = 0; j < kChunk; j += 16) {
+                    const int first = (k - P) * kChunk + j;
+                    if (first >= x.count) break;
+                    float d[1][NG][4];
+                    uint32_t p[NG][2];
+                    extra_scores<D, NG>(w, d[0], a, x, b, h, first, g, c);
+                    keep_in_range<D, NG, 1>(w, d, -1.f, true);
+                    const float f = w.weight * kCode;                    // (a weight meets values here, not codes)
+                    #pragma unroll
+                    for (int n = 0; n < NG; ++n) {
+                        const float x0 = exp2_approx(d[0][n][0]), x1 = exp2_approx(d[0][n][1]), x2 = exp2_approx(d[0][n][2]), x3 = exp2_approx(d[0][n][3]);
+                        w.sum[n][0] += x0 + x2;
+                        w.sum[n][1] += x1 + x3;
+                        p[n][0] = transpose_8x8(pack2_bf16(x0 * f, x1 * f));
+                        p[n][1] = transpose_8x8(pack2_bf16(x2 * f, x3 * f));
+                    }
+                    extra_values<D, NG>(w, p, a, x, b, h, first, g, c);
                 }
-                if ((k - P) * kChunk < x.count) extra_chunk<D, NG>(w, a, x, b, h, (k - P) * kChunk, g, c);
             }
-            if (++stage == G::kStages) stage = 0;
         }
         copy_wait<0>();
         __syncthreads();                             // all rings are at rest: their place is taken by the warps' partial results
@@ -631,35 +824,44 @@ __global__ void __launch_bounds__(256, NG == 1 ? 2 : 1) msa_attention_kvq_rows_k
             for (int e = 0; e < 2; ++e) {
                 #pragma unroll
                 for (int x = 4; x < 32; x <<= 1) w.sum[n][e] += __shfl_xor_sync(0xffffffffu, w.sum[n][e], x);
-                if (g == 0) stats[warp * ROWS + 8 * n + 2 * c + e] = make_float2(w.ref[n][e], w.sum[n][e]);
+                if (g == 0) stats[warp * ROWS + 8 * n + 2 * c + e] = make_float2(w.sum[n][e] == 0.f ? kNoRef : w.ref[n][e], w.sum[n][e]);
             }
         }
+        const float unweigh = 1.f / (kCode * w.weight);
         #pragma unroll
         for (int k = 0; k < G::kTiles; ++k) {
             const int dim = tile_dim<D>(k, g);
+            const float f = k < 4 * G::kWordsV && (k & 1) ? 0.0625f : 1.f;
             #pragma unroll
             for (int n = 0; n < NG; ++n) {
                 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
                     float* dst = parts + (warp * ROWS + 8 * n + 2 * c + e) * PAD + dim;
-                    if (k < 4 * G::kWordsV) *reinterpret_cast<float2*>(dst) = make_float2(w.o[k][n][e], w.o[k][n][2 + e]);
-                    else dst[0] = w.o[k][n][e], dst[8] = w.o[k][n][2 + e];
+                    const float x = fmaf(w.o[k][n][e], f, -w.zo[n][e]) * unweigh, y = fmaf(w.o[k][n][2 + e], f, -w.zo[n][e]) * unweigh;
+                    if (k < 4 * G::kWordsV) *reinterpret_cast<float2*>(dst) = make_float2(x, y);
+                    else dst[0] = x, dst[8] = y;
                 }
             }
         }
         __syncthreads();
 
         // whole unit: output.  A piece of one: partial rows to the workspace; the last CTA of the unit joins them.
-        const bool whole = from == 0 && to == s.chunks;
-        const long long i0 = whole ? 0 : owner(unit0), i1 = whole ? 0 : owner(unit0 + s.chunks - 1);
+        const bool whole = from == 0 && to == steps;
+        int i0 = me, i1 = me;                        // the CTAs that have a piece of the unit
+        long long at0 = unit0;
+        if (!whole) {
+            #pragma unroll 1
+            for (at0 = cut(i0); at0 > unit0; at0 = cut(--i0)) {}
+            #pragma unroll 1
+            while (cut(i1 + 1) < unit0 + steps) ++i1;
+        }
         // (a CTA's first unit and its last one: two places per CTA)
-        const auto place = [&](long long i) { return partial + (2 * i + (i == i0 && cut(i) < unit0 ? 1 : 0)) * partial_floats(D, ROWS); };
-        float* const mine = place(blockIdx.x);
-        constexpr int kItems = ROWS * (D / 8);
-        const auto store_row = [&](int r, int d0, const float (&o)[8], float m, float l) {
-            if (row0 + r >= s.rows) return;
+        const int second = at0 < unit0 ? 1 : 0;
+        const auto place = [&](int i) { return partial + (2ll * i + (i == i0 ? second : 0)) * partial_floats(D, ROWS); };
+        const int rows = min(ROWS, s.rows - row0), items = min(HW, a.n_heads - h0) * rows * (D / 8);
+        const auto store_row = [&](int hd, int r, int d0, const float (&o)[8], float m, float l) {
             const Row x = row_of(row0 + r, s.T, a.gamma);
-            const long long off = row_offset(a, D, b, h, x);
+            const long long off = row_offset(a, D, b, h0 + hd, x);
             const float f = 1.f / l;
             uint4 v;
             v.x = pack2_bf16(o[0] * f, o[1] * f), v.y = pack2_bf16(o[2] * f, o[3] * f);
@@ -668,68 +870,73 @@ __global__ void __launch_bounds__(256, NG == 1 ? 2 : 1) msa_attention_kvq_rows_k
             float* lse = x.j < 0 ? a.lse_main : a.lse_spec;
             if (d0 == 0 && lse != nullptr) lse[off / D] = (m + log2f(l)) * 0.6931471805599453f;
         };
-        for (int item = tid; item < kItems; item += 256) {
-            const int r = item / (D / 8), d0 = (item - r * (D / 8)) * 8;
+        // one more partial row into (o, m, l)
+        const auto join = [](float (&o)[8], float& m, float& l, const float2& st, const float4& u, const float4& v) {
+            const float now = fmaxf(m, st.x), f = exp2_approx(m - now), e = exp2_approx(st.x - now);
+            m = now, l = l * f + st.y * e;
+            o[0] = o[0] * f + u.x * e, o[1] = o[1] * f + u.y * e, o[2] = o[2] * f + u.z * e, o[3] = o[3] * f + u.w * e;
+            o[4] = o[4] * f + v.x * e, o[5] = o[5] * f + v.y * e, o[6] = o[6] * f + v.z * e, o[7] = o[7] * f + v.w * e;
+        };
+        #pragma unroll 1
+        for (int item = tid; item < items; item += kThreads) {
+            const int hr = item / (D / 8), d0 = (item - hr * (D / 8)) * 8, hd = hr / rows, r = hr - hd * rows;
             float m = kNoRef, l = 0.f, o[8] = {};
-            #pragma unroll
-            for (int i = 0; i < G::kWarps; ++i) m = fmaxf(m, stats[i * ROWS + r].x);
-            #pragma unroll
-            for (int i = 0; i < G::kWarps; ++i) {
-                const float2 st = stats[i * ROWS + r];
-                const float f = exp2_approx(st.x - m);
-                l += st.y * f;
+            #pragma unroll 1
+            for (int i = hd; i < kWarps; i += HW) {
                 const float* src = parts + (i * ROWS + r) * PAD + d0;
-                const float4 u = *reinterpret_cast<const float4*>(src), v = *reinterpret_cast<const float4*>(src + 4);
-                o[0] += u.x * f, o[1] += u.y * f, o[2] += u.z * f, o[3] += u.w * f;
-                o[4] += v.x * f, o[5] += v.y * f, o[6] += v.z * f, o[7] += v.w * f;
+                join(o, m, l, stats[i * ROWS + r], *reinterpret_cast<const float4*>(src), *reinterpret_cast<const float4*>(src + 4));
             }
             if (whole) {
-                store_row(r, d0, o, m, l);
+                store_row(hd, r, d0, o, m, l);
             } else {
-                float* dst = mine + r * D + d0;
+                float* dst = place(me) + hr * (D + 4) + d0;
                 __stcg(reinterpret_cast<float4*>(dst), make_float4(o[0], o[1], o[2], o[3]));
                 __stcg(reinterpret_cast<float4*>(dst) + 1, make_float4(o[4], o[5], o[6], o[7]));
-                if (d0 == 0) __stcg(reinterpret_cast<float2*>(mine + ROWS * D) + r, make_float2(m, l));
+                if (d0 == 0) __stcg(reinterpret_cast<float2*>(dst + D), make_float2(m, l));
             }
         }
         if (!whole) {
             __threadfence();
             __syncthreads();
             if (tid == 0) {
-                const int n = static_cast<int>(i1 - i0 + 1);
-                const int before = atomicAdd(counters + i0, 1);
-                joined = before == n - 1;
+                joined = atomicAdd(counters + i0, 1) == i1 - i0;
                 if (joined) counters[i0] = 0;
                 __threadfence();
             }
             __syncthreads();
             if (joined) {
-                for (int item = tid; item < kItems; item += 256) {
-                    const int r = item / (D / 8), d0 = (item - r * (D / 8)) * 8;
+                #pragma unroll 1
+                for (int item = tid; item < items; item += kThreads) {
+                    const int hr = item / (D / 8), d0 = (item - hr * (D / 8)) * 8, hd = hr / rows, r = hr - hd * rows;
                     float m = kNoRef, l = 0.f, o[8] = {};
-                    for (long long i = i0; i <= i1; ++i) m = fmaxf(m, __ldcg(reinterpret_cast<const float2*>(place(i) + ROWS * D) + r).x);
-                    for (long long i = i0; i <= i1; ++i) {
-                        const float* src = place(i);
-                        const float2 st = __ldcg(reinterpret_cast<const float2*>(src + ROWS * D) + r);
-                        const float f = exp2_approx(st.x - m);
-                        l += st.y * f;
-                        const float4 u = __ldcg(reinterpret_cast<const float4*>(src + r * D + d0)), v = __ldcg(reinterpret_cast<const float4*>(src + r * D + d0) + 1);
-                        o[0] += u.x * f, o[1] += u.y * f, o[2] += u.z * f, o[3] += u.w * f;
-                        o[4] += v.x * f, o[5] += v.y * f, o[6] += v.z * f, o[7] += v.w * f;
+                    #pragma unroll 1
+                    for (int i = i0; i <= i1; i += 4) {          // (four partial rows on their way at a time)
+                        float2 st[4];
+                        float4 u[4], v[4];
+                        #pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            const float* src = place(min(i + k, i1)) + hr * (D + 4);
+                            st[k] = __ldcg(reinterpret_cast<const float2*>(src + D));
+                            u[k] = __ldcg(reinterpret_cast<const float4*>(src + d0)), v[k] = __ldcg(reinterpret_cast<const float4*>(src + d0) + 1);
+                        }
+                        #pragma unroll
+                        for (int k = 0; k < 4; ++k)
+                            if (i + k <= i1) join(o, m, l, st[k], u[k], v[k]);
                     }
-                    store_row(r, d0, o, m, l);
+                    store_row(hd, r, d0, o, m, l);
                 }
             }
         }
         __syncthreads();                             // the partial results' place goes back to the rings
         pos = unit0 + to;
+        ++unit;                                      // (only if it is done: else pos is the end)
     }
 }
 
 // ---- host ---------------------------------------------------------------------------------------
 static int q_rows(const ss_kvq_attn_params& p) { return p.max_nodes * (1 + p.gamma); }
 static int group_count(const ss_kvq_attn_params& p) { return q_rows(p) <= 8 ? 1 : 2; }
-static int most_ctas(const ss_kvq_attn_params& p) { return sm_count() * (group_count(p) == 1 ? 2 : 1); }
+static int most_ctas(const ss_kvq_attn_params& p) { return sm_count() * (group_count(p) == 1 ? 3 : 2); }
 
 static size_t kvq_workspace(const ss_kvq_attn_params& p) {
     const size_t ctas = static_cast<size_t>(most_ctas(p));
@@ -749,7 +956,7 @@ static int32_t launch_kvq_rows(const KvqArgs& args, int ctas, cudaStream_t strea
     }
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(static_cast<unsigned>(ctas));
-    cfg.blockDim = dim3(256);
+    cfg.blockDim = dim3(kThreads);
     cfg.dynamicSmemBytes = bytes;
     cfg.stream = stream;
     cudaLaunchAttribute attr[1];
@@ -814,11 +1021,11 @@ extern "C" int32_t ss_msa_attention_kvq(const ss_kvq_attn_params* p, void* strea
     a.ws = static_cast<unsigned char*>(p->workspace);
     a.scale = p->sm_scale * 1.4426950408889634f;
     a.batch = p->batch, a.n_heads = c.n_heads, a.gamma = p->gamma, a.max_nodes = p->max_nodes;
-    // no more CTAs than the slab can give chunks for (eight to a CTA)
+    // no more CTAs than the slab can give steps for
     const int block = 8 * group_count(*p), blocks = (q_rows(*p) + block - 1) / block;
     const long long chunks = static_cast<long long>(c.n_heads) * blocks *
                              ((c.total_slots + kChunk - 1) / kChunk + p->batch * (1ll + extra_chunks(p->max_nodes, p->gamma, block)));
-    const int ctas = static_cast<int>(std::min<long long>(most_ctas(*p), (chunks + 7) / 8));
+    const int ctas = static_cast<int>(std::min<long long>(most_ctas(*p), chunks));
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     return c.head_dim == 128 ? launch_kvq<128>(*p, a, ctas, s) : c.head_dim == 80 ? launch_kvq<80>(*p, a, ctas, s) : launch_kvq<64>(*p, a, ctas, s);
 }

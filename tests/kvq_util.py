@@ -76,11 +76,21 @@ def ancestors(parent):
     return see
 
 
-def attention(parent, gamma, scale, q_main, q_spec, k_held, v_held, k_tree, v_tree, k_spec, v_spec):
-    """One sequence in 64 bits.  Rows are the nodes, then the nodes' streams; returns o, lse and the bounds of both.
+def value_scales(cache, layer, device="cpu"):
+    """Scales of a layer's values, [slots][H], 0 where they are not finite."""
+    s = torch.from_numpy(from_bits((cache.tensors[3][layer].cpu().numpy() & 0xFFFF).astype(np.uint16))).to(device)
+    return torch.nan_to_num(s, nan=0.0, posinf=0.0)
 
-    Bound of o: the weights meet V rounded to bf16 (2^-8 of sum p |v| / l), the output is rounded once (2^-8 of itself), and a
-    score is off by what fp32 sums of its d products, the scales and the exponential lose: delta, which moves weights and their sum."""
+
+def attention(parent, gamma, scale, q_main, q_spec, k_held, v_held, k_tree, v_tree, k_spec, v_spec, v_scale=None):
+    """One sequence in 64 bits.  Rows are the nodes, then the nodes' streams; returns o, lse and the bounds of both.  v_scale: scales of
+    the held values, [L][H].
+
+    Bound of o: the weights meet V rounded to 8 bits (2^-8 of sum p |v| / l), the output is rounded once (2^-8 of itself), and a
+    score is off by what fp32 sums of its d products, the scales and the exponential lose: delta, which moves weights and their sum.
+    Sums over cached keys: sum p s c and sum p s z are taken apart, in fp32, 16 keys at a time; both are at most 15 sum p s, a step rounds
+    by at most 2^-23 of that, and there are L / 16 steps and what joins partial sums: (L / 16 + 64) 2^-22 15 sum p s in all.  A weight
+    p s is off by at most 2^-31 of the largest scale where it is too small for fp16's 11 bits: 15 L 2^-31 max s."""
     T, H, d = q_main.shape
     rows = [q_main.double()] + ([q_spec.double().flatten(0, 1)] if gamma else [])
     keys = [k_held, k_tree.double()] + ([k_spec.double().flatten(0, 1)] if gamma else [])
@@ -107,4 +117,7 @@ def attention(parent, gamma, scale, q_main, q_spec, k_held, v_held, k_tree, v_tr
     delta = ((d + 16) * 2.0 ** -23 * size + 2.0 ** -20 + (L / 32 + 64) * 2.0 ** -24).T                      # [rows][H]
     o_tol = HALF_BF16 * (mass + o.abs()) * (1 + 2.0 ** -6) + 2 * delta[..., None] * mass + 2.0 ** -126
     lse_tol = delta + 2.0 ** -22 * lse.T.abs() + 2.0 ** -20
+    if v_scale is not None and L:
+        sums = torch.einsum("hrk,kh->rh", p[..., :L], v_scale)
+        o_tol = o_tol + (15 * (L / 16 + 64) * 2.0 ** -22 * sums + 15 * L * 2.0 ** -31 * v_scale.amax(0))[..., None]
     return o, lse.T, o_tol, lse_tol

@@ -240,13 +240,14 @@ class Layer:
 
     def check(self, seqs=None):
         kv, vv = U.cache_values(self.cache, 0, "cuda")
+        vs = U.value_scales(self.cache, 0, "cuda")
         T, g = max(self.nodes), self.gamma
         for b in range(self.B) if seqs is None else seqs:
             n, s0, L = self.nodes[b], self.starts[b], self.lens[b]
             if n:
                 spec = [t[b, :n] if g else None for t in (self.q_spec, self.k_spec, self.v_spec)] if g else [None] * 3
                 o, lse, o_tol, lse_tol = U.attention(self.parents[b], g, self.scale, self.q_main[b, :n], spec[0], kv[s0:s0 + L], vv[s0:s0 + L],
-                                                     self.k_tree[b, :n], self.v_tree[b, :n], spec[1], spec[2])
+                                                     self.k_tree[b, :n], self.v_tree[b, :n], spec[1], spec[2], vs[s0:s0 + L])
                 got = [self.o_main[b, :n].double()] + ([self.o_spec[b, :n].double().flatten(0, 1)] if g else [])
                 err = (torch.cat(got) - o).abs()
                 assert torch.isfinite(err).all(), b
@@ -371,7 +372,7 @@ def test_attention_beyond_32_bit_offsets(api):
     v = U.unpack(vc[0, at:at + 300].cpu().numpy(), vp[0, at:at + 300].cpu().numpy())
     assert torch.equal(back[0][0, 0].cpu(), torch.from_numpy(k).to(torch.bfloat16))
     o, _, tol, _ = U.attention(x.parents[0], 0, x.scale, x.q_main[0].cpu(), None, torch.from_numpy(k), torch.from_numpy(v), x.k_tree[0].cpu(),
-                               x.v_tree[0].cpu(), None, None)
+                               x.v_tree[0].cpu(), None, None, U.value_scales(x.cache, 0)[at:at + 300])
     assert ((x.o_main[0].cpu().double() - o).abs() <= tol).all()
 
 
@@ -452,10 +453,11 @@ def test_a_decode_loop_over_a_cache_in_4_bits(api, d):
             api.ss_msa_attention_kvq(api.make_kvq_attn_params(workspace=ws, **kw))
             assert api.ss_status(ws) == 0
             kv, vv = U.cache_values(cache, layer, "cuda")
+            vs = U.value_scales(cache, layer, "cuda")
             for b in range(B):
                 s0, L = int(starts[b]), int(kv_len[b])
                 ref = U.attention(parents[b], gamma, d ** -0.5, q[b], spec[0][b] if gamma else None, kv[s0:s0 + L], vv[s0:s0 + L], nodes[0][layer, b],
-                                  nodes[1][layer, b], spec[1][b] if gamma else None, spec[2][b] if gamma else None)
+                                  nodes[1][layer, b], spec[1][b] if gamma else None, spec[2][b] if gamma else None, vs[s0:s0 + L])
                 got = torch.cat([o[b].double()] + ([os_[b].double().flatten(0, 1)] if gamma else []))
                 assert ((got - ref[0]).abs() <= ref[2]).all()
         al, ap, ln, bt = _i32([0] * B), _i32([[0] * 64] * B), _i32([0] * B), _i32([0] * B)
