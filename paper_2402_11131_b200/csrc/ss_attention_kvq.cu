@@ -23,14 +23,13 @@ struct alignas(16) KvqArgs {
 };
 
 // ---- work ---------------------------------------------------------------------------------------
-// A unit is a block of query rows of HW neighbouring heads of one sequence.  Its keys are cut in chunks of 32: the cached slots, then
-// the tree's nodes and the stream keys of the block's own nodes.  A CTA's eight warps take HW heads and 8 / HW chunks of each at a time,
-// a step.  All units' steps, in order of sequence, heads and block, are one line that is cut into equal pieces, one per CTA: a CTA
-// takes the end of a unit, whole units, and the beginning of another.  So every CTA reads the same amount, whatever the lengths (which
-// only the device knows).
-// HW: a CTA that reads eight neighbouring heads of a slot reads 512 bytes in a row where slots are the outer dimension of the cache
-// (one head's 64 bytes at a time kept DRAM at 2.4 TB/s), and its warps have nothing to join.  Where there are only a few
-// steps for each CTA, one head's keys over all warps leave fewer partial results to join.
+// A unit is a block of query rows of some neighbouring heads of one sequence.  Its keys are cut in chunks of 32: the cached slots, then
+// the tree's nodes and the stream keys of the block's own nodes.  A team of CTAs takes a unit together: each of its CTAs has HW
+// heads, whose chunks go to its warps, warps / HW chunks of each at a time, a step.  All units' steps, in order of sequence, heads
+// and block, are one line that is cut into equal pieces, one per team: a team takes the end of a unit, whole units, and the beginning of
+// another.  So every CTA reads the same amount, whatever the lengths (which only the device knows).
+// Why neighbouring heads at the same time: with slots as the outer dimension of the cache a head's row of a slot is 64 bytes, and CTAs
+// that read single heads at unrelated slots keep DRAM at 2.5 TB/s (64 users, 267638 keys of 128: 485 us; four heads per CTA 265 us).
 constexpr int kChunk = 32;
 constexpr int kWarps = 4, kWarpsLog2 = 2, kThreads = 32 * kWarps;
 constexpr int kStepsForHeads = 6;
@@ -70,13 +69,20 @@ __device__ __forceinline__ Seq load_seq(const KvqArgs& a, int b) {
     return s;
 }
 
-// Heads per CTA (its log2) for `chunks` chunks and `blocks` blocks of one head: as many as eight where every CTA then has some steps,
-// at most an eighth of the warps have no head, and a unit is not cut in more than some ten pieces
-__device__ __forceinline__ int heads_log2(const KvqArgs& a, long long chunks, long long blocks) {
-    if (chunks * a.n_heads < static_cast<long long>(kStepsForHeads) * kWarps * gridDim.x) return 0;
-    int lg = kWarpsLog2;
-    while (lg > 0 && (8 * ((a.n_heads + (1 << lg) - 1) >> lg << lg) > 9 * a.n_heads || 10 * blocks * (a.n_heads >> lg) < gridDim.x)) --lg;
-    return lg;
+// Heads per CTA and CTAs per team (log2 of both), for `chunks` chunks and `blocks` blocks of one head.  Where every CTA has some steps a
+// unit has as many as 32 heads, as long as at most an eighth of the places have none; a CTA has as many of them as it has warps (there is
+// nothing to join then), as long as a unit is not cut in more than some ten pieces.  With only a few steps, one head's keys over
+// all warps leave fewer partial results to join.
+struct Shape {
+    int heads, team;
+};
+__device__ __forceinline__ Shape shape_of(const KvqArgs& a, long long chunks, long long blocks) {
+    Shape s{0, 0};
+    if (chunks * a.n_heads < static_cast<long long>(kStepsForHeads) * kWarps * gridDim.x) return s;
+    const auto fits = [&](int lg) { return 8 * ((a.n_heads + (1 << lg) - 1) >> lg << lg) <= 9 * a.n_heads; };
+    while (s.heads < kWarpsLog2 && fits(s.heads + 1) && 10 * blocks * (a.n_heads >> (s.heads + 1)) >= gridDim.x) ++s.heads;
+    while (s.heads + s.team < 5 && fits(s.heads + s.team + 1)) ++s.team;
+    return s;
 }
 
 __device__ __forceinline__ long long warp_sum(long long x) {
@@ -642,31 +648,31 @@ __global__ void __launch_bounds__(kThreads, NG == 1 ? 3 : 2) msa_attention_kvq_r
         chunks += warp_sum(static_cast<long long>(s.chunks) * s.blocks);
         blocks += warp_sum(s.blocks);
     }
-    const int lg = heads_log2(a, chunks, blocks);
-    const int HW = 1 << lg, KS = kWarps >> lg, groups = (a.n_heads + HW - 1) >> lg;
+    const Shape shape = shape_of(a, chunks, blocks);
+    const int lg = shape.heads, lt = shape.team, HW = 1 << lg, KS = kWarps >> lg, groups = (a.n_heads + (HW << lt) - 1) >> (lg + lt);
     const auto steps_of = [&](const Seq& s) { return (s.chunks + KS - 1) >> (kWarpsLog2 - lg); };
     const auto line_of = [&](const Seq& s) { return static_cast<long long>(steps_of(s)) * s.blocks * groups; };
     long long total = 0;
     #pragma unroll 1
     for (int b0 = 0; b0 < a.batch; b0 += 32)
         total += warp_sum(b0 + lane < a.batch ? line_of(b0 == 0 ? mine : load_seq<ROWS>(a, b0 + lane)) : 0);
-    long long ctas = min(static_cast<long long>(gridDim.x), total);
-    // one sequence with fewer units than CTAs: every unit in the same number of pieces, so that all heads' pieces read the same slots at
+    long long teams = min(static_cast<long long>(gridDim.x >> lt), total);
+    // one sequence with fewer units than teams: every unit in the same number of pieces, so that all heads' pieces read the same slots at
     // the same time
     int pieces = 0, whole_steps = 0;
     if (a.batch == 1 && total > 0) {
         const int units = __shfl_sync(0xffffffffu, mine.blocks, 0) * groups;
         whole_steps = __shfl_sync(0xffffffffu, steps_of(mine), 0);
-        pieces = static_cast<int>(static_cast<uint32_t>(ctas) / static_cast<uint32_t>(units));
-        if (pieces > 0) ctas = static_cast<long long>(pieces) * units;
+        pieces = static_cast<int>(static_cast<uint32_t>(teams) / static_cast<uint32_t>(units));
+        if (pieces > 0) teams = static_cast<long long>(pieces) * units;
     }
-    if (static_cast<long long>(blockIdx.x) >= ctas) return;
-    const long long share = pieces > 0 ? whole_steps / pieces : divide(total, ctas), rest = (pieces > 0 ? whole_steps : total) - share * (pieces > 0 ? pieces : ctas);
+    const int me = static_cast<int>(blockIdx.x) >> lt, member = static_cast<int>(blockIdx.x) - (me << lt);
+    if (me >= teams) return;
+    const long long share = pieces > 0 ? whole_steps / pieces : divide(total, teams), rest = (pieces > 0 ? whole_steps : total) - share * (pieces > 0 ? pieces : teams);
     const auto cut = [&](int i) {
         const int u = pieces > 0 ? i / pieces : 0, k = i - u * pieces;
         return static_cast<long long>(u) * whole_steps + k * share + min(static_cast<long long>(k), rest);
     };
-    const int me = static_cast<int>(blockIdx.x);
     long long pos = cut(me);
     const long long end = cut(me + 1);
     // the sequence that holds the piece's first step
@@ -706,7 +712,7 @@ __global__ void __launch_bounds__(kThreads, NG == 1 ? 3 : 2) msa_attention_kvq_r
         const long long unit0 = base + static_cast<long long>(unit) * steps;
         const int from = static_cast<int>(pos - unit0), to = static_cast<int>(min(end - unit0, static_cast<long long>(steps)));
         const int group = static_cast<int>(static_cast<uint32_t>(unit) / static_cast<uint32_t>(s.blocks)), row0 = (unit - group * s.blocks) * ROWS;
-        const int h0 = group << lg, h = h0 + my_head;
+        const int h0 = ((group << lt) + member) << lg, h = h0 + my_head;
         const int P = prefix_chunks(s.L), stop = h < a.n_heads ? min(to * KS, s.chunks) : 0;       // (a warp without a head has no chunks)
 
         WarpState<D, NG> w;
@@ -847,7 +853,7 @@ __global__ void __launch_bounds__(kThreads, NG == 1 ? 3 : 2) msa_attention_kvq_r
 
         // whole unit: output.  A piece of one: partial rows to the workspace; the last CTA of the unit joins them.
         const bool whole = from == 0 && to == steps;
-        int i0 = me, i1 = me;                        // the CTAs that have a piece of the unit
+        int i0 = me, i1 = me;                        // the teams that have a piece of the unit
         long long at0 = unit0;
         if (!whole) {
             #pragma unroll 1
@@ -857,8 +863,8 @@ __global__ void __launch_bounds__(kThreads, NG == 1 ? 3 : 2) msa_attention_kvq_r
         }
         // (a CTA's first unit and its last one: two places per CTA)
         const int second = at0 < unit0 ? 1 : 0;
-        const auto place = [&](int i) { return partial + (2ll * i + (i == i0 ? second : 0)) * partial_floats(D, ROWS); };
-        const int rows = min(ROWS, s.rows - row0), items = min(HW, a.n_heads - h0) * rows * (D / 8);
+        const auto place = [&](int i) { return partial + (2ll * ((i << lt) + member) + (i == i0 ? second : 0)) * partial_floats(D, ROWS); };
+        const int rows = min(ROWS, s.rows - row0), items = max(0, min(HW, a.n_heads - h0)) * rows * (D / 8);
         const auto store_row = [&](int hd, int r, int d0, const float (&o)[8], float m, float l) {
             const Row x = row_of(row0 + r, s.T, a.gamma);
             const long long off = row_offset(a, D, b, h0 + hd, x);
@@ -899,8 +905,8 @@ __global__ void __launch_bounds__(kThreads, NG == 1 ? 3 : 2) msa_attention_kvq_r
             __threadfence();
             __syncthreads();
             if (tid == 0) {
-                joined = atomicAdd(counters + i0, 1) == i1 - i0;
-                if (joined) counters[i0] = 0;
+                joined = atomicAdd(counters + (i0 << lt) + member, 1) == i1 - i0;
+                if (joined) counters[(i0 << lt) + member] = 0;
                 __threadfence();
             }
             __syncthreads();
