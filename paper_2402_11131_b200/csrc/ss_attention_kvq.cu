@@ -39,20 +39,22 @@ struct Seq {
     long long start;
 };
 
-__device__ __forceinline__ int prefix_chunks(int L) { return (L + kChunk - 1) / kChunk; }
+template <int CHUNK>
+__device__ __forceinline__ int prefix_chunks(int L) { return (L + CHUNK - 1) / CHUNK; }
 
 // Most keys behind the prefix that a block of `block` rows sees: all nodes, and the streams of the nodes its rows belong to
+template <int CHUNK>
 __host__ __device__ __forceinline__ int extra_chunks(int T, int gamma, int block) {
     int stream = 0;
     if (gamma > 0) {
         const int nodes = (block + gamma - 2) / gamma + 1;
         stream = (nodes < T ? nodes : T) * gamma;
     }
-    return (T + stream + kChunk - 1) / kChunk;
+    return (T + stream + CHUNK - 1) / CHUNK;
 }
 
 // One sequence as the call gives it.  A sequence that cannot be run has no blocks.
-template <int ROWS>
+template <int ROWS, int CHUNK>
 __device__ __forceinline__ Seq load_seq(const KvqArgs& a, int b) {
     Seq s;
     s.L = a.kv_len[b];
@@ -64,7 +66,7 @@ __device__ __forceinline__ Seq load_seq(const KvqArgs& a, int b) {
     else {
         s.rows = s.T * (1 + a.gamma);
         s.blocks = (s.rows + ROWS - 1) / ROWS;
-        s.chunks = prefix_chunks(s.L) + extra_chunks(s.T, a.gamma, ROWS);
+        s.chunks = prefix_chunks<CHUNK>(s.L) + extra_chunks<CHUNK>(s.T, a.gamma, ROWS);
     }
     return s;
 }
@@ -76,12 +78,13 @@ __device__ __forceinline__ Seq load_seq(const KvqArgs& a, int b) {
 struct Shape {
     int heads, team;
 };
+template <int WARPS_LOG2>
 __device__ __forceinline__ Shape shape_of(const KvqArgs& a, long long chunks, long long blocks) {
     Shape s{0, 0};
-    if (chunks * a.n_heads < static_cast<long long>(kStepsForHeads) * kWarps * gridDim.x) return s;
+    if (chunks * a.n_heads < (static_cast<long long>(kStepsForHeads) << WARPS_LOG2) * gridDim.x) return s;
     const auto fits = [&](int lg) { return 8 * ((a.n_heads + (1 << lg) - 1) >> lg << lg) <= 9 * a.n_heads; };
-    while (s.heads < kWarpsLog2 && fits(s.heads + 1) && 10 * blocks * (a.n_heads >> (s.heads + 1)) >= gridDim.x) ++s.heads;
-    while (s.heads + s.team < 5 && fits(s.heads + s.team + 1)) ++s.team;
+    while (s.heads < WARPS_LOG2 && fits(s.heads + 1) && 10 * blocks * (a.n_heads >> (s.heads + 1)) >= gridDim.x) ++s.heads;
+    while (s.team < 3 && fits(s.heads + s.team + 1)) ++s.team;
     return s;
 }
 
@@ -181,6 +184,131 @@ __device__ __forceinline__ uint32_t zero_pair(uint32_t a, uint32_t b) { return l
 __device__ __forceinline__ float scale_of(uint32_t word) { return __uint_as_float(word << 16); }
 __device__ __forceinline__ float zero_over_16(uint32_t word) { return __uint_as_float(((word & 0xf0000u) << 3) | 0x3f800000u); }     // 1 + z / 16
 constexpr float kCode = 5.9604644775390625e-08f;                 // 2^-24: what a code counts in an MMA
+
+// The line of steps as one CTA sees it (every thread, or one warp of a role, works it out for itself)
+template <int ROWS, int CHUNK, int WARPS_LOG2>
+struct Line {
+    int heads_log2, team_log2, steps_log2;           // heads and chunks per step of a CTA, CTAs of a team
+    int groups, me, member;                          // of heads; this CTA's team and its place there
+    int pieces, whole_steps;
+    long long total, share, rest;
+    long long pos, end, base;                        // the piece's next step and its end; first step of sequence b
+    int b, steps, units, unit;                       // sequence; its units and their steps; the next unit
+    Seq s;
+    // the unit at hand
+    long long unit0;
+    int from, to, head0, row0;                       // steps of it, its first head for this CTA and its first row
+
+    __device__ __forceinline__ int steps_of(const Seq& q) const { return (q.chunks + (1 << steps_log2) - 1) >> steps_log2; }
+    __device__ __forceinline__ long long line_of(const Seq& q) const { return static_cast<long long>(steps_of(q)) * q.blocks * groups; }
+    // first step of team i's piece
+    __device__ __forceinline__ long long cut(int i) const {
+        const int u = pieces > 0 ? i / pieces : 0, k = i - u * pieces;
+        return static_cast<long long>(u) * whole_steps + k * share + min(static_cast<long long>(k), rest);
+    }
+    // false: nothing for this CTA.  All lanes of a warp come here.
+    __device__ __forceinline__ bool begin(const KvqArgs& a, int lane) {
+        long long chunks = 0, blocks = 0;            // of all sequences, for one head
+        Seq mine;                                    // the lane's sequence of the first 32
+        #pragma unroll 1
+        for (int b0 = 0; b0 < a.batch; b0 += 32) {
+            const Seq q = b0 + lane < a.batch ? load_seq<ROWS, CHUNK>(a, b0 + lane) : Seq{};
+            if (b0 == 0) mine = q;
+            chunks += warp_sum(static_cast<long long>(q.chunks) * q.blocks);
+            blocks += warp_sum(q.blocks);
+        }
+        const Shape shape = shape_of<WARPS_LOG2>(a, chunks, blocks);
+        heads_log2 = shape.heads, team_log2 = shape.team, steps_log2 = WARPS_LOG2 - shape.heads;
+        groups = (a.n_heads + (1 << (heads_log2 + team_log2)) - 1) >> (heads_log2 + team_log2);
+        total = 0;
+        #pragma unroll 1
+        for (int b0 = 0; b0 < a.batch; b0 += 32)
+            total += warp_sum(b0 + lane < a.batch ? line_of(b0 == 0 ? mine : load_seq<ROWS, CHUNK>(a, b0 + lane)) : 0);
+        long long teams = min(static_cast<long long>(gridDim.x >> team_log2), total);
+        // one sequence with fewer units than teams: every unit in the same number of pieces, so that all heads' pieces read the same slots
+        // at the same time
+        pieces = whole_steps = 0;
+        if (a.batch == 1 && total > 0) {
+            const int n = __shfl_sync(0xffffffffu, mine.blocks, 0) * groups;
+            whole_steps = __shfl_sync(0xffffffffu, steps_of(mine), 0);
+            pieces = static_cast<int>(static_cast<uint32_t>(teams) / static_cast<uint32_t>(n));
+            if (pieces > 0) teams = static_cast<long long>(pieces) * n;
+        }
+        me = static_cast<int>(blockIdx.x) >> team_log2, member = static_cast<int>(blockIdx.x) - (me << team_log2);
+        if (me >= teams) return false;
+        share = pieces > 0 ? whole_steps / pieces : divide(total, teams);
+        rest = (pieces > 0 ? whole_steps : total) - share * (pieces > 0 ? pieces : teams);
+        pos = cut(me), end = cut(me + 1);
+        // the sequence that holds the piece's first step
+        base = 0, b = 0;
+        #pragma unroll 1
+        for (int b0 = 0; b0 < a.batch; b0 += 32) {
+            const long long own = b0 + lane < a.batch ? line_of(b0 == 0 ? mine : load_seq<ROWS, CHUNK>(a, b0 + lane)) : 0;
+            long long upto = own;
+            #pragma unroll
+            for (int x = 1; x < 32; x <<= 1) {
+                const long long y = __shfl_up_sync(0xffffffffu, upto, x);
+                if (lane >= x) upto += y;
+            }
+            const unsigned here = __ballot_sync(0xffffffffu, base + upto > pos);
+            if (here) {
+                const int l = __ffs(here) - 1;
+                b = b0 + l;
+                base += __shfl_sync(0xffffffffu, upto - own, l);
+                break;
+            }
+            base += __shfl_sync(0xffffffffu, upto, 31);
+        }
+        s = load_seq<ROWS, CHUNK>(a, b);
+        steps = steps_of(s), units = s.blocks * groups;
+        unit = static_cast<int>(divide(pos - base, steps));
+        return true;
+    }
+    // the unit at hand, or false at the end of the piece
+    __device__ __forceinline__ bool next(const KvqArgs& a) {
+        if (pos >= end) return false;
+        while (unit >= units) {                      // on to the next sequence that has units
+            base += static_cast<long long>(units) * steps;
+            s = load_seq<ROWS, CHUNK>(a, ++b);
+            steps = steps_of(s), units = s.blocks * groups, unit = 0;
+        }
+        unit0 = base + static_cast<long long>(unit) * steps;
+        from = static_cast<int>(pos - unit0), to = static_cast<int>(min(end - unit0, static_cast<long long>(steps)));
+        const int group = static_cast<int>(static_cast<uint32_t>(unit) / static_cast<uint32_t>(s.blocks));
+        row0 = (unit - group * s.blocks) * ROWS;
+        head0 = ((group << team_log2) + member) << heads_log2;
+        pos = unit0 + to;
+        ++unit;                                      // (only if it is done: else pos is the end)
+        return true;
+    }
+    __device__ __forceinline__ bool whole() const { return from == 0 && to == steps; }
+};
+
+// The CTAs that have a piece of a unit, and where their partial results lie: two places per CTA, for its first unit and its last one
+struct Pieces {
+    int first, last, second;                         // teams; 1 if the first one has begun another unit before
+    template <typename L>
+    __device__ __forceinline__ explicit Pieces(const L& line) : first(line.me), last(line.me) {
+        long long at = line.unit0;
+        if (!line.whole()) {
+            #pragma unroll 1
+            for (at = line.cut(first); at > line.unit0; at = line.cut(--first)) {}
+            #pragma unroll 1
+            while (line.cut(last + 1) < line.unit0 + line.steps) ++last;
+        }
+        second = at < line.unit0 ? 1 : 0;
+    }
+    template <typename L>
+    __device__ __forceinline__ long long place(const L& line, int i) const { return 2ll * ((i << line.team_log2) + line.member) + (i == first ? second : 0); }
+};
+
+// One more partial row into (o, m, l)
+__device__ __forceinline__ void join_row(float (&o)[8], float& m, float& l, const float2& st, const float4& u, const float4& v) {
+    const float now = fmaxf(m, st.x), f = exp2_approx(m - now), e = exp2_approx(st.x - now);
+    m = now, l = l * f + st.y * e;
+    o[0] = o[0] * f + u.x * e, o[1] = o[1] * f + u.y * e, o[2] = o[2] * f + u.z * e, o[3] = o[3] * f + u.w * e;
+    o[4] = o[4] * f + v.x * e, o[5] = o[5] * f + v.y * e, o[6] = o[6] * f + v.z * e, o[7] = o[7] * f + v.w * e;
+}
 
 // ---- the kernel ---------------------------------------------------------------------------------
 // S^T = K Q^T and O^T = V^T P^T on mma.sync m16n8k16 with the keys (the dimensions) as the 16 rows of A and NG groups of 8 query
@@ -638,82 +766,17 @@ __global__ void __launch_bounds__(kThreads, NG == 1 ? 3 : 2) msa_attention_kvq_r
     wait_for_previous_kernel();
     release_next_kernel();
 
-    // how long the line is, and this CTA's piece of it
-    long long chunks = 0, blocks = 0;                             // of all sequences, for one head
-    Seq mine;                                                     // the lane's sequence of the first 32
-    #pragma unroll 1
-    for (int b0 = 0; b0 < a.batch; b0 += 32) {
-        const Seq s = b0 + lane < a.batch ? load_seq<ROWS>(a, b0 + lane) : Seq{};
-        if (b0 == 0) mine = s;
-        chunks += warp_sum(static_cast<long long>(s.chunks) * s.blocks);
-        blocks += warp_sum(s.blocks);
-    }
-    const Shape shape = shape_of(a, chunks, blocks);
-    const int lg = shape.heads, lt = shape.team, HW = 1 << lg, KS = kWarps >> lg, groups = (a.n_heads + (HW << lt) - 1) >> (lg + lt);
-    const auto steps_of = [&](const Seq& s) { return (s.chunks + KS - 1) >> (kWarpsLog2 - lg); };
-    const auto line_of = [&](const Seq& s) { return static_cast<long long>(steps_of(s)) * s.blocks * groups; };
-    long long total = 0;
-    #pragma unroll 1
-    for (int b0 = 0; b0 < a.batch; b0 += 32)
-        total += warp_sum(b0 + lane < a.batch ? line_of(b0 == 0 ? mine : load_seq<ROWS>(a, b0 + lane)) : 0);
-    long long teams = min(static_cast<long long>(gridDim.x >> lt), total);
-    // one sequence with fewer units than teams: every unit in the same number of pieces, so that all heads' pieces read the same slots at
-    // the same time
-    int pieces = 0, whole_steps = 0;
-    if (a.batch == 1 && total > 0) {
-        const int units = __shfl_sync(0xffffffffu, mine.blocks, 0) * groups;
-        whole_steps = __shfl_sync(0xffffffffu, steps_of(mine), 0);
-        pieces = static_cast<int>(static_cast<uint32_t>(teams) / static_cast<uint32_t>(units));
-        if (pieces > 0) teams = static_cast<long long>(pieces) * units;
-    }
-    const int me = static_cast<int>(blockIdx.x) >> lt, member = static_cast<int>(blockIdx.x) - (me << lt);
-    if (me >= teams) return;
-    const long long share = pieces > 0 ? whole_steps / pieces : divide(total, teams), rest = (pieces > 0 ? whole_steps : total) - share * (pieces > 0 ? pieces : teams);
-    const auto cut = [&](int i) {
-        const int u = pieces > 0 ? i / pieces : 0, k = i - u * pieces;
-        return static_cast<long long>(u) * whole_steps + k * share + min(static_cast<long long>(k), rest);
-    };
-    long long pos = cut(me);
-    const long long end = cut(me + 1);
-    // the sequence that holds the piece's first step
-    long long base = 0;
-    int b = 0;
-    #pragma unroll 1
-    for (int b0 = 0; b0 < a.batch; b0 += 32) {
-        const long long own = b0 + lane < a.batch ? line_of(b0 == 0 ? mine : load_seq<ROWS>(a, b0 + lane)) : 0;
-        long long upto = own;
-        #pragma unroll
-        for (int x = 1; x < 32; x <<= 1) {
-            const long long y = __shfl_up_sync(0xffffffffu, upto, x);
-            if (lane >= x) upto += y;
-        }
-        const unsigned here = __ballot_sync(0xffffffffu, base + upto > pos);
-        if (here) {
-            const int l = __ffs(here) - 1;
-            b = b0 + l;
-            base += __shfl_sync(0xffffffffu, upto - own, l);
-            break;
-        }
-        base += __shfl_sync(0xffffffffu, upto, 31);
-    }
-    Seq s = load_seq<ROWS>(a, b);
+    Line<ROWS, kChunk, kWarpsLog2> line;
+    if (!line.begin(a, lane)) return;
+    const int HW = 1 << line.heads_log2, KS = 1 << line.steps_log2;
     int* const counters = reinterpret_cast<int*>(a.ws + kWsHeaderBytes);
     float* const partial = reinterpret_cast<float*>(a.ws + kWsHeaderBytes + (4ull * gridDim.x + 255) / 256 * 256);
-    const int my_head = warp & (HW - 1), slice = warp >> lg;
+    const int my_head = warp & (HW - 1), slice = warp >> line.heads_log2;
 
-    int steps = steps_of(s), units = s.blocks * groups;
-    int unit = static_cast<int>(divide(pos - base, steps));
-    while (pos < end) {
-        while (unit >= units) {                      // on to the next sequence that has units
-            base += static_cast<long long>(units) * steps;
-            s = load_seq<ROWS>(a, ++b);
-            steps = steps_of(s), units = s.blocks * groups, unit = 0;
-        }
-        const long long unit0 = base + static_cast<long long>(unit) * steps;
-        const int from = static_cast<int>(pos - unit0), to = static_cast<int>(min(end - unit0, static_cast<long long>(steps)));
-        const int group = static_cast<int>(static_cast<uint32_t>(unit) / static_cast<uint32_t>(s.blocks)), row0 = (unit - group * s.blocks) * ROWS;
-        const int h0 = ((group << lt) + member) << lg, h = h0 + my_head;
-        const int P = prefix_chunks(s.L), stop = h < a.n_heads ? min(to * KS, s.chunks) : 0;       // (a warp without a head has no chunks)
+    while (line.next(a)) {
+        const Seq& s = line.s;
+        const int b = line.b, from = line.from, to = line.to, row0 = line.row0, h0 = line.head0, h = h0 + my_head;
+        const int P = prefix_chunks<kChunk>(s.L), stop = h < a.n_heads ? min(to * KS, s.chunks) : 0;       // (a warp without a head has no chunks)
 
         WarpState<D, NG> w;
         #pragma unroll
@@ -852,18 +915,9 @@ __global__ void __launch_bounds__(kThreads, NG == 1 ? 3 : 2) msa_attention_kvq_r
         __syncthreads();
 
         // whole unit: output.  A piece of one: partial rows to the workspace; the last CTA of the unit joins them.
-        const bool whole = from == 0 && to == steps;
-        int i0 = me, i1 = me;                        // the teams that have a piece of the unit
-        long long at0 = unit0;
-        if (!whole) {
-            #pragma unroll 1
-            for (at0 = cut(i0); at0 > unit0; at0 = cut(--i0)) {}
-            #pragma unroll 1
-            while (cut(i1 + 1) < unit0 + steps) ++i1;
-        }
-        // (a CTA's first unit and its last one: two places per CTA)
-        const int second = at0 < unit0 ? 1 : 0;
-        const auto place = [&](int i) { return partial + (2ll * ((i << lt) + member) + (i == i0 ? second : 0)) * partial_floats(D, ROWS); };
+        const bool whole = line.whole();
+        const Pieces share(line);
+        const auto place = [&](int i) { return partial + share.place(line, i) * partial_floats(D, ROWS); };
         const int rows = min(ROWS, s.rows - row0), items = max(0, min(HW, a.n_heads - h0)) * rows * (D / 8);
         const auto store_row = [&](int hd, int r, int d0, const float (&o)[8], float m, float l) {
             const Row x = row_of(row0 + r, s.T, a.gamma);
@@ -876,13 +930,6 @@ __global__ void __launch_bounds__(kThreads, NG == 1 ? 3 : 2) msa_attention_kvq_r
             float* lse = x.j < 0 ? a.lse_main : a.lse_spec;
             if (d0 == 0 && lse != nullptr) lse[off / D] = (m + log2f(l)) * 0.6931471805599453f;
         };
-        // one more partial row into (o, m, l)
-        const auto join = [](float (&o)[8], float& m, float& l, const float2& st, const float4& u, const float4& v) {
-            const float now = fmaxf(m, st.x), f = exp2_approx(m - now), e = exp2_approx(st.x - now);
-            m = now, l = l * f + st.y * e;
-            o[0] = o[0] * f + u.x * e, o[1] = o[1] * f + u.y * e, o[2] = o[2] * f + u.z * e, o[3] = o[3] * f + u.w * e;
-            o[4] = o[4] * f + v.x * e, o[5] = o[5] * f + v.y * e, o[6] = o[6] * f + v.z * e, o[7] = o[7] * f + v.w * e;
-        };
         #pragma unroll 1
         for (int item = tid; item < items; item += kThreads) {
             const int hr = item / (D / 8), d0 = (item - hr * (D / 8)) * 8, hd = hr / rows, r = hr - hd * rows;
@@ -890,12 +937,12 @@ __global__ void __launch_bounds__(kThreads, NG == 1 ? 3 : 2) msa_attention_kvq_r
             #pragma unroll 1
             for (int i = hd; i < kWarps; i += HW) {
                 const float* src = parts + (i * ROWS + r) * PAD + d0;
-                join(o, m, l, stats[i * ROWS + r], *reinterpret_cast<const float4*>(src), *reinterpret_cast<const float4*>(src + 4));
+                join_row(o, m, l, stats[i * ROWS + r], *reinterpret_cast<const float4*>(src), *reinterpret_cast<const float4*>(src + 4));
             }
             if (whole) {
                 store_row(hd, r, d0, o, m, l);
             } else {
-                float* dst = place(me) + hr * (D + 4) + d0;
+                float* dst = place(line.me) + hr * (D + 4) + d0;
                 __stcg(reinterpret_cast<float4*>(dst), make_float4(o[0], o[1], o[2], o[3]));
                 __stcg(reinterpret_cast<float4*>(dst) + 1, make_float4(o[4], o[5], o[6], o[7]));
                 if (d0 == 0) __stcg(reinterpret_cast<float2*>(dst + D), make_float2(m, l));
@@ -905,8 +952,9 @@ __global__ void __launch_bounds__(kThreads, NG == 1 ? 3 : 2) msa_attention_kvq_r
             __threadfence();
             __syncthreads();
             if (tid == 0) {
-                joined = atomicAdd(counters + (i0 << lt) + member, 1) == i1 - i0;
-                if (joined) counters[(i0 << lt) + member] = 0;
+                int* const counter = counters + (share.first << line.team_log2) + line.member;
+                joined = atomicAdd(counter, 1) == share.last - share.first;
+                if (joined) *counter = 0;
                 __threadfence();
             }
             __syncthreads();
@@ -916,26 +964,24 @@ __global__ void __launch_bounds__(kThreads, NG == 1 ? 3 : 2) msa_attention_kvq_r
                     const int hr = item / (D / 8), d0 = (item - hr * (D / 8)) * 8, hd = hr / rows, r = hr - hd * rows;
                     float m = kNoRef, l = 0.f, o[8] = {};
                     #pragma unroll 1
-                    for (int i = i0; i <= i1; i += 4) {          // (four partial rows on their way at a time)
+                    for (int i = share.first; i <= share.last; i += 4) {          // (four partial rows on their way at a time)
                         float2 st[4];
                         float4 u[4], v[4];
                         #pragma unroll
                         for (int k = 0; k < 4; ++k) {
-                            const float* src = place(min(i + k, i1)) + hr * (D + 4);
+                            const float* src = place(min(i + k, share.last)) + hr * (D + 4);
                             st[k] = __ldcg(reinterpret_cast<const float2*>(src + D));
                             u[k] = __ldcg(reinterpret_cast<const float4*>(src + d0)), v[k] = __ldcg(reinterpret_cast<const float4*>(src + d0) + 1);
                         }
                         #pragma unroll
                         for (int k = 0; k < 4; ++k)
-                            if (i + k <= i1) join(o, m, l, st[k], u[k], v[k]);
+                            if (i + k <= share.last) join_row(o, m, l, st[k], u[k], v[k]);
                     }
                     store_row(hd, r, d0, o, m, l);
                 }
             }
         }
         __syncthreads();                             // the partial results' place goes back to the rings
-        pos = unit0 + to;
-        ++unit;                                      // (only if it is done: else pos is the end)
     }
 }
 
@@ -1030,7 +1076,7 @@ extern "C" int32_t ss_msa_attention_kvq(const ss_kvq_attn_params* p, void* strea
     // no more CTAs than the slab can give steps for
     const int block = 8 * group_count(*p), blocks = (q_rows(*p) + block - 1) / block;
     const long long chunks = static_cast<long long>(c.n_heads) * blocks *
-                             ((c.total_slots + kChunk - 1) / kChunk + p->batch * (1ll + extra_chunks(p->max_nodes, p->gamma, block)));
+                             ((c.total_slots + kChunk - 1) / kChunk + p->batch * (1ll + extra_chunks<kChunk>(p->max_nodes, p->gamma, block)));
     const int ctas = static_cast<int>(std::min<long long>(most_ctas(*p), chunks));
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     return c.head_dim == 128 ? launch_kvq<128>(*p, a, ctas, s) : c.head_dim == 80 ? launch_kvq<80>(*p, a, ctas, s) : launch_kvq<64>(*p, a, ctas, s);
