@@ -113,6 +113,8 @@ __device__ __forceinline__ long long row_offset(const KvqArgs& a, int hd, int b,
     return ((r.j < 0 ? node : node * a.gamma + r.j) * a.n_heads + h) * hd;
 }
 
+constexpr float kNoRef = -FLT_MAX / 2;               // reference of a partial result that has seen no key
+
 // ---- small helpers ------------------------------------------------------------------------------
 __device__ __forceinline__ uint32_t smem_addr(const void* p) { return static_cast<uint32_t>(__cvta_generic_to_shared(p)); }
 template <int BYTES>
@@ -302,6 +304,20 @@ struct Pieces {
     __device__ __forceinline__ long long place(const L& line, int i) const { return 2ll * ((i << line.team_log2) + line.member) + (i == first ? second : 0); }
 };
 
+// Eight values of a row's output, and its log-sum-exp: o / l
+template <int D, typename L>
+__device__ __forceinline__ void store_row(const KvqArgs& a, const L& line, int r, int d0, const float (&o)[8], float m, float l, int h) {
+    const Row x = row_of(line.row0 + r, line.s.T, a.gamma);
+    const long long off = row_offset(a, D, line.b, h, x);
+    const float f = 1.f / l;
+    uint4 v;
+    v.x = pack2_bf16(o[0] * f, o[1] * f), v.y = pack2_bf16(o[2] * f, o[3] * f);
+    v.z = pack2_bf16(o[4] * f, o[5] * f), v.w = pack2_bf16(o[6] * f, o[7] * f);
+    *reinterpret_cast<uint4*>((x.j < 0 ? a.o_main : a.o_spec) + off + d0) = v;
+    float* lse = x.j < 0 ? a.lse_main : a.lse_spec;
+    if (d0 == 0 && lse != nullptr) lse[off / D] = (m + log2f(l)) * 0.6931471805599453f;
+}
+
 // One more partial row into (o, m, l)
 __device__ __forceinline__ void join_row(float (&o)[8], float& m, float& l, const float2& st, const float4& u, const float4& v) {
     const float now = fmaxf(m, st.x), f = exp2_approx(m - now), e = exp2_approx(st.x - now);
@@ -401,8 +417,6 @@ __device__ __forceinline__ void raise_scale(WarpState<D, NG>& w, float scale) {
         }
     }
 }
-
-constexpr float kNoRef = -FLT_MAX / 2;               // reference of a partial result that has seen no key
 
 // Scores above their references (d, log2 units; -inf: not seen) of H tiles of 16 keys: where one is more than 8 above, references are
 // raised to the maxima and d lowered by as much.  A row that has seen no key so far takes the maximum whatever it is: so the first chunk
@@ -919,17 +933,6 @@ __global__ void __launch_bounds__(kThreads, NG == 1 ? 3 : 2) msa_attention_kvq_r
         const Pieces share(line);
         const auto place = [&](int i) { return partial + share.place(line, i) * partial_floats(D, ROWS); };
         const int rows = min(ROWS, s.rows - row0), items = max(0, min(HW, a.n_heads - h0)) * rows * (D / 8);
-        const auto store_row = [&](int hd, int r, int d0, const float (&o)[8], float m, float l) {
-            const Row x = row_of(row0 + r, s.T, a.gamma);
-            const long long off = row_offset(a, D, b, h0 + hd, x);
-            const float f = 1.f / l;
-            uint4 v;
-            v.x = pack2_bf16(o[0] * f, o[1] * f), v.y = pack2_bf16(o[2] * f, o[3] * f);
-            v.z = pack2_bf16(o[4] * f, o[5] * f), v.w = pack2_bf16(o[6] * f, o[7] * f);
-            *reinterpret_cast<uint4*>((x.j < 0 ? a.o_main : a.o_spec) + off + d0) = v;
-            float* lse = x.j < 0 ? a.lse_main : a.lse_spec;
-            if (d0 == 0 && lse != nullptr) lse[off / D] = (m + log2f(l)) * 0.6931471805599453f;
-        };
         #pragma unroll 1
         for (int item = tid; item < items; item += kThreads) {
             const int hr = item / (D / 8), d0 = (item - hr * (D / 8)) * 8, hd = hr / rows, r = hr - hd * rows;
@@ -940,7 +943,7 @@ __global__ void __launch_bounds__(kThreads, NG == 1 ? 3 : 2) msa_attention_kvq_r
                 join_row(o, m, l, stats[i * ROWS + r], *reinterpret_cast<const float4*>(src), *reinterpret_cast<const float4*>(src + 4));
             }
             if (whole) {
-                store_row(hd, r, d0, o, m, l);
+                store_row<D>(a, line, r, d0, o, m, l, h0 + hd);
             } else {
                 float* dst = place(line.me) + hr * (D + 4) + d0;
                 __stcg(reinterpret_cast<float4*>(dst), make_float4(o[0], o[1], o[2], o[3]));
@@ -977,7 +980,7 @@ __global__ void __launch_bounds__(kThreads, NG == 1 ? 3 : 2) msa_attention_kvq_r
                         for (int k = 0; k < 4; ++k)
                             if (i + k <= share.last) join_row(o, m, l, st[k], u[k], v[k]);
                     }
-                    store_row(hd, r, d0, o, m, l);
+                    store_row<D>(a, line, r, d0, o, m, l, h0 + hd);
                 }
             }
         }
@@ -985,31 +988,42 @@ __global__ void __launch_bounds__(kThreads, NG == 1 ? 3 : 2) msa_attention_kvq_r
     }
 }
 
+}  // namespace ss
+
+#include "ss_kvq_tiles.cuh"
+
+namespace ss {
+
 // ---- host ---------------------------------------------------------------------------------------
 static int q_rows(const ss_kvq_attn_params& p) { return p.max_nodes * (1 + p.gamma); }
-static int group_count(const ss_kvq_attn_params& p) { return q_rows(p) <= 8 ? 1 : 2; }
-static int most_ctas(const ss_kvq_attn_params& p) { return sm_count() * (group_count(p) == 1 ? 3 : 2); }
 
-static size_t kvq_workspace(const ss_kvq_attn_params& p) {
-    const size_t ctas = static_cast<size_t>(most_ctas(p));
-    return kWsHeaderBytes + (4 * ctas + 255) / 256 * 256 + 2 * ctas * partial_floats(p.cache.head_dim, 8 * group_count(p)) * sizeof(float);
+// Which kernel takes a call: `tile` > 0: blocks of so many rows on tcgen05, else groups of 8 rows on register-level MMAs
+struct KvqPlan {
+    int tile, groups, block, ctas;
+};
+static KvqPlan kvq_plan(const ss_kvq_attn_params& p) {
+    const int rows = q_rows(p);
+    KvqPlan k{0, rows <= 8 ? 1 : 2, 0, 0};
+    if (rows > 16) k.tile = rows <= 32 ? 32 : 64;
+    k.block = k.tile > 0 ? k.tile : 8 * k.groups;
+    k.ctas = sm_count() * (k.tile > 0 ? 1 : k.groups == 1 ? 3 : 2);
+    return k;
 }
 
-template <int D, int NG>
-static int32_t launch_kvq_rows(const KvqArgs& args, int ctas, cudaStream_t stream) {
-    const auto kernel = msa_attention_kvq_rows_kernel<D, NG>;
-    constexpr int bytes = KvqSmem<D, NG>::kBytes;
-    static bool set[64] = {};                        // (per device; setting it twice does no harm)
-    int dev = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess) return SS_ERR_CUDA;
-    if (dev < 0 || dev >= 64 || !set[dev]) {
-        if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) return SS_ERR_CUDA;
-        if (dev >= 0 && dev < 64) set[dev] = true;
-    }
+static size_t kvq_workspace(const ss_kvq_attn_params& p) {
+    const KvqPlan k = kvq_plan(p);
+    const size_t ctas = static_cast<size_t>(k.ctas), d = static_cast<size_t>(p.cache.head_dim);
+    const size_t floats = k.tile > 0 ? k.tile * (d + 4) : static_cast<size_t>(partial_floats(p.cache.head_dim, k.block));
+    return kWsHeaderBytes + (4 * ctas + 255) / 256 * 256 + 2 * ctas * floats * sizeof(float);
+}
+
+template <typename Kernel>
+static int32_t launch_kvq_kernel(Kernel kernel, int bytes, int threads, const KvqArgs& args, int ctas, cudaStream_t stream) {
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) return SS_ERR_CUDA;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(static_cast<unsigned>(ctas));
-    cfg.blockDim = dim3(kThreads);
-    cfg.dynamicSmemBytes = bytes;
+    cfg.blockDim = dim3(static_cast<unsigned>(threads));
+    cfg.dynamicSmemBytes = static_cast<size_t>(bytes);
     cfg.stream = stream;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -1020,8 +1034,11 @@ static int32_t launch_kvq_rows(const KvqArgs& args, int ctas, cudaStream_t strea
 }
 
 template <int D>
-static int32_t launch_kvq(const ss_kvq_attn_params& p, const KvqArgs& args, int ctas, cudaStream_t stream) {
-    return group_count(p) == 1 ? launch_kvq_rows<D, 1>(args, ctas, stream) : launch_kvq_rows<D, 2>(args, ctas, stream);
+static int32_t launch_kvq(const KvqPlan& k, const KvqArgs& args, int ctas, cudaStream_t stream) {
+    if (k.tile == 32) return launch_kvq_kernel(msa_attention_kvq_tiles_kernel<D, 32>, TileGeo<D, 32>::kBytes, kTileThreads, args, ctas, stream);
+    if (k.tile == 64) return launch_kvq_kernel(msa_attention_kvq_tiles_kernel<D, 64>, TileGeo<D, 64>::kBytes, kTileThreads, args, ctas, stream);
+    return k.groups == 1 ? launch_kvq_kernel(msa_attention_kvq_rows_kernel<D, 1>, KvqSmem<D, 1>::kBytes, kThreads, args, ctas, stream)
+                         : launch_kvq_kernel(msa_attention_kvq_rows_kernel<D, 2>, KvqSmem<D, 2>::kBytes, kThreads, args, ctas, stream);
 }
 
 static int32_t kvq_check_shapes(const ss_kvq_attn_params* p) {
@@ -1074,10 +1091,11 @@ extern "C" int32_t ss_msa_attention_kvq(const ss_kvq_attn_params* p, void* strea
     a.scale = p->sm_scale * 1.4426950408889634f;
     a.batch = p->batch, a.n_heads = c.n_heads, a.gamma = p->gamma, a.max_nodes = p->max_nodes;
     // no more CTAs than the slab can give steps for
-    const int block = 8 * group_count(*p), blocks = (q_rows(*p) + block - 1) / block;
-    const long long chunks = static_cast<long long>(c.n_heads) * blocks *
-                             ((c.total_slots + kChunk - 1) / kChunk + p->batch * (1ll + extra_chunks<kChunk>(p->max_nodes, p->gamma, block)));
-    const int ctas = static_cast<int>(std::min<long long>(most_ctas(*p), chunks));
+    const KvqPlan k = kvq_plan(*p);
+    const int blocks = (q_rows(*p) + k.block - 1) / k.block, chunk = k.tile > 0 ? kTileOfKeys : kChunk;
+    const int extra = k.tile > 0 ? extra_chunks<kTileOfKeys>(p->max_nodes, p->gamma, k.block) : extra_chunks<kChunk>(p->max_nodes, p->gamma, k.block);
+    const long long chunks = static_cast<long long>(c.n_heads) * blocks * ((c.total_slots + chunk - 1) / chunk + p->batch * (1ll + extra));
+    const int ctas = static_cast<int>(std::min<long long>(k.ctas, chunks));
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    return c.head_dim == 128 ? launch_kvq<128>(*p, a, ctas, s) : c.head_dim == 80 ? launch_kvq<80>(*p, a, ctas, s) : launch_kvq<64>(*p, a, ctas, s);
+    return c.head_dim == 128 ? launch_kvq<128>(k, a, ctas, s) : c.head_dim == 80 ? launch_kvq<80>(k, a, ctas, s) : launch_kvq<64>(k, a, ctas, s);
 }

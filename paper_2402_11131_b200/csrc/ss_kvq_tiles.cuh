@@ -1,0 +1,618 @@
+// Attention over a 4-bit prefix for blocks of more rows than a warp can hold, on tcgen05.  Included by ss_attention_kvq.cu.
+//
+// S^T = K Q^T and O^T = V^T P^T with 128 keys (dimensions) as the 128 lanes of TMEM and the N <= 64 query rows as columns: what
+// grows with the rows is the cheap side, and codes go from registers to TMEM as A operands, never through shared memory.
+//   K: the thread of a key turns the key's codes into bf16 c - z (exact), one TMEM lane; its scale multiplies the lane's scores.
+//   V: transposing loads (ldmatrix, 16 keys by 16 bytes) give a thread four keys' codes of two dimensions; a TMEM lane is a dimension.
+//      The scale is part of the weight that meets it.
+// Lane 32 w + x of V^T and O^T (w < D / 32) holds, for x < 16, the low codes of byte 16 w + x of a row, else the high codes of
+// byte 16 w + x - 16.
+//
+// Seventeen warps: 0..3 K, 4..7 V, 8..15 softmax (two groups of four, each half of the rows, thread = key), 16 issues the MMAs.  Two
+// buffers each for K, V, S and P, so that the five work on different tiles.  Nothing but the order of tiles is shared: every role
+// walks the same list of units.
+#pragma once
+#include "ss_tcgen05.cuh"
+
+namespace ss {
+
+constexpr int kTileOfKeys = 128, kTileThreads = 544;
+
+template <int D, int N>
+struct TileGeo {
+    static constexpr int kHalf = N / 2;                           // rows of a softmax group
+    static constexpr int kPitch = D == 128 ? 64 : D == 80 ? 48 : 32;         // bytes of a key's codes in shared memory (16-byte aligned)
+    static constexpr int kCopy = D == 80 ? 8 : 16, kPer = D / 2 / kCopy;     // asynchronous copies per key
+    static constexpr int kWords = D / 8;
+    static constexpr int kColumns = D / 2;                        // TMEM columns of a K tile
+    static constexpr int kQuads = (D + 31) / 32;                  // warps that have V lanes
+    static constexpr int kCodes = kTileOfKeys * kPitch;
+    static constexpr int kStages = 4, kParams = 8;
+    static constexpr int kBoxes = D > 64 ? 2 : 1, kBox = N * 128;
+    static constexpr int kRowOfV = 64 * kQuads;                   // bytes of a bf16 row in lane order
+    static constexpr int kP = kTileOfKeys * 128;
+    static constexpr int oP = 0, oQ = oP + 2 * kP, oK = oQ + kBoxes * kBox, oV = oK + kStages * kCodes;
+    static constexpr int oKParams = oV + kStages * kCodes, oVParams = oKParams + kParams * kTileOfKeys * 8;
+    static constexpr int kBytes = oVParams + kStages * kTileOfKeys * 4;
+    static_assert(kTileOfKeys * kRowOfV <= kStages * kCodes, "bf16 values take the place of the ring");
+    static constexpr uint32_t kTmemK = 0, kTmemV = 128, kTmemS = 256, kTmemO = 256 + 2 * N;
+    static constexpr uint32_t kIdesc = (1u << 4) | (1u << 7) | (1u << 10) | (static_cast<uint32_t>(N >> 3) << 17) | ((128u >> 4) << 24);
+    static constexpr uint32_t kIdescS = kIdesc, kIdescPV = kIdesc | (1u << 16);
+};
+
+struct TileCtrl {
+    unsigned long long k_full[2], s_full[2], s_free[2], v_full[2], p_full[2], pv_done[2], o_free, drain;
+    unsigned long long see[64];                                   // per row: ancestors; stream keys it sees; where its output goes
+    long long out[64];                                            // element offset, -1: no row
+    int2 streams[64];
+    float neg_ref[64];
+    int tile_max[2][4][32];
+    float sums[2][4][32];
+    uint32_t tmem;
+    int abort, joined;
+};
+
+__device__ __forceinline__ void tile_wait(uint32_t bar, uint32_t parity, TileCtrl& c, int* status) {
+    if (!mbar_try(bar, parity)) mbar_wait_slow(bar, parity, &c.abort, status);
+}
+// 128 threads agree on "any"
+__device__ __forceinline__ bool any_of_group(int id, bool x) {
+    uint32_t r;
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %2, 0;\n\tbar.red.or.pred q, %1, 128, p;\n\tselp.u32 %0, 1, 0, q;\n\t}" : "=r"(r) : "r"(id), "r"(static_cast<uint32_t>(x)) : "memory");
+    return r != 0u;
+}
+template <int C>
+__device__ __forceinline__ void tmem_load(uint32_t addr, uint32_t (&r)[C]) {
+    if constexpr (C == 32) tmem_ld32<0>(addr, r);
+    else if constexpr (C == 16) tmem_ld16<0>(addr, r);
+    else
+        asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                     : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]) : "r"(addr) : "memory");
+}
+template <int C, int O, int M>
+__device__ __forceinline__ void tmem_store(uint32_t addr, const uint32_t (&r)[M]) {
+    if constexpr (C == 32)
+        asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
+                     "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31};" ::SS_W16(r, O), SS_W16(r, O + 16), "r"(addr) : "memory");
+    else if constexpr (C == 16) tmem_st16<O>(addr, r);
+    else
+        asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%8], {%0,%1,%2,%3,%4,%5,%6,%7};"
+                     ::"r"(r[O]), "r"(r[O + 1]), "r"(r[O + 2]), "r"(r[O + 3]), "r"(r[O + 4]), "r"(r[O + 5]), "r"(r[O + 6]), "r"(r[O + 7]), "r"(addr) : "memory");
+}
+// 16 lanes by 32 columns: r[2 k + e] is column 4 k + lane % 4 of TMEM lane lane / 4 + 8 e
+__device__ __forceinline__ void tmem_store_lanes16(uint32_t addr, const uint32_t (&r)[16]) {
+    asm volatile("tcgen05.st.sync.aligned.16x128b.x8.b32 [%16], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15};" ::SS_W16(r, 0), "r"(addr) : "memory");
+}
+// one step of 16: A in TMEM, by the warp's elected lane
+__device__ __forceinline__ void tile_mma(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
+    asm volatile("{\n\t.reg .pred p, e;\n\telect.sync _|e, 0xffffffff;\n\tsetp.ne.b32 p, %4, 0;\n\t@e tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+                 ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(acc) : "memory");
+}
+// bytes of 16 rows (an address each, lanes 0..15) transposed: lane holds bytes 4 (lane % 4) .. of column lane / 4 (r0) and 8 further (r1)
+__device__ __forceinline__ void load_transposed_bytes(uint32_t addr, uint32_t& r0, uint32_t& r1) {
+    asm volatile("ldmatrix.sync.aligned.m16n16.x1.trans.shared.b8 {%0, %1}, [%2];" : "=r"(r0), "=r"(r1) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void load_transposed_halves(uint32_t addr, uint32_t (&r)[4]) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+// codes to bf16: 128 + c, which 128 + z is taken from
+__device__ __forceinline__ uint32_t code_plus_128(uint32_t x) {
+    uint32_t r;
+    asm("lop3.b32 %0, %1, 0x000f000f, 0x43004300, 0xea;" : "=r"(r) : "r"(x));     // (x & mask) | two bf16 of 128
+    return r;
+}
+__device__ __forceinline__ uint32_t sub_bf16x2(uint32_t a, uint32_t b) {
+    uint32_t r;
+    asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+// floats in the order of integers
+__device__ __forceinline__ int ordered(float x) {
+    const int i = __float_as_int(x);
+    return i ^ ((i >> 31) & 0x7fffffff);
+}
+__device__ __forceinline__ float from_ordered(int i) { return __int_as_float(i ^ ((i >> 31) & 0x7fffffff)); }
+
+// The keys behind the prefix of a unit
+__device__ __forceinline__ Extra extra_of(const KvqArgs& a, const Seq& s, int row0, int block) {
+    Extra x;
+    x.T = s.T, x.gamma = max(a.gamma, 1), x.row0 = row0, x.rows = s.rows, x.t0 = 0, x.count = s.T;
+    const int last = min(row0 + block, s.rows) - 1;
+    if (last >= s.T) {                               // the block has stream rows: the streams of their nodes
+        x.t0 = row0 < s.T ? 0 : (row0 - s.T) / a.gamma;
+        x.count = s.T + ((last - s.T) / a.gamma - x.t0 + 1) * a.gamma;
+    }
+    return x;
+}
+
+template <int D, int N>
+__global__ void __launch_bounds__(kTileThreads, 1) msa_attention_kvq_tiles_kernel(const __grid_constant__ KvqArgs a) {
+    using G = TileGeo<D, N>;
+    constexpr int C = G::kHalf;
+    extern __shared__ __align__(1024) unsigned char smem_raw[];
+    __shared__ __align__(16) TileCtrl c;
+    const int tid = threadIdx.x, lane = tid & 31, warp = static_cast<int>(uniform(tid >> 5)), quad = warp & 3;
+    const uint32_t smem = smem_u32(smem_raw);
+    int* const status = reinterpret_cast<int*>(a.ws);
+    wait_for_previous_kernel();
+    release_next_kernel();
+    Line<N, kTileOfKeys, 0> line;
+    if (!line.begin(a, lane)) return;                // the same for all warps
+
+    if (tid == 0) {
+        c.abort = 0;
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(smem_u32(&c.k_full[i]), 128), mbar_init(smem_u32(&c.v_full[i]), 128);
+            mbar_init(smem_u32(&c.s_free[i]), 256), mbar_init(smem_u32(&c.p_full[i]), 256);
+            mbar_init(smem_u32(&c.s_full[i]), 2), mbar_init(smem_u32(&c.pv_done[i]), 1);
+        }
+        mbar_init(smem_u32(&c.o_free), 256), mbar_init(smem_u32(&c.drain), 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 16) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&c.tmem)) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = uniform(c.tmem), lanes = static_cast<uint32_t>(32 * quad) << 16;
+    // (a wait that runs out leaves the roles in step: everyone goes through the same tiles without waiting, and no output is written)
+    const auto wait = [&](unsigned long long& bar, uint32_t parity) { tile_wait(smem_u32(&bar), parity, c, status); };
+    uint32_t tau = 0;                                // tiles so far, over all units: buffer tau & 1, phase (tau >> 1) & 1
+
+    if (warp < 4) {
+        // ---- K ------------------------------------------------------------------------------
+        const int key = tid;
+        while (line.next(a)) {
+            const Seq& s = line.s;
+            const int P = prefix_chunks<kTileOfKeys>(s.L), held = min(line.to, P), h = min(line.head0, a.n_heads - 1);
+            const bool real = line.head0 < a.n_heads;
+            // the rows of the unit before have been read once its last S is complete; the rings' last stage has been read by all
+            if (tau > 0) wait(c.s_full[(tau - 1) & 1], ((tau - 1) >> 1) & 1);
+            named_barrier(1, 128);
+            const uint32_t tau0 = tau;
+            const auto load = [&](int k) {           // codes, scales and zero points of tile k
+                if (k < held) {
+                    const long long slot0 = s.start + static_cast<long long>(k) * kTileOfKeys;
+                    const int last = s.L - 1 - k * kTileOfKeys;
+                    const uint32_t stage = smem + G::oK + ((k - line.from) % G::kStages) * G::kCodes;
+                    #pragma unroll
+                    for (int i = 0; i < G::kPer; ++i) {
+                        const int item = i * 128 + tid, row = item / G::kPer, at = item - row * G::kPer;
+                        const int place = D == 128 ? at ^ ((row >> 1) & 3) : D == 64 ? at ^ ((row >> 2) & 1) : at;
+                        copy_async<G::kCopy>(stage + row * G::kPitch + place * G::kCopy, a.k_codes + (slot0 + min(row, last)) * a.slot_stride + h * a.head_stride + at * G::kCopy);
+                    }
+                    const long long p = (slot0 + min(key, last)) * a.p_slot + h * a.p_head;
+                    const uint32_t dst = smem + G::oKParams + (((tau0 + (k - line.from)) % G::kParams) * kTileOfKeys + key) * 8;
+                    copy_async<4>(dst, a.k_params + p);
+                    copy_async<4>(dst + 4, a.v_params + p);
+                }
+                copy_commit();
+            };
+            #pragma unroll 1
+            for (int i = 0; i < G::kStages - 1; ++i) load(line.from + i);
+            // query rows, 16 bytes at a time, swizzled
+            #pragma unroll 1
+            for (int item = tid; item < N * (D / 8); item += 128) {
+                const int r = item / (D / 8), at = item - r * (D / 8);
+                uint4 v = {};
+                if (real && line.row0 + r < s.rows) {
+                    const Row x = row_of(line.row0 + r, s.T, a.gamma);
+                    v = *reinterpret_cast<const uint4*>((x.j < 0 ? a.q_main : a.q_spec) + row_offset(a, D, line.b, h, x) + 8 * at);
+                }
+                st_shared_v4(smem + G::oQ + (at >> 3) * G::kBox + r * 128 + (((at & 7) ^ (r & 7)) << 4), v.x, v.y, v.z, v.w);
+            }
+            fence_async_smem();
+            const Extra x = extra_of(a, s, line.row0, N);
+            #pragma unroll 1
+            for (int k = line.from; k < line.to; ++k, ++tau) {
+                uint32_t w[G::kWords];
+                uint32_t z = 0u;
+                const uint32_t params = smem + G::oKParams + ((tau % G::kParams) * kTileOfKeys + key) * 8;
+                if (k < held) {
+                    copy_wait<G::kStages - 2>();
+                    named_barrier(1, 128);
+                    load(k + G::kStages - 1);
+                    const uint32_t row = smem + G::oK + ((k - line.from) % G::kStages) * G::kCodes + key * G::kPitch;
+                    #pragma unroll
+                    for (int i = 0; i < G::kWords / 4; ++i) {
+                        const uint4 v = lds128(row + 16 * (D == 128 ? i ^ ((key >> 1) & 3) : D == 64 ? i ^ ((key >> 2) & 1) : i));
+                        w[4 * i] = v.x, w[4 * i + 1] = v.y, w[4 * i + 2] = v.z, w[4 * i + 3] = v.w;
+                    }
+                    if constexpr (D == 80) {
+                        const uint2 v = lds64(row + 32);
+                        w[8] = v.x, w[9] = v.y;
+                    }
+                    z = code_plus_128(__byte_perm(lds32(params), 0u, 0x3232));
+                } else {
+                    asm volatile("st.shared.v2.u32 [%0], {%1, %1};" ::"r"(params), "r"(0x3f80u) : "memory");      // scales of 1
+                }
+                if (tau >= 2) wait(c.s_full[tau & 1], ((tau - 2) >> 1) & 1);
+                tc_fence_after();
+                const uint32_t dst = tmem + G::kTmemK + (tau & 1) * 64 + lanes;
+                const int e = (k - P) * kTileOfKeys + key;
+                const __nv_bfloat16* src = nullptr;
+                if (k >= held && real && e < x.count) src = (e < x.T ? a.k_tree : a.k_spec) + extra_offset(a, x, D, line.b, h, e);
+                #pragma unroll
+                for (int i = 0; i < G::kWords; i += 8) {
+                    uint32_t r[32];
+                    #pragma unroll
+                    for (int q = 0; q < 8; ++q) {
+                        if (i + q < G::kWords) {
+                            if (k < held) {
+                                #pragma unroll
+                                for (int n = 0; n < 4; ++n) r[4 * q + n] = sub_bf16x2(code_plus_128(w[i + q] >> (4 * n)), z);
+                            } else {
+                                uint4 v = {};
+                                if (src) v = *reinterpret_cast<const uint4*>(src + 8 * (i + q));
+                                r[4 * q] = v.x, r[4 * q + 1] = v.y, r[4 * q + 2] = v.z, r[4 * q + 3] = v.w;
+                            }
+                        }
+                    }
+                    if (i + 8 <= G::kWords) tmem_store<32, 0>(dst + 4 * i, r);
+                    else tmem_store<8, 0>(dst + 4 * i, r);           // (80: the last two words)
+                }
+                tmem_wait_st();
+                tc_fence_before();
+                mbar_arrive(smem_u32(&c.k_full[tau & 1]));
+            }
+            copy_wait<0>();
+        }
+    } else if (warp < 8) {
+        // ---- V ------------------------------------------------------------------------------
+        const int t = tid - 128;
+        const bool mine = quad < G::kQuads;
+        // keys in the order in which the columns of V^T follow one another: transposed byte 4 q + e of 16 keys goes to column q (e < 2) or
+        // 4 + q, which hold keys 2 q, 2 q + 1 and 8 + 2 q, 8 + 2 q + 1
+        const int from16 = (lane & 3) < 2 ? 2 * ((lane & 15) >> 2) + (lane & 3) : 8 + 2 * ((lane & 15) >> 2) + (lane & 3) - 2;
+        while (line.next(a)) {
+            const Seq& s = line.s;
+            const int P = prefix_chunks<kTileOfKeys>(s.L), held = min(line.to, P), h = min(line.head0, a.n_heads - 1);
+            const bool real = line.head0 < a.n_heads;
+            named_barrier(2, 128);
+            const auto load = [&](int k) {
+                if (k < held) {
+                    const long long slot0 = s.start + static_cast<long long>(k) * kTileOfKeys;
+                    const int last = s.L - 1 - k * kTileOfKeys, st = (k - line.from) % G::kStages;
+                    const uint32_t stage = smem + G::oV + st * G::kCodes;
+                    #pragma unroll
+                    for (int i = 0; i < G::kPer; ++i) {
+                        const int item = i * 128 + t, row = item / G::kPer, at = item - row * G::kPer;
+                        const int place = D == 128 ? at ^ ((row >> 1) & 3) : D == 64 ? at ^ ((row >> 2) & 1) : at;
+                        copy_async<G::kCopy>(stage + row * G::kPitch + place * G::kCopy, a.v_codes + (slot0 + min(row, last)) * a.slot_stride + h * a.head_stride + at * G::kCopy);
+                    }
+                    copy_async<4>(smem + G::oVParams + (st * kTileOfKeys + t) * 4, a.v_params + (slot0 + min(t, last)) * a.p_slot + h * a.p_head);
+                }
+                copy_commit();
+            };
+            #pragma unroll 1
+            for (int i = 0; i < G::kStages - 1; ++i) load(line.from + i);
+            const Extra x = extra_of(a, s, line.row0, N);
+            #pragma unroll 1
+            for (int k = line.from; k < line.to; ++k, ++tau) {
+                const int st = (k - line.from) % G::kStages;
+                const uint32_t dst = tmem + G::kTmemV + (tau & 1) * 64 + lanes;
+                if (k < held) {
+                    copy_wait<G::kStages - 2>();
+                    named_barrier(2, 128);
+                    load(k + G::kStages - 1);
+                    if (tau >= 2) wait(c.pv_done[tau & 1], ((tau - 2) >> 1) & 1);
+                    tc_fence_after();
+                    if (mine) {
+                        const uint32_t codes = smem + G::oV + st * G::kCodes, words = smem + G::oVParams + st * kTileOfKeys * 4 + 8 * (lane & 3);
+                        #pragma unroll
+                        for (int half = 0; half < 2; ++half) {
+                            uint32_t lo[16], hi[16];
+                            #pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                const int key0 = 64 * half + 16 * i, row = key0 + from16;
+                                const int place = D == 128 ? quad ^ ((row >> 1) & 3) : D == 64 ? quad ^ ((row >> 2) & 1) : quad;
+                                uint32_t r0, r1;
+                                load_transposed_bytes(codes + row * G::kPitch + place * 16, r0, r1);
+                                const uint2 p0 = lds64(words + 4 * key0), p1 = lds64(words + 4 * key0 + 32);
+                                const uint32_t z0 = code_plus_128(__byte_perm(p0.x, p0.y, 0x7632)), z1 = code_plus_128(__byte_perm(p1.x, p1.y, 0x7632));
+                                const uint32_t e0 = __byte_perm(r0, 0u, 0x4140), e1 = __byte_perm(r0, 0u, 0x4342);
+                                const uint32_t f0 = __byte_perm(r1, 0u, 0x4140), f1 = __byte_perm(r1, 0u, 0x4342);
+                                lo[4 * i] = sub_bf16x2(code_plus_128(e0), z0), lo[4 * i + 1] = sub_bf16x2(code_plus_128(f0), z0);
+                                lo[4 * i + 2] = sub_bf16x2(code_plus_128(e1), z1), lo[4 * i + 3] = sub_bf16x2(code_plus_128(f1), z1);
+                                hi[4 * i] = sub_bf16x2(code_plus_128(e0 >> 4), z0), hi[4 * i + 1] = sub_bf16x2(code_plus_128(f0 >> 4), z0);
+                                hi[4 * i + 2] = sub_bf16x2(code_plus_128(e1 >> 4), z1), hi[4 * i + 3] = sub_bf16x2(code_plus_128(f1 >> 4), z1);
+                            }
+                            tmem_store_lanes16(dst + 32 * half, lo);
+                            tmem_store_lanes16(dst + 32 * half + (16u << 16), hi);
+                        }
+                    }
+                } else {
+                    // bf16 rows in the order of the lanes: of 8 values the low codes' would be 0, 4, 1, 5, the high codes' 2, 6, 3, 7
+                    const int e = (k - P) * kTileOfKeys + t;
+                    const __nv_bfloat16* src = nullptr;
+                    if (real && e < x.count) src = (e < x.T ? a.v_tree : a.v_spec) + extra_offset(a, x, D, line.b, h, e);
+                    named_barrier(2, 128);
+                    const uint32_t row = smem + G::oV + t * G::kRowOfV;
+                    #pragma unroll
+                    for (int i = 0; i < 4 * G::kQuads; ++i) {
+                        uint4 v = {};
+                        if (src && i < G::kWords) v = *reinterpret_cast<const uint4*>(src + 8 * i);
+                        // bytes: 64 to a quad, low ones first, 8 to a word; 16-byte places swizzled by the key
+                        const int at = 64 * (i >> 2) + 8 * (i & 3);
+                        const uint32_t lo = row + (((at >> 4) ^ (t & 3)) << 4) + (at & 15), hi = row + ((((at + 32) >> 4) ^ (t & 3)) << 4) + (at & 15);
+                        st_shared_v2(lo, __byte_perm(v.x, v.z, 0x5410), __byte_perm(v.x, v.z, 0x7632));
+                        st_shared_v2(hi, __byte_perm(v.y, v.w, 0x5410), __byte_perm(v.y, v.w, 0x7632));
+                    }
+                    named_barrier(2, 128);
+                    if (tau >= 2) wait(c.pv_done[tau & 1], ((tau - 2) >> 1) & 1);
+                    tc_fence_after();
+                    if (mine) {
+                        #pragma unroll 1
+                        for (int part = 0; part < 4; ++part) {       // low and high lanes of 64 keys each
+                            const int half = part >> 1, high = part & 1;
+                            uint32_t r[16];
+                            #pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                const int kk = 64 * half + 16 * i + 8 * (lane >> 4) + (lane & 7);          // matrices: dims 0..7, 8..15 of 8 keys, then of 8 more
+                                const int at = 64 * quad + 32 * high + 16 * ((lane >> 3) & 1);
+                                uint32_t q[4];
+                                load_transposed_halves(smem + G::oV + kk * G::kRowOfV + (((at >> 4) ^ (kk & 3)) << 4), q);
+                                r[4 * i] = q[0], r[4 * i + 1] = q[1], r[4 * i + 2] = q[2], r[4 * i + 3] = q[3];
+                            }
+                            tmem_store_lanes16(dst + 32 * half + (high ? 16u << 16 : 0u), r);
+                        }
+                    }
+                }
+                tmem_wait_st();
+                tc_fence_before();
+                mbar_arrive(smem_u32(&c.v_full[tau & 1]));
+            }
+            copy_wait<0>();
+        }
+    } else if (warp < 16) {
+        // ---- softmax ------------------------------------------------------------------------
+        const int group = (warp - 8) >> 2, key = 32 * quad + lane, bar = 3 + group;
+        const uint32_t all = C == 32 ? 0xffffffffu : (1u << C) - 1u;
+        uint32_t unit = 0;
+        int* const counters = reinterpret_cast<int*>(a.ws + kWsHeaderBytes);
+        float* const partial = reinterpret_cast<float*>(a.ws + kWsHeaderBytes + (4ull * gridDim.x + 255) / 256 * 256);
+        constexpr int kPartial = N * (D + 4);
+        // TMEM lane to dimension
+        const int byte = 16 * quad + (lane & 15), dim = 8 * (byte >> 2) + ((byte & 1) << 2) + ((byte >> 1) & 1) + ((lane >> 4) << 1);
+        while (line.next(a)) {
+            const Seq& s = line.s;
+            const int P = prefix_chunks<kTileOfKeys>(s.L);
+            const Extra x = extra_of(a, s, line.row0, N);
+            named_barrier(bar, 128);                 // the rows before are done with
+            if (key < C) {
+                const int n = group * C + key, r = line.row0 + n;
+                unsigned long long see = 0;
+                long long out = -1;
+                int2 st = make_int2(0, 0);
+                if (r < s.rows && line.head0 < a.n_heads) {
+                    const Row q = row_of(r, s.T, a.gamma);
+                    see = a.trees[line.b].anc_mask[q.t];
+                    const int first = s.T + (q.t - x.t0) * x.gamma;
+                    st = make_int2(first, q.j < 0 ? first : first + q.j + 1);
+                    out = row_offset(a, D, line.b, line.head0, q);
+                }
+                c.see[n] = see, c.streams[n] = st, c.out[n] = out, c.neg_ref[n] = 0.f;
+            }
+            named_barrier(bar, 128);
+            float l[C];
+            #pragma unroll
+            for (int i = 0; i < C; ++i) l[i] = 0.f;
+            uint32_t seen = 0u;                      // rows that have seen a key (the same in all warps of the group)
+            #pragma unroll 1
+            for (int k = line.from; k < line.to; ++k, ++tau) {
+                const uint32_t parity = (tau >> 1) & 1;
+                wait(c.s_full[tau & 1], parity);
+                tc_fence_after();
+                uint32_t raw[C];
+                tmem_load<C>(tmem + G::kTmemS + (tau & 1) * N + group * C + lanes, raw);
+                const uint2 params = lds64(smem + G::oKParams + ((tau % G::kParams) * kTileOfKeys + key) * 8);
+                tmem_wait_ld();
+                tc_fence_before();
+                mbar_arrive(smem_u32(&c.s_free[tau & 1]));
+                const float sk = scale_of(params.x) * a.scale, sv = scale_of(params.y);
+                float d[C];
+                #pragma unroll
+                for (int i = 0; i < C; i += 4) {
+                    const float4 r = *reinterpret_cast<const float4*>(&c.neg_ref[group * C + i]);
+                    d[i] = fmaf(sk, __uint_as_float(raw[i]), r.x), d[i + 1] = fmaf(sk, __uint_as_float(raw[i + 1]), r.y);
+                    d[i + 2] = fmaf(sk, __uint_as_float(raw[i + 2]), r.z), d[i + 3] = fmaf(sk, __uint_as_float(raw[i + 3]), r.w);
+                }
+                if (k < P) {
+                    if ((k + 1) * kTileOfKeys > s.L && k * kTileOfKeys + key >= s.L) {
+                        #pragma unroll
+                        for (int i = 0; i < C; ++i) d[i] = -INFINITY;
+                    }
+                } else {
+                    const int e = (k - P) * kTileOfKeys + key;
+                    #pragma unroll
+                    for (int i = 0; i < C; ++i) {
+                        const int2 st = c.streams[group * C + i];
+                        const bool ok = e < x.T ? (c.see[group * C + i] >> e & 1ull) : (e >= st.x && e < st.y);
+                        if (!ok) d[i] = -INFINITY;
+                    }
+                }
+                float most = d[0];
+                #pragma unroll
+                for (int i = 1; i < C; ++i) most = fmaxf(most, d[i]);
+                if (any_of_group(bar, most > 8.f || k == line.from || (k >= P && seen != all))) {
+                    // references go up to the maxima (a row's first one: to its maximum, whatever it is)
+                    int own = 0;
+                    #pragma unroll
+                    for (int i = 0; i < C; ++i) {
+                        const int m = __reduce_max_sync(0xffffffffu, ordered(d[i]));
+                        if (lane == i) own = m;
+                    }
+                    if (lane < C) c.tile_max[group][quad][lane] = own;
+                    named_barrier(bar, 128);
+                    float by = 0.f, f = 1.f;
+                    bool any = false;
+                    if (lane < C) {
+                        const float m = from_ordered(max(max(c.tile_max[group][0][lane], c.tile_max[group][1][lane]), max(c.tile_max[group][2][lane], c.tile_max[group][3][lane])));
+                        any = m > -INFINITY;
+                        if (seen >> lane & 1u) by = fmaxf(m, 0.f), f = exp2_approx(-by);
+                        else if (any) by = m;
+                        if (quad == 0) c.neg_ref[group * C + lane] -= by;
+                    }
+                    seen |= __ballot_sync(0xffffffffu, any);
+                    #pragma unroll
+                    for (int i = 0; i < C; ++i) {
+                        d[i] -= __shfl_sync(0xffffffffu, by, i);
+                        l[i] *= __shfl_sync(0xffffffffu, f, i);
+                    }
+                    if (k > line.from) {             // and O with them: the products so far are complete, this tile's waits for our weights
+                        wait(c.pv_done[(tau - 1) & 1], ((tau - 1) >> 1) & 1);
+                        tc_fence_after();
+                        tmem_load<C>(tmem + G::kTmemO + group * C + lanes, raw);
+                        tmem_wait_ld();
+                        #pragma unroll
+                        for (int i = 0; i < C; ++i) raw[i] = __float_as_uint(__uint_as_float(raw[i]) * __shfl_sync(0xffffffffu, f, i));
+                        tmem_store<C, 0>(tmem + G::kTmemO + group * C + lanes, raw);
+                        tmem_wait_st();
+                        tc_fence_before();
+                    }
+                    named_barrier(bar, 128);
+                }
+                if (tau >= 2) wait(c.pv_done[tau & 1], ((tau - 2) >> 1) & 1);
+                #pragma unroll
+                for (int i = 0; i < C; i += 8) {
+                    uint32_t y[4];
+                    #pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        const float u = exp2_approx(d[i + 2 * q]), v = exp2_approx(d[i + 2 * q + 1]);
+                        l[i + 2 * q] += u, l[i + 2 * q + 1] += v;
+                        y[q] = pack2_bf16(u * sv, v * sv);
+                    }
+                    st_shared_v4(smem + G::oP + (tau & 1) * G::kP + key * 128 + (((group * (C / 8) + (i >> 3)) ^ (key & 7)) << 4), y[0], y[1], y[2], y[3]);
+                }
+                fence_async_smem();
+                mbar_arrive(smem_u32(&c.p_full[tau & 1]));
+            }
+            // ---- the unit's end: sums over the keys, O
+            wait(c.pv_done[(tau - 1) & 1], ((tau - 1) >> 1) & 1);
+            tc_fence_after();
+            uint32_t raw[C];
+            tmem_load<C>(tmem + G::kTmemO + group * C + lanes, raw);
+            #pragma unroll
+            for (int w = 16; w >= C; w >>= 1) {      // (fewer rows than lanes: whole sums first)
+                #pragma unroll
+                for (int i = 0; i < C; ++i) l[i] += __shfl_xor_sync(0xffffffffu, l[i], w);
+            }
+            #pragma unroll
+            for (int w = C / 2; w > 0; w >>= 1) {    // lane i ends with row i
+                #pragma unroll
+                for (int i = 0; i < w; ++i) {
+                    const bool up = lane & w;
+                    const float give = up ? l[i] : l[i + w], keep = up ? l[i + w] : l[i];
+                    l[i] = keep + __shfl_xor_sync(0xffffffffu, give, w);
+                }
+            }
+            c.sums[group][quad][lane] = l[0];
+            named_barrier(bar, 128);
+            const int at = lane & (C - 1);
+            const float sum = (c.sums[group][0][at] + c.sums[group][1][at]) + (c.sums[group][2][at] + c.sums[group][3][at]);
+            const float ref = -c.neg_ref[group * C + at];
+            tmem_wait_ld();
+            tc_fence_before();
+            mbar_arrive(smem_u32(&c.o_free));
+            const bool ok = *const_cast<volatile int*>(&c.abort) == 0;
+            const Pieces share(line);
+            float* const mine = partial + share.place(line, line.me) * kPartial;
+            const int rows = line.head0 < a.n_heads ? min(N, s.rows - line.row0) : 0;
+            if (line.whole()) {
+                const float f = 1.f / sum;
+                if (quad == 0 && lane < C && ok) {
+                    const int n = group * C + lane;
+                    if (n < rows) {
+                        float* lse = line.row0 + n < s.T ? a.lse_main : a.lse_spec;
+                        if (lse != nullptr) lse[c.out[n] / D] = (ref + log2f(sum)) * 0.6931471805599453f;
+                    }
+                }
+                #pragma unroll
+                for (int i = 0; i < C; ++i) {
+                    const float y = __uint_as_float(raw[i]) * __shfl_sync(0xffffffffu, f, i);
+                    const int n = group * C + i;
+                    if (n < rows && dim < D && ok) (line.row0 + n < s.T ? a.o_main : a.o_spec)[c.out[n] + dim] = __float2bfloat16_rn(y);
+                }
+            } else {
+                if (quad == 0 && lane < C && group * C + lane < rows)
+                    __stcg(reinterpret_cast<float2*>(mine + (group * C + lane) * (D + 4) + D), make_float2(seen >> lane & 1u ? ref : kNoRef, sum));
+                #pragma unroll
+                for (int i = 0; i < C; ++i)
+                    if (group * C + i < rows && dim < D) __stcg(mine + (group * C + i) * (D + 4) + dim, __uint_as_float(raw[i]));
+                __threadfence();
+                named_barrier(5, 256);
+                if (tid == 256) {
+                    int* const counter = counters + (share.first << line.team_log2) + line.member;
+                    c.joined = atomicAdd(counter, 1) == share.last - share.first;
+                    if (c.joined) *counter = 0;
+                    __threadfence();
+                }
+                named_barrier(5, 256);
+                if (c.joined) {
+                    #pragma unroll 1
+                    for (int item = tid - 256; item < rows * (D / 8); item += 256) {
+                        const int r = item / (D / 8), d0 = (item - r * (D / 8)) * 8;
+                        float m = kNoRef, sm = 0.f, o[8] = {};
+                        #pragma unroll 1
+                        for (int i = share.first; i <= share.last; i += 2) {
+                            float2 st[2];
+                            float4 u[2], v[2];
+                            #pragma unroll
+                            for (int q = 0; q < 2; ++q) {
+                                const float* src = partial + share.place(line, min(i + q, share.last)) * kPartial + r * (D + 4);
+                                st[q] = __ldcg(reinterpret_cast<const float2*>(src + D));
+                                u[q] = __ldcg(reinterpret_cast<const float4*>(src + d0)), v[q] = __ldcg(reinterpret_cast<const float4*>(src + d0) + 1);
+                            }
+                            #pragma unroll
+                            for (int q = 0; q < 2; ++q)
+                                if (i + q <= share.last) join_row(o, m, sm, st[q], u[q], v[q]);
+                        }
+                        if (ok) store_row<D>(a, line, r, d0, o, m, sm, line.head0);
+                    }
+                }
+            }
+            ++unit;
+        }
+    } else {
+        // ---- MMAs ---------------------------------------------------------------------------
+        uint32_t unit = 0;
+        while (line.next(a)) {
+            const auto product = [&](uint32_t t, bool first) {       // O^T (+)= V^T P^T of tile t
+                if (first && unit > 0) wait(c.o_free, (unit - 1) & 1);
+                wait(c.v_full[t & 1], (t >> 1) & 1);
+                wait(c.p_full[t & 1], (t >> 1) & 1);
+                tc_fence_after();
+                const uint64_t b = desc_mn_major(uniform(smem + G::oP + (t & 1) * G::kP), 0);
+                const uint32_t va = tmem + G::kTmemV + (t & 1) * 64;
+                #pragma unroll
+                for (int i = 0; i < kTileOfKeys / 16; ++i) tile_mma(tmem + G::kTmemO, va + 8 * i, b + 128 * i, G::kIdescPV, first && i == 0 ? 0u : 1u);
+                tc_commit_e(smem_u32(&c.pv_done[t & 1]));
+            };
+            #pragma unroll 1
+            for (int k = line.from; k < line.to; ++k, ++tau) {
+                wait(c.k_full[tau & 1], (tau >> 1) & 1);
+                if (tau >= 2) wait(c.s_free[tau & 1], ((tau - 2) >> 1) & 1);
+                tc_fence_after();
+                const uint32_t ka = tmem + G::kTmemK + (tau & 1) * 64, sd = tmem + G::kTmemS + (tau & 1) * N;
+                #pragma unroll
+                for (int i = 0; i < D / 16; ++i)
+                    tile_mma(sd, ka + 8 * i, desc_k_major(uniform(smem + G::oQ + (i >> 2) * G::kBox)) + 2 * (i & 3), G::kIdescS, i == 0 ? 0u : 1u);
+                tc_commit_e(smem_u32(&c.s_full[tau & 1]));
+                if (lane == 0) mbar_arrive(smem_u32(&c.s_full[tau & 1]));            // (passes on what the K warps have written: the keys' scales)
+                if (k > line.from) product(tau - 1, k - 1 == line.from);
+            }
+            product(tau - 1, line.to - 1 == line.from);
+            ++unit;
+        }
+        tc_commit_e(smem_u32(&c.drain));
+        mbar_drain(smem_u32(&c.drain), 0);           // (nothing is in flight when TMEM goes back)
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    if (warp == 16) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem));
+}
+
+}  // namespace ss

@@ -36,7 +36,7 @@ __device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity) {
     return ok != 0;
 }
 // Bounded wait: gives up when another thread of the CTA already gave up, or after kWaitCycles.
-__device__ __noinline__ bool mbar_wait_slow(uint32_t bar, uint32_t parity, volatile int* abort, int* status) {
+static __device__ __noinline__ bool mbar_wait_slow(uint32_t bar, uint32_t parity, volatile int* abort, int* status) {
     const long long t0 = clock64();
     for (;;) {
         for (int i = 0; i < 256; ++i) {
@@ -63,7 +63,7 @@ __device__ __forceinline__ bool mbar_wait_warp(uint32_t bar, uint32_t parity, vo
 __device__ __forceinline__ long long limit_cycles(const int& wait_limit) {
     return static_cast<long long>(*const_cast<const volatile int*>(&wait_limit)) << 10;
 }
-__device__ __noinline__ bool mbar_wait_limit_slow(uint32_t bar, uint32_t parity, volatile int* abort, const int* wait_limit, int* status) {
+static __device__ __noinline__ bool mbar_wait_limit_slow(uint32_t bar, uint32_t parity, volatile int* abort, const int* wait_limit, int* status) {
     const long long t0 = clock64(), limit = limit_cycles(*wait_limit);
     for (;;) {
         for (int i = 0; i < 256; ++i) {
@@ -105,7 +105,7 @@ __device__ __forceinline__ bool mbar_wait_uniform(uint32_t bar, uint32_t parity,
     return true;
 }
 // after giving up: a short bounded wait that lets a copy already in flight land
-__device__ __noinline__ void mbar_drain(uint32_t bar, uint32_t parity) {
+static __device__ __noinline__ void mbar_drain(uint32_t bar, uint32_t parity) {
     const long long t0 = clock64();
     while (!mbar_try(bar, parity) && clock64() - t0 < kWaitCycles / 16) {}
 }
