@@ -40,6 +40,14 @@ struct TileGeo {
     static constexpr uint32_t kIdescS = kIdesc, kIdescPV = kIdesc | (1u << 16);
 };
 
+// A role's place in the list of units: the role's first thread goes on, the others read.  In shared memory, since it is used between
+// units only and would cost every thread some 40 registers.
+template <int N>
+struct TileWalk {
+    Line<N, kTileOfKeys, 0> line;
+    int more;
+};
+
 struct TileCtrl {
     unsigned long long k_full[2], s_full[2], s_free[2], v_full[2], p_full[2], pv_done[2], o_free, drain;
     unsigned long long see[64];                                   // per row: ancestors; stream keys it sees; where its output goes
@@ -83,10 +91,18 @@ __device__ __forceinline__ void tmem_store(uint32_t addr, const uint32_t (&r)[M]
 __device__ __forceinline__ void tmem_store_lanes16(uint32_t addr, const uint32_t (&r)[16]) {
     asm volatile("tcgen05.st.sync.aligned.16x128b.x8.b32 [%16], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15};" ::SS_W16(r, 0), "r"(addr) : "memory");
 }
-// one step of 16: A in TMEM, by the warp's elected lane
+// STEPS (1 or 4) steps of 16 with A in TMEM (8 columns a step), by the warp's elected lane; B K-major (32 bytes a step)
+template <int STEPS>
 __device__ __forceinline__ void tile_mma(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
-    asm volatile("{\n\t.reg .pred p, e;\n\telect.sync _|e, 0xffffffff;\n\tsetp.ne.b32 p, %4, 0;\n\t@e tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
-                 ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(acc) : "memory");
+    const uint32_t blo = static_cast<uint32_t>(b), bhi = static_cast<uint32_t>(b >> 32);
+    if constexpr (STEPS == 1)
+        asm volatile("{\n\t.reg .pred p, e;\n\t.reg .b64 b;\n\telect.sync _|e, 0xffffffff;\n\tsetp.ne.b32 p, %5, 0;\n\tmov.b64 b, {%2, %3};\n\t"
+                     "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], b, %4, p;\n\t}" ::"r"(d), "r"(a), "r"(blo), "r"(bhi), "r"(idesc), "r"(acc) : "memory");
+    else
+        asm volatile("{\n\t.reg .pred p, e, t;\n\t.reg .b32 x, y;\n\t.reg .b64 b;\n\telect.sync _|e, 0xffffffff;\n\tsetp.ne.b32 p, %5, 0;\n\tsetp.eq.u32 t, 0, 0;\n\t"
+                     "mov.b64 b, {%2, %3};\n\t@e tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], b, %4, p;\n\t"
+                     SS_MMA_NEXT_TS("8", "2") SS_MMA_NEXT_TS("16", "4") SS_MMA_NEXT_TS("24", "6") "}"
+                     ::"r"(d), "r"(a), "r"(blo), "r"(bhi), "r"(idesc), "r"(acc) : "memory");
 }
 // bytes of 16 rows (an address each, lanes 0..15) transposed: lane holds bytes 4 (lane % 4) .. of column lane / 4 (r0) and 8 further (r1)
 __device__ __forceinline__ void load_transposed_bytes(uint32_t addr, uint32_t& r0, uint32_t& r1) {
@@ -131,13 +147,19 @@ __global__ void __launch_bounds__(kTileThreads, 1) msa_attention_kvq_tiles_kerne
     constexpr int C = G::kHalf;
     extern __shared__ __align__(1024) unsigned char smem_raw[];
     __shared__ __align__(16) TileCtrl c;
+    __shared__ __align__(16) TileWalk<N> walks[5];    // K, V, two softmax groups, MMAs
     const int tid = threadIdx.x, lane = tid & 31, warp = static_cast<int>(uniform(tid >> 5)), quad = warp & 3;
     const uint32_t smem = smem_u32(smem_raw);
     int* const status = reinterpret_cast<int*>(a.ws);
     wait_for_previous_kernel();
     release_next_kernel();
-    Line<N, kTileOfKeys, 0> line;
-    if (!line.begin(a, lane)) return;                // the same for all warps
+    if (warp < 5) {
+        Line<N, kTileOfKeys, 0> line;
+        const bool any = line.begin(a, lane);
+        if (lane == 0) walks[warp].line = line, walks[warp].more = any;
+    }
+    __syncthreads();
+    if (walks[0].more == 0) return;
 
     if (tid == 0) {
         c.abort = 0;
@@ -159,24 +181,31 @@ __global__ void __launch_bounds__(kTileThreads, 1) msa_attention_kvq_tiles_kerne
     const uint32_t tmem = uniform(c.tmem), lanes = static_cast<uint32_t>(32 * quad) << 16;
     // (a wait that runs out leaves the roles in step: everyone goes through the same tiles without waiting, and no output is written)
     const auto wait = [&](unsigned long long& bar, uint32_t parity) { tile_wait(smem_u32(&bar), parity, c, status); };
+    // on to the next unit, all `threads` threads of a role together; id: their barrier
+    const auto next_unit = [&](TileWalk<N>& w, bool leader, int id, int threads) {
+        if (threads > 32) named_barrier(id, threads); else __syncwarp();
+        if (leader) w.more = w.line.next(a);
+        if (threads > 32) named_barrier(id, threads); else __syncwarp();
+        return w.more != 0;
+    };
     uint32_t tau = 0;                                // tiles so far, over all units: buffer tau & 1, phase (tau >> 1) & 1
 
     if (warp < 4) {
         // ---- K ------------------------------------------------------------------------------
         const int key = tid;
-        while (line.next(a)) {
-            const Seq& s = line.s;
-            const int P = prefix_chunks<kTileOfKeys>(s.L), held = min(line.to, P), h = min(line.head0, a.n_heads - 1);
+        const Line<N, kTileOfKeys, 0>& line = walks[0].line;
+        while (next_unit(walks[0], tid == 0, 1, 128)) {
+            const Seq s = line.s;
+            const int P = prefix_chunks<kTileOfKeys>(s.L), from = line.from, to = line.to, held = min(to, P), h = min(line.head0, a.n_heads - 1);
             const bool real = line.head0 < a.n_heads;
-            // the rows of the unit before have been read once its last S is complete; the rings' last stage has been read by all
+            // (the ring's last stage has been read by all, and the unit before's rows once its last S is complete)
             if (tau > 0) wait(c.s_full[(tau - 1) & 1], ((tau - 1) >> 1) & 1);
-            named_barrier(1, 128);
             const uint32_t tau0 = tau;
             const auto load = [&](int k) {           // codes, scales and zero points of tile k
                 if (k < held) {
                     const long long slot0 = s.start + static_cast<long long>(k) * kTileOfKeys;
                     const int last = s.L - 1 - k * kTileOfKeys;
-                    const uint32_t stage = smem + G::oK + ((k - line.from) % G::kStages) * G::kCodes;
+                    const uint32_t stage = smem + G::oK + ((k - from) % G::kStages) * G::kCodes;
                     #pragma unroll
                     for (int i = 0; i < G::kPer; ++i) {
                         const int item = i * 128 + tid, row = item / G::kPer, at = item - row * G::kPer;
@@ -184,14 +213,14 @@ __global__ void __launch_bounds__(kTileThreads, 1) msa_attention_kvq_tiles_kerne
                         copy_async<G::kCopy>(stage + row * G::kPitch + place * G::kCopy, a.k_codes + (slot0 + min(row, last)) * a.slot_stride + h * a.head_stride + at * G::kCopy);
                     }
                     const long long p = (slot0 + min(key, last)) * a.p_slot + h * a.p_head;
-                    const uint32_t dst = smem + G::oKParams + (((tau0 + (k - line.from)) % G::kParams) * kTileOfKeys + key) * 8;
+                    const uint32_t dst = smem + G::oKParams + (((tau0 + (k - from)) % G::kParams) * kTileOfKeys + key) * 8;
                     copy_async<4>(dst, a.k_params + p);
                     copy_async<4>(dst + 4, a.v_params + p);
                 }
                 copy_commit();
             };
             #pragma unroll 1
-            for (int i = 0; i < G::kStages - 1; ++i) load(line.from + i);
+            for (int i = 0; i < G::kStages - 1; ++i) load(from + i);
             // query rows, 16 bytes at a time, swizzled
             #pragma unroll 1
             for (int item = tid; item < N * (D / 8); item += 128) {
@@ -206,7 +235,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) msa_attention_kvq_tiles_kerne
             fence_async_smem();
             const Extra x = extra_of(a, s, line.row0, N);
             #pragma unroll 1
-            for (int k = line.from; k < line.to; ++k, ++tau) {
+            for (int k = from; k < to; ++k, ++tau) {
                 uint32_t w[G::kWords];
                 uint32_t z = 0u;
                 const uint32_t params = smem + G::oKParams + ((tau % G::kParams) * kTileOfKeys + key) * 8;
@@ -214,7 +243,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) msa_attention_kvq_tiles_kerne
                     copy_wait<G::kStages - 2>();
                     named_barrier(1, 128);
                     load(k + G::kStages - 1);
-                    const uint32_t row = smem + G::oK + ((k - line.from) % G::kStages) * G::kCodes + key * G::kPitch;
+                    const uint32_t row = smem + G::oK + ((k - from) % G::kStages) * G::kCodes + key * G::kPitch;
                     #pragma unroll
                     for (int i = 0; i < G::kWords / 4; ++i) {
                         const uint4 v = lds128(row + 16 * (D == 128 ? i ^ ((key >> 1) & 3) : D == 64 ? i ^ ((key >> 2) & 1) : i));
@@ -266,15 +295,15 @@ __global__ void __launch_bounds__(kTileThreads, 1) msa_attention_kvq_tiles_kerne
         // keys in the order in which the columns of V^T follow one another: transposed byte 4 q + e of 16 keys goes to column q (e < 2) or
         // 4 + q, which hold keys 2 q, 2 q + 1 and 8 + 2 q, 8 + 2 q + 1
         const int from16 = (lane & 3) < 2 ? 2 * ((lane & 15) >> 2) + (lane & 3) : 8 + 2 * ((lane & 15) >> 2) + (lane & 3) - 2;
-        while (line.next(a)) {
-            const Seq& s = line.s;
-            const int P = prefix_chunks<kTileOfKeys>(s.L), held = min(line.to, P), h = min(line.head0, a.n_heads - 1);
+        const Line<N, kTileOfKeys, 0>& line = walks[1].line;
+        while (next_unit(walks[1], t == 0, 2, 128)) {            // (the ring's last stage has been read by all)
+            const Seq s = line.s;
+            const int P = prefix_chunks<kTileOfKeys>(s.L), from = line.from, to = line.to, held = min(to, P), h = min(line.head0, a.n_heads - 1);
             const bool real = line.head0 < a.n_heads;
-            named_barrier(2, 128);
             const auto load = [&](int k) {
                 if (k < held) {
                     const long long slot0 = s.start + static_cast<long long>(k) * kTileOfKeys;
-                    const int last = s.L - 1 - k * kTileOfKeys, st = (k - line.from) % G::kStages;
+                    const int last = s.L - 1 - k * kTileOfKeys, st = (k - from) % G::kStages;
                     const uint32_t stage = smem + G::oV + st * G::kCodes;
                     #pragma unroll
                     for (int i = 0; i < G::kPer; ++i) {
@@ -287,11 +316,11 @@ __global__ void __launch_bounds__(kTileThreads, 1) msa_attention_kvq_tiles_kerne
                 copy_commit();
             };
             #pragma unroll 1
-            for (int i = 0; i < G::kStages - 1; ++i) load(line.from + i);
+            for (int i = 0; i < G::kStages - 1; ++i) load(from + i);
             const Extra x = extra_of(a, s, line.row0, N);
             #pragma unroll 1
-            for (int k = line.from; k < line.to; ++k, ++tau) {
-                const int st = (k - line.from) % G::kStages;
+            for (int k = from; k < to; ++k, ++tau) {
+                const int st = (k - from) % G::kStages;
                 const uint32_t dst = tmem + G::kTmemV + (tau & 1) * 64 + lanes;
                 if (k < held) {
                     copy_wait<G::kStages - 2>();
@@ -376,11 +405,11 @@ __global__ void __launch_bounds__(kTileThreads, 1) msa_attention_kvq_tiles_kerne
         constexpr int kPartial = N * (D + 4);
         // TMEM lane to dimension
         const int byte = 16 * quad + (lane & 15), dim = 8 * (byte >> 2) + ((byte & 1) << 2) + ((byte >> 1) & 1) + ((lane >> 4) << 1);
-        while (line.next(a)) {
+        const Line<N, kTileOfKeys, 0>& line = walks[2 + group].line;
+        while (next_unit(walks[2 + group], key == 0, bar, 128)) {
             const Seq& s = line.s;
-            const int P = prefix_chunks<kTileOfKeys>(s.L);
+            const int L = s.L, P = prefix_chunks<kTileOfKeys>(L), from = line.from, to = line.to;
             const Extra x = extra_of(a, s, line.row0, N);
-            named_barrier(bar, 128);                 // the rows before are done with
             if (key < C) {
                 const int n = group * C + key, r = line.row0 + n;
                 unsigned long long see = 0;
@@ -401,7 +430,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) msa_attention_kvq_tiles_kerne
             for (int i = 0; i < C; ++i) l[i] = 0.f;
             uint32_t seen = 0u;                      // rows that have seen a key (the same in all warps of the group)
             #pragma unroll 1
-            for (int k = line.from; k < line.to; ++k, ++tau) {
+            for (int k = from; k < to; ++k, ++tau) {
                 const uint32_t parity = (tau >> 1) & 1;
                 wait(c.s_full[tau & 1], parity);
                 tc_fence_after();
@@ -413,14 +442,15 @@ __global__ void __launch_bounds__(kTileThreads, 1) msa_attention_kvq_tiles_kerne
                 mbar_arrive(smem_u32(&c.s_free[tau & 1]));
                 const float sk = scale_of(params.x) * a.scale, sv = scale_of(params.y);
                 float d[C];
+                const unsigned long long sk2 = pack_f32x2(sk, sk);
                 #pragma unroll
                 for (int i = 0; i < C; i += 4) {
                     const float4 r = *reinterpret_cast<const float4*>(&c.neg_ref[group * C + i]);
-                    d[i] = fmaf(sk, __uint_as_float(raw[i]), r.x), d[i + 1] = fmaf(sk, __uint_as_float(raw[i + 1]), r.y);
-                    d[i + 2] = fmaf(sk, __uint_as_float(raw[i + 2]), r.z), d[i + 3] = fmaf(sk, __uint_as_float(raw[i + 3]), r.w);
+                    unpack_f32x2(fma_f32x2(sk2, pack_f32x2(__uint_as_float(raw[i]), __uint_as_float(raw[i + 1])), pack_f32x2(r.x, r.y)), d[i], d[i + 1]);
+                    unpack_f32x2(fma_f32x2(sk2, pack_f32x2(__uint_as_float(raw[i + 2]), __uint_as_float(raw[i + 3])), pack_f32x2(r.z, r.w)), d[i + 2], d[i + 3]);
                 }
                 if (k < P) {
-                    if ((k + 1) * kTileOfKeys > s.L && k * kTileOfKeys + key >= s.L) {
+                    if ((k + 1) * kTileOfKeys > L && k * kTileOfKeys + key >= L) {
                         #pragma unroll
                         for (int i = 0; i < C; ++i) d[i] = -INFINITY;
                     }
@@ -436,7 +466,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) msa_attention_kvq_tiles_kerne
                 float most = d[0];
                 #pragma unroll
                 for (int i = 1; i < C; ++i) most = fmaxf(most, d[i]);
-                if (any_of_group(bar, most > 8.f || k == line.from || (k >= P && seen != all))) {
+                if (any_of_group(bar, most > 8.f || k == from || (k >= P && seen != all))) {
                     // references go up to the maxima (a row's first one: to its maximum, whatever it is)
                     int own = 0;
                     #pragma unroll
@@ -461,28 +491,35 @@ __global__ void __launch_bounds__(kTileThreads, 1) msa_attention_kvq_tiles_kerne
                         d[i] -= __shfl_sync(0xffffffffu, by, i);
                         l[i] *= __shfl_sync(0xffffffffu, f, i);
                     }
-                    if (k > line.from) {             // and O with them: the products so far are complete, this tile's waits for our weights
+                    if (k > from) {             // and O with them: the products so far are complete, this tile's waits for our weights
                         wait(c.pv_done[(tau - 1) & 1], ((tau - 1) >> 1) & 1);
                         tc_fence_after();
-                        tmem_load<C>(tmem + G::kTmemO + group * C + lanes, raw);
-                        tmem_wait_ld();
                         #pragma unroll
-                        for (int i = 0; i < C; ++i) raw[i] = __float_as_uint(__uint_as_float(raw[i]) * __shfl_sync(0xffffffffu, f, i));
-                        tmem_store<C, 0>(tmem + G::kTmemO + group * C + lanes, raw);
+                        for (int i = 0; i < C; i += 8) {
+                            uint32_t o[8];
+                            tmem_load<8>(tmem + G::kTmemO + group * C + i + lanes, o);
+                            tmem_wait_ld();
+                            #pragma unroll
+                            for (int q = 0; q < 8; ++q) o[q] = __float_as_uint(__uint_as_float(o[q]) * __shfl_sync(0xffffffffu, f, i + q));
+                            tmem_store<8, 0>(tmem + G::kTmemO + group * C + i + lanes, o);
+                        }
                         tmem_wait_st();
                         tc_fence_before();
                     }
                     named_barrier(bar, 128);
                 }
                 if (tau >= 2) wait(c.pv_done[tau & 1], ((tau - 2) >> 1) & 1);
+                const unsigned long long sv2 = pack_f32x2(sv, sv);
                 #pragma unroll
                 for (int i = 0; i < C; i += 8) {
                     uint32_t y[4];
                     #pragma unroll
                     for (int q = 0; q < 4; ++q) {
-                        const float u = exp2_approx(d[i + 2 * q]), v = exp2_approx(d[i + 2 * q + 1]);
-                        l[i + 2 * q] += u, l[i + 2 * q + 1] += v;
-                        y[q] = pack2_bf16(u * sv, v * sv);
+                        const unsigned long long e = pack_f32x2(exp2_approx(d[i + 2 * q]), exp2_approx(d[i + 2 * q + 1]));
+                        unpack_f32x2(add_f32x2(pack_f32x2(l[i + 2 * q], l[i + 2 * q + 1]), e), l[i + 2 * q], l[i + 2 * q + 1]);
+                        float u, v;
+                        unpack_f32x2(fma_f32x2(e, sv2, 0ull), u, v);
+                        y[q] = pack2_bf16(u, v);
                     }
                     st_shared_v4(smem + G::oP + (tau & 1) * G::kP + key * 128 + (((group * (C / 8) + (i >> 3)) ^ (key & 7)) << 4), y[0], y[1], y[2], y[3]);
                 }
@@ -492,8 +529,6 @@ __global__ void __launch_bounds__(kTileThreads, 1) msa_attention_kvq_tiles_kerne
             // ---- the unit's end: sums over the keys, O
             wait(c.pv_done[(tau - 1) & 1], ((tau - 1) >> 1) & 1);
             tc_fence_after();
-            uint32_t raw[C];
-            tmem_load<C>(tmem + G::kTmemO + group * C + lanes, raw);
             #pragma unroll
             for (int w = 16; w >= C; w >>= 1) {      // (fewer rows than lanes: whole sums first)
                 #pragma unroll
@@ -509,6 +544,8 @@ __global__ void __launch_bounds__(kTileThreads, 1) msa_attention_kvq_tiles_kerne
                 }
             }
             c.sums[group][quad][lane] = l[0];
+            uint32_t raw[C];
+            tmem_load<C>(tmem + G::kTmemO + group * C + lanes, raw);
             named_barrier(bar, 128);
             const int at = lane & (C - 1);
             const float sum = (c.sums[group][0][at] + c.sums[group][1][at]) + (c.sums[group][2][at] + c.sums[group][3][at]);
@@ -578,32 +615,36 @@ __global__ void __launch_bounds__(kTileThreads, 1) msa_attention_kvq_tiles_kerne
     } else {
         // ---- MMAs ---------------------------------------------------------------------------
         uint32_t unit = 0;
-        while (line.next(a)) {
+        const uint32_t base = uniform(smem);
+        const uint64_t dq = desc_k_major(base + G::oQ), dp = desc_mn_major(base + G::oP, 0);
+        const Line<N, kTileOfKeys, 0>& line = walks[4].line;
+        while (next_unit(walks[4], lane == 0, 0, 32)) {
+            const uint32_t tiles = uniform(static_cast<uint32_t>(line.to - line.from));
             const auto product = [&](uint32_t t, bool first) {       // O^T (+)= V^T P^T of tile t
                 if (first && unit > 0) wait(c.o_free, (unit - 1) & 1);
                 wait(c.v_full[t & 1], (t >> 1) & 1);
                 wait(c.p_full[t & 1], (t >> 1) & 1);
                 tc_fence_after();
-                const uint64_t b = desc_mn_major(uniform(smem + G::oP + (t & 1) * G::kP), 0);
+                const uint64_t b = dp + (t & 1) * (G::kP >> 4);
                 const uint32_t va = tmem + G::kTmemV + (t & 1) * 64;
-                #pragma unroll
-                for (int i = 0; i < kTileOfKeys / 16; ++i) tile_mma(tmem + G::kTmemO, va + 8 * i, b + 128 * i, G::kIdescPV, first && i == 0 ? 0u : 1u);
+                tc_mma_ts_steps(tmem + G::kTmemO, va, b, G::kIdescPV, first ? 0u : 1u);
+                tc_mma_ts_steps(tmem + G::kTmemO, va + 32, b + 4 * 128, G::kIdescPV, 1u);
                 tc_commit_e(smem_u32(&c.pv_done[t & 1]));
             };
             #pragma unroll 1
-            for (int k = line.from; k < line.to; ++k, ++tau) {
+            for (uint32_t i = 0; i < tiles; ++i, ++tau) {
                 wait(c.k_full[tau & 1], (tau >> 1) & 1);
                 if (tau >= 2) wait(c.s_free[tau & 1], ((tau - 2) >> 1) & 1);
                 tc_fence_after();
                 const uint32_t ka = tmem + G::kTmemK + (tau & 1) * 64, sd = tmem + G::kTmemS + (tau & 1) * N;
-                #pragma unroll
-                for (int i = 0; i < D / 16; ++i)
-                    tile_mma(sd, ka + 8 * i, desc_k_major(uniform(smem + G::oQ + (i >> 2) * G::kBox)) + 2 * (i & 3), G::kIdescS, i == 0 ? 0u : 1u);
+                tile_mma<4>(sd, ka, dq, G::kIdescS, 0u);
+                if constexpr (D == 128) tile_mma<4>(sd, ka + 32, dq + (G::kBox >> 4), G::kIdescS, 1u);
+                if constexpr (D == 80) tile_mma<1>(sd, ka + 32, dq + (G::kBox >> 4), G::kIdescS, 1u);
                 tc_commit_e(smem_u32(&c.s_full[tau & 1]));
                 if (lane == 0) mbar_arrive(smem_u32(&c.s_full[tau & 1]));            // (passes on what the K warps have written: the keys' scales)
-                if (k > line.from) product(tau - 1, k - 1 == line.from);
+                if (i > 0) product(tau - 1, i == 1);
             }
-            product(tau - 1, line.to - 1 == line.from);
+            product(tau - 1, tiles == 1);
             ++unit;
         }
         tc_commit_e(smem_u32(&c.drain));
