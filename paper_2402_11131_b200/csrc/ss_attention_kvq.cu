@@ -88,10 +88,10 @@ __device__ __forceinline__ Shape shape_of(const KvqArgs& a, long long chunks, lo
     return s;
 }
 
+// Sum over a warp of numbers from 0 to 2^42
 __device__ __forceinline__ long long warp_sum(long long x) {
-    #pragma unroll 1
-    for (int i = 16; i > 0; i >>= 1) x += __shfl_xor_sync(0xffffffffu, x, i);
-    return x;
+    const uint32_t lo = __reduce_add_sync(0xffffffffu, static_cast<uint32_t>(x) & 0xffffu), hi = __reduce_add_sync(0xffffffffu, static_cast<uint32_t>(x >> 16));
+    return (static_cast<long long>(hi) << 16) + lo;
 }
 __device__ __forceinline__ long long divide(long long a, long long b) {
     return (a >> 32) == 0 && (b >> 32) == 0 ? static_cast<long long>(static_cast<uint32_t>(a) / static_cast<uint32_t>(b)) : a / b;
@@ -261,7 +261,12 @@ struct Line {
             }
             base += __shfl_sync(0xffffffffu, upto, 31);
         }
-        s = load_seq<ROWS, CHUNK>(a, b);
+        if (b < 32) {                                // (a lane has it)
+            s.L = __shfl_sync(0xffffffffu, mine.L, b), s.T = __shfl_sync(0xffffffffu, mine.T, b), s.rows = __shfl_sync(0xffffffffu, mine.rows, b);
+            s.blocks = __shfl_sync(0xffffffffu, mine.blocks, b), s.chunks = __shfl_sync(0xffffffffu, mine.chunks, b), s.start = __shfl_sync(0xffffffffu, mine.start, b);
+        } else {
+            s = load_seq<ROWS, CHUNK>(a, b);
+        }
         steps = steps_of(s), units = s.blocks * groups;
         unit = static_cast<int>(divide(pos - base, steps));
         return true;
@@ -292,7 +297,9 @@ struct Pieces {
     template <typename L>
     __device__ __forceinline__ explicit Pieces(const L& line) : first(line.me), last(line.me) {
         long long at = line.unit0;
-        if (!line.whole()) {
+        if (line.pieces > 0) {
+            first -= first % line.pieces, last = first + line.pieces - 1;
+        } else if (!line.whole()) {
             #pragma unroll 1
             for (at = line.cut(first); at > line.unit0; at = line.cut(--first)) {}
             #pragma unroll 1
@@ -304,18 +311,26 @@ struct Pieces {
     __device__ __forceinline__ long long place(const L& line, int i) const { return 2ll * ((i << line.team_log2) + line.member) + (i == first ? second : 0); }
 };
 
-// Eight values of a row's output, and its log-sum-exp: o / l
-template <int D, typename L>
-__device__ __forceinline__ void store_row(const KvqArgs& a, const L& line, int r, int d0, const float (&o)[8], float m, float l, int h) {
-    const Row x = row_of(line.row0 + r, line.s.T, a.gamma);
-    const long long off = row_offset(a, D, line.b, h, x);
+// Eight values, from d0 on, of the output of a row that lies at element `off`, and its log-sum-exp: o / l
+template <int D>
+__device__ __forceinline__ void store_row(const KvqArgs& a, bool main, long long off, int d0, const float (&o)[8], float m, float l) {
     const float f = 1.f / l;
     uint4 v;
     v.x = pack2_bf16(o[0] * f, o[1] * f), v.y = pack2_bf16(o[2] * f, o[3] * f);
     v.z = pack2_bf16(o[4] * f, o[5] * f), v.w = pack2_bf16(o[6] * f, o[7] * f);
-    *reinterpret_cast<uint4*>((x.j < 0 ? a.o_main : a.o_spec) + off + d0) = v;
-    float* lse = x.j < 0 ? a.lse_main : a.lse_spec;
+    *reinterpret_cast<uint4*>((main ? a.o_main : a.o_spec) + off + d0) = v;
+    float* lse = main ? a.lse_main : a.lse_spec;
     if (d0 == 0 && lse != nullptr) lse[off / D] = (m + log2f(l)) * 0.6931471805599453f;
+}
+
+// One more piece of a unit is in the workspace: true for the last of `n`, who joins them and leaves the counter at zero.  Called by one
+// thread behind a barrier of those that wrote: the operation releases their partial rows and acquires the others'.
+__device__ __forceinline__ bool last_piece(int* counter, int n) {
+    int before;
+    asm volatile("atom.add.acq_rel.gpu.global.s32 %0, [%1], 1;" : "=r"(before) : "l"(counter) : "memory");
+    if (before != n - 1) return false;
+    *counter = 0;
+    return true;
 }
 
 // One more partial row into (o, m, l)
@@ -943,7 +958,7 @@ __global__ void __launch_bounds__(kThreads, NG == 1 ? 3 : 2) msa_attention_kvq_r
                 join_row(o, m, l, stats[i * ROWS + r], *reinterpret_cast<const float4*>(src), *reinterpret_cast<const float4*>(src + 4));
             }
             if (whole) {
-                store_row<D>(a, line, r, d0, o, m, l, h0 + hd);
+                store_row<D>(a, row0 + r < s.T, row_offset(a, D, b, h0 + hd, row_of(row0 + r, s.T, a.gamma)), d0, o, m, l);
             } else {
                 float* dst = place(line.me) + hr * (D + 4) + d0;
                 __stcg(reinterpret_cast<float4*>(dst), make_float4(o[0], o[1], o[2], o[3]));
@@ -952,13 +967,9 @@ __global__ void __launch_bounds__(kThreads, NG == 1 ? 3 : 2) msa_attention_kvq_r
             }
         }
         if (!whole) {
-            __threadfence();
             __syncthreads();
             if (tid == 0) {
-                int* const counter = counters + (share.first << line.team_log2) + line.member;
-                joined = atomicAdd(counter, 1) == share.last - share.first;
-                if (joined) *counter = 0;
-                __threadfence();
+                joined = last_piece(counters + (share.first << line.team_log2) + line.member, share.last - share.first + 1);
             }
             __syncthreads();
             if (joined) {
@@ -980,7 +991,7 @@ __global__ void __launch_bounds__(kThreads, NG == 1 ? 3 : 2) msa_attention_kvq_r
                         for (int k = 0; k < 4; ++k)
                             if (i + k <= share.last) join_row(o, m, l, st[k], u[k], v[k]);
                     }
-                    store_row<D>(a, line, r, d0, o, m, l, h0 + hd);
+                    store_row<D>(a, row0 + r < s.T, row_offset(a, D, b, h0 + hd, row_of(row0 + r, s.T, a.gamma)), d0, o, m, l);
                 }
             }
         }

@@ -27,14 +27,14 @@ struct TileGeo {
     static constexpr int kColumns = D / 2;                        // TMEM columns of a K tile
     static constexpr int kQuads = (D + 31) / 32;                  // warps that have V lanes
     static constexpr int kCodes = kTileOfKeys * kPitch;
-    static constexpr int kStages = 4, kParams = 8;
+    static constexpr int kStages = 3, kParams = 8;
     static constexpr int kBoxes = D > 64 ? 2 : 1, kBox = N * 128;
     static constexpr int kRowOfV = 64 * kQuads;                   // bytes of a bf16 row in lane order
     static constexpr int kP = kTileOfKeys * 128;
     static constexpr int oP = 0, oQ = oP + 2 * kP, oK = oQ + kBoxes * kBox, oV = oK + kStages * kCodes;
     static constexpr int oKParams = oV + kStages * kCodes, oVParams = oKParams + kParams * kTileOfKeys * 8;
     static constexpr int kBytes = oVParams + kStages * kTileOfKeys * 4;
-    static_assert(kTileOfKeys * kRowOfV <= kStages * kCodes, "bf16 values take the place of the ring");
+    static_assert(64 * kRowOfV <= kStages * kCodes, "half a tile of bf16 values takes the place of the ring");
     static constexpr uint32_t kTmemK = 0, kTmemV = 128, kTmemS = 256, kTmemO = 256 + 2 * N;
     static constexpr uint32_t kIdesc = (1u << 4) | (1u << 7) | (1u << 10) | (static_cast<uint32_t>(N >> 3) << 17) | ((128u >> 4) << 24);
     static constexpr uint32_t kIdescS = kIdesc, kIdescPV = kIdesc | (1u << 16);
@@ -50,9 +50,8 @@ struct TileWalk {
 
 struct TileCtrl {
     unsigned long long k_full[2], s_full[2], s_free[2], v_full[2], p_full[2], pv_done[2], o_free, drain;
-    unsigned long long see[64];                                   // per row: ancestors; stream keys it sees; where its output goes
-    long long out[64];                                            // element offset, -1: no row
-    int2 streams[64];
+    uint32_t see[2][64];                                          // per group and node: the rows that see it
+    long long out[64];                                            // where a row's output goes (element offset)
     float neg_ref[64];
     int tile_max[2][4][32];
     float sums[2][4][32];
@@ -151,16 +150,6 @@ __global__ void __launch_bounds__(kTileThreads, 1) msa_attention_kvq_tiles_kerne
     const int tid = threadIdx.x, lane = tid & 31, warp = static_cast<int>(uniform(tid >> 5)), quad = warp & 3;
     const uint32_t smem = smem_u32(smem_raw);
     int* const status = reinterpret_cast<int*>(a.ws);
-    wait_for_previous_kernel();
-    release_next_kernel();
-    if (warp < 5) {
-        Line<N, kTileOfKeys, 0> line;
-        const bool any = line.begin(a, lane);
-        if (lane == 0) walks[warp].line = line, walks[warp].more = any;
-    }
-    __syncthreads();
-    if (walks[0].more == 0) return;
-
     if (tid == 0) {
         c.abort = 0;
         for (int i = 0; i < 2; ++i) {
@@ -171,6 +160,15 @@ __global__ void __launch_bounds__(kTileThreads, 1) msa_attention_kvq_tiles_kerne
         mbar_init(smem_u32(&c.o_free), 256), mbar_init(smem_u32(&c.drain), 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
+    wait_for_previous_kernel();
+    release_next_kernel();
+    if (warp < 5) {
+        Line<N, kTileOfKeys, 0> line;
+        const bool any = line.begin(a, lane);
+        if (lane == 0) walks[warp].line = line, walks[warp].more = any;
+    }
+    __syncthreads();
+    if (walks[0].more == 0) return;
     if (warp == 16) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&c.tmem)) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
@@ -221,16 +219,24 @@ __global__ void __launch_bounds__(kTileThreads, 1) msa_attention_kvq_tiles_kerne
             };
             #pragma unroll 1
             for (int i = 0; i < G::kStages - 1; ++i) load(from + i);
-            // query rows, 16 bytes at a time, swizzled
-            #pragma unroll 1
-            for (int item = tid; item < N * (D / 8); item += 128) {
-                const int r = item / (D / 8), at = item - r * (D / 8);
-                uint4 v = {};
-                if (real && line.row0 + r < s.rows) {
-                    const Row x = row_of(line.row0 + r, s.T, a.gamma);
-                    v = *reinterpret_cast<const uint4*>((x.j < 0 ? a.q_main : a.q_spec) + row_offset(a, D, line.b, h, x) + 8 * at);
+            // query rows, 16 bytes at a time (all of a thread's on their way at once), swizzled
+            {
+                constexpr int kItems = N * (D / 8) / 128;
+                uint4 v[kItems];
+                #pragma unroll
+                for (int i = 0; i < kItems; ++i) {
+                    const int item = i * 128 + tid, r = item / (D / 8), at = item - r * (D / 8);
+                    v[i] = make_uint4(0u, 0u, 0u, 0u);
+                    if (real && line.row0 + r < s.rows) {
+                        const Row x = row_of(line.row0 + r, s.T, a.gamma);
+                        v[i] = *reinterpret_cast<const uint4*>((x.j < 0 ? a.q_main : a.q_spec) + row_offset(a, D, line.b, h, x) + 8 * at);
+                    }
                 }
-                st_shared_v4(smem + G::oQ + (at >> 3) * G::kBox + r * 128 + (((at & 7) ^ (r & 7)) << 4), v.x, v.y, v.z, v.w);
+                #pragma unroll
+                for (int i = 0; i < kItems; ++i) {
+                    const int item = i * 128 + tid, r = item / (D / 8), at = item - r * (D / 8);
+                    st_shared_v4(smem + G::oQ + (at >> 3) * G::kBox + r * 128 + (((at & 7) ^ (r & 7)) << 4), v[i].x, v[i].y, v[i].z, v[i].w);
+                }
             }
             fence_async_smem();
             const Extra x = extra_of(a, s, line.row0, N);
@@ -353,39 +359,47 @@ __global__ void __launch_bounds__(kTileThreads, 1) msa_attention_kvq_tiles_kerne
                         }
                     }
                 } else {
-                    // bf16 rows in the order of the lanes: of 8 values the low codes' would be 0, 4, 1, 5, the high codes' 2, 6, 3, 7
-                    const int e = (k - P) * kTileOfKeys + t;
-                    const __nv_bfloat16* src = nullptr;
-                    if (real && e < x.count) src = (e < x.T ? a.v_tree : a.v_spec) + extra_offset(a, x, D, line.b, h, e);
-                    named_barrier(2, 128);
-                    const uint32_t row = smem + G::oV + t * G::kRowOfV;
-                    #pragma unroll
-                    for (int i = 0; i < 4 * G::kQuads; ++i) {
-                        uint4 v = {};
-                        if (src && i < G::kWords) v = *reinterpret_cast<const uint4*>(src + 8 * i);
-                        // bytes: 64 to a quad, low ones first, 8 to a word; 16-byte places swizzled by the key
-                        const int at = 64 * (i >> 2) + 8 * (i & 3);
-                        const uint32_t lo = row + (((at >> 4) ^ (t & 3)) << 4) + (at & 15), hi = row + ((((at + 32) >> 4) ^ (t & 3)) << 4) + (at & 15);
-                        st_shared_v2(lo, __byte_perm(v.x, v.z, 0x5410), __byte_perm(v.x, v.z, 0x7632));
-                        st_shared_v2(hi, __byte_perm(v.y, v.w, 0x5410), __byte_perm(v.y, v.w, 0x7632));
-                    }
-                    named_barrier(2, 128);
+                    // bf16 rows in the order of the lanes: of 8 values the low codes' would be 0, 4, 1, 5, the high codes' 2, 6, 3, 7.  64 keys at
+                    // a time, in the ring's place; a row's words are shared by two threads.
                     if (tau >= 2) wait(c.pv_done[tau & 1], ((tau - 2) >> 1) & 1);
                     tc_fence_after();
-                    if (mine) {
-                        #pragma unroll 1
-                        for (int part = 0; part < 4; ++part) {       // low and high lanes of 64 keys each
-                            const int half = part >> 1, high = part & 1;
-                            uint32_t r[16];
+                    #pragma unroll 1
+                    for (int half = 0; half < 2; ++half) {
+                        const int r = t >> 1, e = (k - P) * kTileOfKeys + 64 * half + r;
+                        const __nv_bfloat16* src = nullptr;
+                        if (real && e < x.count) src = (e < x.T ? a.v_tree : a.v_spec) + extra_offset(a, x, D, line.b, h, e);
+                        uint4 v[2 * G::kQuads];
+                        #pragma unroll
+                        for (int i = 0; i < 2 * G::kQuads; ++i) {
+                            const int word = 2 * i + (t & 1);
+                            v[i] = make_uint4(0u, 0u, 0u, 0u);
+                            if (src && word < G::kWords) v[i] = *reinterpret_cast<const uint4*>(src + 8 * word);
+                        }
+                        named_barrier(2, 128);       // (what lay there has been read)
+                        const uint32_t row = smem + G::oV + r * G::kRowOfV;
+                        #pragma unroll
+                        for (int i = 0; i < 2 * G::kQuads; ++i) {
+                            // bytes: 64 to a quad, low ones first, 8 to a word; 16-byte places swizzled by the key
+                            const int word = 2 * i + (t & 1), at = 64 * (word >> 2) + 8 * (word & 3);
+                            const uint32_t lo = row + (((at >> 4) ^ (r & 3)) << 4) + (at & 15), hi = row + ((((at + 32) >> 4) ^ (r & 3)) << 4) + (at & 15);
+                            st_shared_v2(lo, __byte_perm(v[i].x, v[i].z, 0x5410), __byte_perm(v[i].x, v[i].z, 0x7632));
+                            st_shared_v2(hi, __byte_perm(v[i].y, v[i].w, 0x5410), __byte_perm(v[i].y, v[i].w, 0x7632));
+                        }
+                        named_barrier(2, 128);
+                        if (mine) {
                             #pragma unroll
-                            for (int i = 0; i < 4; ++i) {
-                                const int kk = 64 * half + 16 * i + 8 * (lane >> 4) + (lane & 7);          // matrices: dims 0..7, 8..15 of 8 keys, then of 8 more
-                                const int at = 64 * quad + 32 * high + 16 * ((lane >> 3) & 1);
-                                uint32_t q[4];
-                                load_transposed_halves(smem + G::oV + kk * G::kRowOfV + (((at >> 4) ^ (kk & 3)) << 4), q);
-                                r[4 * i] = q[0], r[4 * i + 1] = q[1], r[4 * i + 2] = q[2], r[4 * i + 3] = q[3];
+                            for (int high = 0; high < 2; ++high) {
+                                uint32_t q16[16];
+                                #pragma unroll
+                                for (int i = 0; i < 4; ++i) {
+                                    const int kk = 16 * i + 8 * (lane >> 4) + (lane & 7);          // matrices: dims 0..7, 8..15 of 8 keys, then of 8 more
+                                    const int at = 64 * quad + 32 * high + 16 * ((lane >> 3) & 1);
+                                    uint32_t q[4];
+                                    load_transposed_halves(smem + G::oV + kk * G::kRowOfV + (((at >> 4) ^ (kk & 3)) << 4), q);
+                                    q16[4 * i] = q[0], q16[4 * i + 1] = q[1], q16[4 * i + 2] = q[2], q16[4 * i + 3] = q[3];
+                                }
+                                tmem_store_lanes16(dst + 32 * half + (high ? 16u << 16 : 0u), q16);
                             }
-                            tmem_store_lanes16(dst + 32 * half + (high ? 16u << 16 : 0u), r);
                         }
                     }
                 }
@@ -410,19 +424,23 @@ __global__ void __launch_bounds__(kTileThreads, 1) msa_attention_kvq_tiles_kerne
             const Seq& s = line.s;
             const int L = s.L, P = prefix_chunks<kTileOfKeys>(L), from = line.from, to = line.to;
             const Extra x = extra_of(a, s, line.row0, N);
-            if (key < C) {
-                const int n = group * C + key, r = line.row0 + n;
+            {
+                const int n = group * C + lane, r = line.row0 + n;
                 unsigned long long see = 0;
-                long long out = -1;
-                int2 st = make_int2(0, 0);
-                if (r < s.rows && line.head0 < a.n_heads) {
+                long long out = 0;
+                if (lane < C && r < s.rows && line.head0 < a.n_heads) {
                     const Row q = row_of(r, s.T, a.gamma);
                     see = a.trees[line.b].anc_mask[q.t];
-                    const int first = s.T + (q.t - x.t0) * x.gamma;
-                    st = make_int2(first, q.j < 0 ? first : first + q.j + 1);
                     out = row_offset(a, D, line.b, line.head0, q);
                 }
-                c.see[n] = see, c.streams[n] = st, c.out[n] = out, c.neg_ref[n] = 0.f;
+                uint32_t own = 0u;
+                #pragma unroll
+                for (int i = 0; i < 16; ++i) {       // nodes 16 quad ..
+                    const uint32_t rows = __ballot_sync(0xffffffffu, see >> (16 * quad + i) & 1ull);
+                    if (lane == i) own = rows;
+                }
+                if (lane < 16) c.see[group][16 * quad + lane] = own;
+                if (quad == 0 && lane < C) c.out[n] = out, c.neg_ref[n] = 0.f;
             }
             named_barrier(bar, 128);
             float l[C];
@@ -455,13 +473,18 @@ __global__ void __launch_bounds__(kTileThreads, 1) msa_attention_kvq_tiles_kerne
                         for (int i = 0; i < C; ++i) d[i] = -INFINITY;
                     }
                 } else {
+                    // rows that see the key: those of its node's descendants; of a stream key, from its own row to its node's last
                     const int e = (k - P) * kTileOfKeys + key;
-                    #pragma unroll
-                    for (int i = 0; i < C; ++i) {
-                        const int2 st = c.streams[group * C + i];
-                        const bool ok = e < x.T ? (c.see[group * C + i] >> e & 1ull) : (e >= st.x && e < st.y);
-                        if (!ok) d[i] = -INFINITY;
+                    uint32_t vis = 0u;
+                    if (e < x.T) {
+                        vis = c.see[group][e];
+                    } else if (e < x.count) {
+                        const int own = e - x.T + x.t0 * x.gamma, first = x.T + own - x.row0 - group * C, last = first + x.gamma - 1 - own % x.gamma;
+                        if (first < C && last >= 0) vis = (0xffffffffu >> (31 - min(last, 31))) & (0xffffffffu << max(first, 0));
                     }
+                    #pragma unroll
+                    for (int i = 0; i < C; ++i)
+                        if (!(vis >> i & 1u)) d[i] = -INFINITY;
                 }
                 float most = d[0];
                 #pragma unroll
@@ -508,7 +531,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) msa_attention_kvq_tiles_kerne
                     }
                     named_barrier(bar, 128);
                 }
-                if (tau >= 2) wait(c.pv_done[tau & 1], ((tau - 2) >> 1) & 1);
+                // (this tile's S was committed behind the product of two tiles ago: its weights' place is free)
                 const unsigned long long sv2 = pack_f32x2(sv, sv);
                 #pragma unroll
                 for (int i = 0; i < C; i += 8) {
@@ -578,36 +601,39 @@ __global__ void __launch_bounds__(kTileThreads, 1) msa_attention_kvq_tiles_kerne
                 #pragma unroll
                 for (int i = 0; i < C; ++i)
                     if (group * C + i < rows && dim < D) __stcg(mine + (group * C + i) * (D + 4) + dim, __uint_as_float(raw[i]));
-                __threadfence();
                 named_barrier(5, 256);
                 if (tid == 256) {
-                    int* const counter = counters + (share.first << line.team_log2) + line.member;
-                    c.joined = atomicAdd(counter, 1) == share.last - share.first;
-                    if (c.joined) *counter = 0;
-                    __threadfence();
+                    c.joined = last_piece(counters + (share.first << line.team_log2) + line.member, share.last - share.first + 1);
                 }
                 named_barrier(5, 256);
                 if (c.joined) {
+                    // 8 values of a row at a time, up to four partial rows on their way
+                    const float* const p0 = partial + share.place(line, share.first) * kPartial;
+                    const long long on = (2ll << line.team_log2) * kPartial;                 // between teams' places
+                    const int n = share.last - share.first + 1, items = rows * (D / 8);
+                    const float* const p1 = partial + share.place(line, share.first + 1) * kPartial;
                     #pragma unroll 1
-                    for (int item = tid - 256; item < rows * (D / 8); item += 256) {
+                    for (int item = tid - 256; item < items; item += 256) {
                         const int r = item / (D / 8), d0 = (item - r * (D / 8)) * 8;
                         float m = kNoRef, sm = 0.f, o[8] = {};
                         #pragma unroll 1
-                        for (int i = share.first; i <= share.last; i += 2) {
-                            float2 st[2];
-                            float4 u[2], v[2];
+                        for (int i = 0; i < n; i += 4) {
+                            float2 st[4];
+                            float4 u[4], v[4];
                             #pragma unroll
-                            for (int q = 0; q < 2; ++q) {
-                                const float* src = partial + share.place(line, min(i + q, share.last)) * kPartial + r * (D + 4);
+                            for (int q = 0; q < 4; ++q) {
+                                const int k = min(i + q, n - 1);
+                                const float* src = (k == 0 ? p0 : p1 + (k - 1) * on) + r * (D + 4);
                                 st[q] = __ldcg(reinterpret_cast<const float2*>(src + D));
                                 u[q] = __ldcg(reinterpret_cast<const float4*>(src + d0)), v[q] = __ldcg(reinterpret_cast<const float4*>(src + d0) + 1);
                             }
                             #pragma unroll
-                            for (int q = 0; q < 2; ++q)
-                                if (i + q <= share.last) join_row(o, m, sm, st[q], u[q], v[q]);
+                            for (int q = 0; q < 4; ++q)
+                                if (i + q < n) join_row(o, m, sm, st[q], u[q], v[q]);
                         }
-                        if (ok) store_row<D>(a, line, r, d0, o, m, sm, line.head0);
+                        if (ok) store_row<D>(a, line.row0 + r < s.T, c.out[r], d0, o, m, sm);
                     }
+                    named_barrier(5, 256);           // (both groups read all rows' places)
                 }
             }
             ++unit;
