@@ -8,7 +8,7 @@
 // Lane 32 w + x of V^T and O^T (w < D / 32) holds, for x < 16, the low codes of byte 16 w + x of a row, else the high codes of
 // byte 16 w + x - 16.
 //
-// Seventeen warps: 0..3 K, 4..7 V, 8..15 softmax (two groups of four, each half of the rows, thread = key), 16 issues the MMAs.  Two
+// 25 warps: 0..3 K, 4..7 V, 8..23 softmax (four groups of four, each a quarter of the rows, thread = key), 24 issues the MMAs.  Two
 // buffers each for K, V, S and P, so that the five work on different tiles.  Nothing but the order of tiles is shared: every role
 // walks the same list of units.
 #pragma once
@@ -16,11 +16,11 @@
 
 namespace ss {
 
-constexpr int kTileOfKeys = 128, kTileThreads = 544;
+constexpr int kTileOfKeys = 128, kTileGroups = 4, kTileSoftmax = 128 * kTileGroups, kTileThreads = 256 + kTileSoftmax + 32;
 
 template <int D, int N>
 struct TileGeo {
-    static constexpr int kHalf = N / 2;                           // rows of a softmax group
+    static constexpr int kRowsOfGroup = N / kTileGroups;          // rows of a softmax group
     static constexpr int kPitch = D == 128 ? 64 : D == 80 ? 48 : 32;         // bytes of a key's codes in shared memory (16-byte aligned)
     static constexpr int kCopy = D == 80 ? 8 : 16, kPer = D / 2 / kCopy;     // asynchronous copies per key
     static constexpr int kWords = D / 8;
@@ -48,13 +48,49 @@ struct TileWalk {
     int more;
 };
 
+// Asynchronous copies of a tile's codes by 128 threads, 16 (8) bytes each, from a pointer that walks along with the tiles.  Slots behind
+// the last one are read as the last one again (their weights are zero).
+template <int D, int N>
+struct TileLoader {
+    using G = TileGeo<D, N>;
+    static constexpr bool kEven = 128 % G::kPer == 0;
+    const unsigned char* at;                         // of the next tile: the thread's first copy (80: key 0)
+    int left;                                        // slots from there on
+    __device__ __forceinline__ TileLoader(const KvqArgs& a, const Seq& s, int h, int tile, int t, const unsigned char* codes) {
+        const long long slot = s.start + static_cast<long long>(tile) * kTileOfKeys + (kEven ? t / G::kPer : 0);
+        at = codes + slot * a.slot_stride + h * a.head_stride + (kEven ? t % G::kPer * G::kCopy : 0);
+        left = s.L - tile * kTileOfKeys;
+    }
+    __device__ __forceinline__ uint32_t place(int row, int column) const {
+        return row * G::kPitch + (D == 128 ? column ^ ((row >> 1) & 3) : D == 64 ? column ^ ((row >> 2) & 1) : column) * G::kCopy;
+    }
+    __device__ __forceinline__ void next(const KvqArgs& a, uint32_t stage, int t) {
+        if (kEven && left >= kTileOfKeys) {
+            // (the swizzle is the same for all of the thread's rows: they are a multiple of 8 apart)
+            const uint32_t dst = stage + place(t / G::kPer, t % G::kPer);
+            #pragma unroll
+            for (int i = 0; i < G::kPer; ++i)
+                copy_async<G::kCopy>(dst + i * (128 / G::kPer) * G::kPitch, at + i * (128 / G::kPer) * a.slot_stride);
+        } else {
+            const int last = left - 1;
+            #pragma unroll 1
+            for (int i = 0; i < G::kPer; ++i) {
+                const int item = i * 128 + t, row = item / G::kPer, column = item - row * G::kPer;
+                copy_async<G::kCopy>(stage + place(row, column), at + (kEven ? (min(row, last) - t / G::kPer) * a.slot_stride : min(row, last) * a.slot_stride + column * G::kCopy));
+            }
+        }
+        at += kTileOfKeys * a.slot_stride;
+        left -= kTileOfKeys;
+    }
+};
+
 struct TileCtrl {
     unsigned long long k_full[2], s_full[2], s_free[2], v_full[2], p_full[2], pv_done[2], o_free, drain;
-    uint32_t see[2][64];                                          // per group and node: the rows that see it
+    uint32_t see[kTileGroups][64];                                          // per group and node: the rows that see it
     long long out[64];                                            // where a row's output goes (element offset)
     float neg_ref[64];
-    int tile_max[2][4][32];
-    float sums[2][4][32];
+    int tile_max[kTileGroups][4][16];
+    float sums[kTileGroups][4][16];
     uint32_t tmem;
     int abort, joined;
 };
@@ -143,10 +179,10 @@ __device__ __forceinline__ Extra extra_of(const KvqArgs& a, const Seq& s, int ro
 template <int D, int N>
 __global__ void __launch_bounds__(kTileThreads, 1) msa_attention_kvq_tiles_kernel(const __grid_constant__ KvqArgs a) {
     using G = TileGeo<D, N>;
-    constexpr int C = G::kHalf;
+    constexpr int C = G::kRowsOfGroup;
     extern __shared__ __align__(1024) unsigned char smem_raw[];
     __shared__ __align__(16) TileCtrl c;
-    __shared__ __align__(16) TileWalk<N> walks[5];    // K, V, two softmax groups, MMAs
+    __shared__ __align__(16) TileWalk<N> walks[3 + kTileGroups];    // K, V, softmax groups, MMAs
     const int tid = threadIdx.x, lane = tid & 31, warp = static_cast<int>(uniform(tid >> 5)), quad = warp & 3;
     const uint32_t smem = smem_u32(smem_raw);
     int* const status = reinterpret_cast<int*>(a.ws);
@@ -154,22 +190,23 @@ __global__ void __launch_bounds__(kTileThreads, 1) msa_attention_kvq_tiles_kerne
         c.abort = 0;
         for (int i = 0; i < 2; ++i) {
             mbar_init(smem_u32(&c.k_full[i]), 128), mbar_init(smem_u32(&c.v_full[i]), 128);
-            mbar_init(smem_u32(&c.s_free[i]), 256), mbar_init(smem_u32(&c.p_full[i]), 256);
+            mbar_init(smem_u32(&c.s_free[i]), kTileSoftmax), mbar_init(smem_u32(&c.p_full[i]), kTileSoftmax);
             mbar_init(smem_u32(&c.s_full[i]), 2), mbar_init(smem_u32(&c.pv_done[i]), 1);
         }
-        mbar_init(smem_u32(&c.o_free), 256), mbar_init(smem_u32(&c.drain), 1);
+        mbar_init(smem_u32(&c.o_free), kTileSoftmax), mbar_init(smem_u32(&c.drain), 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     wait_for_previous_kernel();
     release_next_kernel();
-    if (warp < 5) {
+    if (warp < 3 + kTileGroups) {
         Line<N, kTileOfKeys, 0> line;
         const bool any = line.begin(a, lane);
         if (lane == 0) walks[warp].line = line, walks[warp].more = any;
     }
     __syncthreads();
     if (walks[0].more == 0) return;
-    if (warp == 16) {
+    constexpr int kMmaWarp = kTileThreads / 32 - 1;
+    if (warp == kMmaWarp) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&c.tmem)) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
     }
@@ -199,18 +236,12 @@ __global__ void __launch_bounds__(kTileThreads, 1) msa_attention_kvq_tiles_kerne
             // (the ring's last stage has been read by all, and the unit before's rows once its last S is complete)
             if (tau > 0) wait(c.s_full[(tau - 1) & 1], ((tau - 1) >> 1) & 1);
             const uint32_t tau0 = tau;
+            TileLoader<D, N> loader(a, s, h, from, tid, a.k_codes);
+            const long long words = (s.start + static_cast<long long>(from) * kTileOfKeys) * a.p_slot + h * a.p_head;
             const auto load = [&](int k) {           // codes, scales and zero points of tile k
                 if (k < held) {
-                    const long long slot0 = s.start + static_cast<long long>(k) * kTileOfKeys;
-                    const int last = s.L - 1 - k * kTileOfKeys;
-                    const uint32_t stage = smem + G::oK + ((k - from) % G::kStages) * G::kCodes;
-                    #pragma unroll
-                    for (int i = 0; i < G::kPer; ++i) {
-                        const int item = i * 128 + tid, row = item / G::kPer, at = item - row * G::kPer;
-                        const int place = D == 128 ? at ^ ((row >> 1) & 3) : D == 64 ? at ^ ((row >> 2) & 1) : at;
-                        copy_async<G::kCopy>(stage + row * G::kPitch + place * G::kCopy, a.k_codes + (slot0 + min(row, last)) * a.slot_stride + h * a.head_stride + at * G::kCopy);
-                    }
-                    const long long p = (slot0 + min(key, last)) * a.p_slot + h * a.p_head;
+                    loader.next(a, smem + G::oK + ((k - from) % G::kStages) * G::kCodes, tid);
+                    const long long p = words + (static_cast<long long>(k - from) * kTileOfKeys + min(key, s.L - 1 - k * kTileOfKeys)) * a.p_slot;
                     const uint32_t dst = smem + G::oKParams + (((tau0 + (k - from)) % G::kParams) * kTileOfKeys + key) * 8;
                     copy_async<4>(dst, a.k_params + p);
                     copy_async<4>(dst + 4, a.v_params + p);
@@ -306,18 +337,14 @@ __global__ void __launch_bounds__(kTileThreads, 1) msa_attention_kvq_tiles_kerne
             const Seq s = line.s;
             const int P = prefix_chunks<kTileOfKeys>(s.L), from = line.from, to = line.to, held = min(to, P), h = min(line.head0, a.n_heads - 1);
             const bool real = line.head0 < a.n_heads;
+            TileLoader<D, N> loader(a, s, h, from, t, a.v_codes);
+            const long long words = (s.start + static_cast<long long>(from) * kTileOfKeys) * a.p_slot + h * a.p_head;
             const auto load = [&](int k) {
                 if (k < held) {
-                    const long long slot0 = s.start + static_cast<long long>(k) * kTileOfKeys;
-                    const int last = s.L - 1 - k * kTileOfKeys, st = (k - from) % G::kStages;
-                    const uint32_t stage = smem + G::oV + st * G::kCodes;
-                    #pragma unroll
-                    for (int i = 0; i < G::kPer; ++i) {
-                        const int item = i * 128 + t, row = item / G::kPer, at = item - row * G::kPer;
-                        const int place = D == 128 ? at ^ ((row >> 1) & 3) : D == 64 ? at ^ ((row >> 2) & 1) : at;
-                        copy_async<G::kCopy>(stage + row * G::kPitch + place * G::kCopy, a.v_codes + (slot0 + min(row, last)) * a.slot_stride + h * a.head_stride + at * G::kCopy);
-                    }
-                    copy_async<4>(smem + G::oVParams + (st * kTileOfKeys + t) * 4, a.v_params + (slot0 + min(t, last)) * a.p_slot + h * a.p_head);
+                    const int st = (k - from) % G::kStages;
+                    loader.next(a, smem + G::oV + st * G::kCodes, t);
+                    copy_async<4>(smem + G::oVParams + (st * kTileOfKeys + t) * 4,
+                                  a.v_params + words + (static_cast<long long>(k - from) * kTileOfKeys + min(t, s.L - 1 - k * kTileOfKeys)) * a.p_slot);
                 }
                 copy_commit();
             };
@@ -409,10 +436,10 @@ __global__ void __launch_bounds__(kTileThreads, 1) msa_attention_kvq_tiles_kerne
             }
             copy_wait<0>();
         }
-    } else if (warp < 16) {
+    } else if (warp < kMmaWarp) {
         // ---- softmax ------------------------------------------------------------------------
         const int group = (warp - 8) >> 2, key = 32 * quad + lane, bar = 3 + group;
-        const uint32_t all = C == 32 ? 0xffffffffu : (1u << C) - 1u;
+        constexpr uint32_t all = (1u << C) - 1u;
         uint32_t unit = 0;
         int* const counters = reinterpret_cast<int*>(a.ws + kWsHeaderBytes);
         float* const partial = reinterpret_cast<float*>(a.ws + kWsHeaderBytes + (4ull * gridDim.x + 255) / 256 * 256);
@@ -486,9 +513,10 @@ __global__ void __launch_bounds__(kTileThreads, 1) msa_attention_kvq_tiles_kerne
                     for (int i = 0; i < C; ++i)
                         if (!(vis >> i & 1u)) d[i] = -INFINITY;
                 }
-                float most = d[0];
+                float top[4] = {d[0], d[1], d[2], d[3]};
                 #pragma unroll
-                for (int i = 1; i < C; ++i) most = fmaxf(most, d[i]);
+                for (int i = 4; i < C; ++i) top[i & 3] = fmaxf(top[i & 3], d[i]);
+                const float most = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
                 if (any_of_group(bar, most > 8.f || k == from || (k >= P && seen != all))) {
                     // references go up to the maxima (a row's first one: to its maximum, whatever it is)
                     int own = 0;
@@ -566,7 +594,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) msa_attention_kvq_tiles_kerne
                     l[i] = keep + __shfl_xor_sync(0xffffffffu, give, w);
                 }
             }
-            c.sums[group][quad][lane] = l[0];
+            if (lane < C) c.sums[group][quad][lane] = l[0];
             uint32_t raw[C];
             tmem_load<C>(tmem + G::kTmemO + group * C + lanes, raw);
             named_barrier(bar, 128);
@@ -601,11 +629,11 @@ __global__ void __launch_bounds__(kTileThreads, 1) msa_attention_kvq_tiles_kerne
                 #pragma unroll
                 for (int i = 0; i < C; ++i)
                     if (group * C + i < rows && dim < D) __stcg(mine + (group * C + i) * (D + 4) + dim, __uint_as_float(raw[i]));
-                named_barrier(5, 256);
+                named_barrier(3 + kTileGroups, kTileSoftmax);
                 if (tid == 256) {
                     c.joined = last_piece(counters + (share.first << line.team_log2) + line.member, share.last - share.first + 1);
                 }
-                named_barrier(5, 256);
+                named_barrier(3 + kTileGroups, kTileSoftmax);
                 if (c.joined) {
                     // 8 values of a row at a time, up to four partial rows on their way
                     const float* const p0 = partial + share.place(line, share.first) * kPartial;
@@ -613,7 +641,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) msa_attention_kvq_tiles_kerne
                     const int n = share.last - share.first + 1, items = rows * (D / 8);
                     const float* const p1 = partial + share.place(line, share.first + 1) * kPartial;
                     #pragma unroll 1
-                    for (int item = tid - 256; item < items; item += 256) {
+                    for (int item = tid - 256; item < items; item += kTileSoftmax) {
                         const int r = item / (D / 8), d0 = (item - r * (D / 8)) * 8;
                         float m = kNoRef, sm = 0.f, o[8] = {};
                         #pragma unroll 1
@@ -633,7 +661,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) msa_attention_kvq_tiles_kerne
                         }
                         if (ok) store_row<D>(a, line.row0 + r < s.T, c.out[r], d0, o, m, sm);
                     }
-                    named_barrier(5, 256);           // (both groups read all rows' places)
+                    named_barrier(3 + kTileGroups, kTileSoftmax);           // (all groups read all rows' places)
                 }
             }
             ++unit;
@@ -643,8 +671,8 @@ __global__ void __launch_bounds__(kTileThreads, 1) msa_attention_kvq_tiles_kerne
         uint32_t unit = 0;
         const uint32_t base = uniform(smem);
         const uint64_t dq = desc_k_major(base + G::oQ), dp = desc_mn_major(base + G::oP, 0);
-        const Line<N, kTileOfKeys, 0>& line = walks[4].line;
-        while (next_unit(walks[4], lane == 0, 0, 32)) {
+        const Line<N, kTileOfKeys, 0>& line = walks[2 + kTileGroups].line;
+        while (next_unit(walks[2 + kTileGroups], lane == 0, 0, 32)) {
             const uint32_t tiles = uniform(static_cast<uint32_t>(line.to - line.from));
             const auto product = [&](uint32_t t, bool first) {       // O^T (+)= V^T P^T of tile t
                 if (first && unit > 0) wait(c.o_free, (unit - 1) & 1);
@@ -679,7 +707,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) msa_attention_kvq_tiles_kerne
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    if (warp == 16) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem));
+    if (warp == kMmaWarp) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem));
 }
 
 }  // namespace ss
