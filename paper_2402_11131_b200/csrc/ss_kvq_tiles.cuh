@@ -89,8 +89,11 @@ struct TileCtrl {
     uint32_t see[kTileGroups][64];                                          // per group and node: the rows that see it
     long long out[64];                                            // where a row's output goes (element offset)
     float neg_ref[64];
-    int tile_max[kTileGroups][4][16];
-    float sums[kTileGroups][4][16];
+    int tile_max[kTileGroups][4][32];
+    float sums[kTileGroups][4][32];
+    unsigned long long vote[kTileGroups][2];                      // the warps of a group have looked at their scores; a reference has to go up
+    int hot[kTileGroups][2];
+    int first[kTileGroups], last[kTileGroups], second[kTileGroups];          // the unit's pieces
     uint32_t tmem;
     int abort, joined;
 };
@@ -193,6 +196,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) msa_attention_kvq_tiles_kerne
             mbar_init(smem_u32(&c.s_free[i]), kTileSoftmax), mbar_init(smem_u32(&c.p_full[i]), kTileSoftmax);
             mbar_init(smem_u32(&c.s_full[i]), 2), mbar_init(smem_u32(&c.pv_done[i]), 1);
         }
+        for (int i = 0; i < 2 * kTileGroups; ++i) mbar_init(smem_u32(&c.vote[i >> 1][i & 1]), 4), c.hot[i >> 1][i & 1] = 0;
         mbar_init(smem_u32(&c.o_free), kTileSoftmax), mbar_init(smem_u32(&c.drain), 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -439,11 +443,12 @@ __global__ void __launch_bounds__(kTileThreads, 1) msa_attention_kvq_tiles_kerne
     } else if (warp < kMmaWarp) {
         // ---- softmax ------------------------------------------------------------------------
         const int group = (warp - 8) >> 2, key = 32 * quad + lane, bar = 3 + group;
-        constexpr uint32_t all = (1u << C) - 1u;
+        constexpr uint32_t all = C == 32 ? 0xffffffffu : (1u << C) - 1u;
         uint32_t unit = 0;
         int* const counters = reinterpret_cast<int*>(a.ws + kWsHeaderBytes);
         float* const partial = reinterpret_cast<float*>(a.ws + kWsHeaderBytes + (4ull * gridDim.x + 255) / 256 * 256);
         constexpr int kPartial = N * (D + 4);
+        const uint32_t weights = smem + G::oP + key * 128;        // the key's row of P^T
         // TMEM lane to dimension
         const int byte = 16 * quad + (lane & 15), dim = 8 * (byte >> 2) + ((byte & 1) << 2) + ((byte >> 1) & 1) + ((lane >> 4) << 1);
         const Line<N, kTileOfKeys, 0>& line = walks[2 + group].line;
@@ -468,6 +473,10 @@ __global__ void __launch_bounds__(kTileThreads, 1) msa_attention_kvq_tiles_kerne
                 }
                 if (lane < 16) c.see[group][16 * quad + lane] = own;
                 if (quad == 0 && lane < C) c.out[n] = out, c.neg_ref[n] = 0.f;
+                if (key == 96) {
+                    const Pieces share(line);
+                    c.first[group] = share.first, c.last[group] = share.last, c.second[group] = share.second;
+                }
             }
             named_barrier(bar, 128);
             float l[C];
@@ -479,46 +488,59 @@ __global__ void __launch_bounds__(kTileThreads, 1) msa_attention_kvq_tiles_kerne
                 const uint32_t parity = (tau >> 1) & 1;
                 wait(c.s_full[tau & 1], parity);
                 tc_fence_after();
-                uint32_t raw[C];
-                tmem_load<C>(tmem + G::kTmemS + (tau & 1) * N + group * C + lanes, raw);
                 const uint2 params = lds64(smem + G::oKParams + ((tau % G::kParams) * kTileOfKeys + key) * 8);
-                tmem_wait_ld();
-                tc_fence_before();
-                mbar_arrive(smem_u32(&c.s_free[tau & 1]));
                 const float sk = scale_of(params.x) * a.scale, sv = scale_of(params.y);
-                float d[C];
-                const unsigned long long sk2 = pack_f32x2(sk, sk);
-                #pragma unroll
-                for (int i = 0; i < C; i += 4) {
-                    const float4 r = *reinterpret_cast<const float4*>(&c.neg_ref[group * C + i]);
-                    unpack_f32x2(fma_f32x2(sk2, pack_f32x2(__uint_as_float(raw[i]), __uint_as_float(raw[i + 1])), pack_f32x2(r.x, r.y)), d[i], d[i + 1]);
-                    unpack_f32x2(fma_f32x2(sk2, pack_f32x2(__uint_as_float(raw[i + 2]), __uint_as_float(raw[i + 3])), pack_f32x2(r.z, r.w)), d[i + 2], d[i + 3]);
-                }
+                // rows that see the key: all of them if it is a cached one; else those of its node's descendants; of a stream key, from its
+                // own row to its node's last
+                uint32_t vis = all;
                 if (k < P) {
-                    if ((k + 1) * kTileOfKeys > L && k * kTileOfKeys + key >= L) {
-                        #pragma unroll
-                        for (int i = 0; i < C; ++i) d[i] = -INFINITY;
-                    }
+                    if (k * kTileOfKeys + key >= L) vis = 0u;
                 } else {
-                    // rows that see the key: those of its node's descendants; of a stream key, from its own row to its node's last
                     const int e = (k - P) * kTileOfKeys + key;
-                    uint32_t vis = 0u;
+                    vis = 0u;
                     if (e < x.T) {
                         vis = c.see[group][e];
                     } else if (e < x.count) {
                         const int own = e - x.T + x.t0 * x.gamma, first = x.T + own - x.row0 - group * C, last = first + x.gamma - 1 - own % x.gamma;
                         if (first < C && last >= 0) vis = (0xffffffffu >> (31 - min(last, 31))) & (0xffffffffu << max(first, 0));
                     }
-                    #pragma unroll
-                    for (int i = 0; i < C; ++i)
-                        if (!(vis >> i & 1u)) d[i] = -INFINITY;
                 }
+                const bool masked = __any_sync(0xffffffffu, (vis & all) != all);
+                float d[C];
+                // scores above their references, in log2 units; -inf where the row does not see the key
+                const auto scores = [&]() {
+                    uint32_t raw[C];
+                    tmem_load<C>(tmem + G::kTmemS + (tau & 1) * N + group * C + lanes, raw);
+                    tmem_wait_ld();
+                    const unsigned long long sk2 = pack_f32x2(sk, sk);
+                    #pragma unroll
+                    for (int i = 0; i < C; i += 4) {
+                        const float4 r = *reinterpret_cast<const float4*>(&c.neg_ref[group * C + i]);
+                        unpack_f32x2(fma_f32x2(sk2, pack_f32x2(__uint_as_float(raw[i]), __uint_as_float(raw[i + 1])), pack_f32x2(r.x, r.y)), d[i], d[i + 1]);
+                        unpack_f32x2(fma_f32x2(sk2, pack_f32x2(__uint_as_float(raw[i + 2]), __uint_as_float(raw[i + 3])), pack_f32x2(r.z, r.w)), d[i + 2], d[i + 3]);
+                    }
+                    if (masked) {
+                        #pragma unroll
+                        for (int i = 0; i < C; ++i)
+                            if (!(vis >> i & 1u)) d[i] = -INFINITY;
+                    }
+                };
+                scores();
                 float top[4] = {d[0], d[1], d[2], d[3]};
                 #pragma unroll
                 for (int i = 4; i < C; ++i) top[i & 3] = fmaxf(top[i & 3], d[i]);
-                const float most = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
-                if (any_of_group(bar, most > 8.f || k == from || (k >= P && seen != all))) {
+                // does a row of the group need a higher reference?  While the four warps' answers come in, the weights are computed as if not.
+                const bool hot = __any_sync(0xffffffffu, fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) > 8.f) || k == from || (k >= P && seen != all);
+                if (lane == 0) {
+                    if (hot) *const_cast<volatile int*>(&c.hot[group][tau & 1]) = 1;
+                    mbar_arrive(smem_u32(&c.vote[group][tau & 1]));
+                }
+                #pragma unroll
+                for (int i = 0; i < C; ++i) d[i] = exp2_approx(d[i]);
+                wait(c.vote[group][tau & 1], parity);
+                if (*const_cast<volatile int*>(&c.hot[group][tau & 1])) {
                     // references go up to the maxima (a row's first one: to its maximum, whatever it is)
+                    scores();
                     int own = 0;
                     #pragma unroll
                     for (int i = 0; i < C; ++i) {
@@ -527,6 +549,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) msa_attention_kvq_tiles_kerne
                     }
                     if (lane < C) c.tile_max[group][quad][lane] = own;
                     named_barrier(bar, 128);
+                    c.hot[group][tau & 1] = 0;
                     float by = 0.f, f = 1.f;
                     bool any = false;
                     if (lane < C) {
@@ -539,10 +562,10 @@ __global__ void __launch_bounds__(kTileThreads, 1) msa_attention_kvq_tiles_kerne
                     seen |= __ballot_sync(0xffffffffu, any);
                     #pragma unroll
                     for (int i = 0; i < C; ++i) {
-                        d[i] -= __shfl_sync(0xffffffffu, by, i);
+                        d[i] = exp2_approx(d[i] - __shfl_sync(0xffffffffu, by, i));
                         l[i] *= __shfl_sync(0xffffffffu, f, i);
                     }
-                    if (k > from) {             // and O with them: the products so far are complete, this tile's waits for our weights
+                    if (k > from) {                  // and O with them: the products so far are complete, this tile's waits for our weights
                         wait(c.pv_done[(tau - 1) & 1], ((tau - 1) >> 1) & 1);
                         tc_fence_after();
                         #pragma unroll
@@ -559,6 +582,8 @@ __global__ void __launch_bounds__(kTileThreads, 1) msa_attention_kvq_tiles_kerne
                     }
                     named_barrier(bar, 128);
                 }
+                tc_fence_before();
+                mbar_arrive(smem_u32(&c.s_free[tau & 1]));
                 // (this tile's S was committed behind the product of two tiles ago: its weights' place is free)
                 const unsigned long long sv2 = pack_f32x2(sv, sv);
                 #pragma unroll
@@ -566,13 +591,13 @@ __global__ void __launch_bounds__(kTileThreads, 1) msa_attention_kvq_tiles_kerne
                     uint32_t y[4];
                     #pragma unroll
                     for (int q = 0; q < 4; ++q) {
-                        const unsigned long long e = pack_f32x2(exp2_approx(d[i + 2 * q]), exp2_approx(d[i + 2 * q + 1]));
+                        const unsigned long long e = pack_f32x2(d[i + 2 * q], d[i + 2 * q + 1]);
                         unpack_f32x2(add_f32x2(pack_f32x2(l[i + 2 * q], l[i + 2 * q + 1]), e), l[i + 2 * q], l[i + 2 * q + 1]);
                         float u, v;
                         unpack_f32x2(fma_f32x2(e, sv2, 0ull), u, v);
                         y[q] = pack2_bf16(u, v);
                     }
-                    st_shared_v4(smem + G::oP + (tau & 1) * G::kP + key * 128 + (((group * (C / 8) + (i >> 3)) ^ (key & 7)) << 4), y[0], y[1], y[2], y[3]);
+                    st_shared_v4(weights + (tau & 1) * G::kP + ((((i >> 3) + group * (C / 8)) ^ (key & 7)) << 4), y[0], y[1], y[2], y[3]);
                 }
                 fence_async_smem();
                 mbar_arrive(smem_u32(&c.p_full[tau & 1]));
@@ -605,41 +630,59 @@ __global__ void __launch_bounds__(kTileThreads, 1) msa_attention_kvq_tiles_kerne
             tc_fence_before();
             mbar_arrive(smem_u32(&c.o_free));
             const bool ok = *const_cast<volatile int*>(&c.abort) == 0;
-            const Pieces share(line);
-            float* const mine = partial + share.place(line, line.me) * kPartial;
             const int rows = line.head0 < a.n_heads ? min(N, s.rows - line.row0) : 0;
             if (line.whole()) {
                 const float f = 1.f / sum;
-                if (quad == 0 && lane < C && ok) {
+                if (quad == 0 && lane < C && ok && group * C + lane < rows) {
                     const int n = group * C + lane;
-                    if (n < rows) {
-                        float* lse = line.row0 + n < s.T ? a.lse_main : a.lse_spec;
-                        if (lse != nullptr) lse[c.out[n] / D] = (ref + log2f(sum)) * 0.6931471805599453f;
+                    float* lse = line.row0 + n < s.T ? a.lse_main : a.lse_spec;
+                    if (lse != nullptr) lse[c.out[n] / D] = (ref + log2f(sum)) * 0.6931471805599453f;
+                }
+                // to rows of dimensions, by way of the group's part of the first buffer of P: a TMEM lane's rows lie where a key's weights do
+                #pragma unroll
+                for (int i = 0; i < C; i += 8) {
+                    uint32_t y[4];
+                    #pragma unroll
+                    for (int q = 0; q < 4; ++q)
+                        y[q] = pack2_bf16(__uint_as_float(raw[i + 2 * q]) * __shfl_sync(0xffffffffu, f, i + 2 * q),
+                                          __uint_as_float(raw[i + 2 * q + 1]) * __shfl_sync(0xffffffffu, f, i + 2 * q + 1));
+                    st_shared_v4(weights + ((((i >> 3) + group * (C / 8)) ^ (key & 7)) << 4), y[0], y[1], y[2], y[3]);
+                }
+                named_barrier(bar, 128);
+                // matrices of 8 dimensions (a word's) by 8 rows, transposed: a lane gets two dimensions of a row
+                #pragma unroll 1
+                for (int m0 = 4 * quad; m0 < D / 8 * (C / 8); m0 += 16) {
+                    const int m = m0 + (lane >> 3), word = m / (C / 8), eight = m - word * (C / 8), dd = lane & 7;
+                    const int from_lane = 32 * (word >> 2) + 4 * (word & 3) + ((dd >> 2) & 1) + 2 * (dd & 1) + 8 * (dd & 2);
+                    uint32_t q[4];
+                    load_transposed_halves(smem + G::oP + from_lane * 128 + (((eight + group * (C / 8)) ^ (from_lane & 7)) << 4), q);
+                    #pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int mi = m0 + i, wi = mi / (C / 8), n = group * C + 8 * (mi - wi * (C / 8)) + (lane >> 2);
+                        if (n < rows && ok)
+                            *reinterpret_cast<uint32_t*>((line.row0 + n < s.T ? a.o_main : a.o_spec) + c.out[n] + 8 * wi + 2 * (lane & 3)) = q[i];
                     }
                 }
-                #pragma unroll
-                for (int i = 0; i < C; ++i) {
-                    const float y = __uint_as_float(raw[i]) * __shfl_sync(0xffffffffu, f, i);
-                    const int n = group * C + i;
-                    if (n < rows && dim < D && ok) (line.row0 + n < s.T ? a.o_main : a.o_spec)[c.out[n] + dim] = __float2bfloat16_rn(y);
-                }
+                named_barrier(bar, 128);             // (the next unit's weights go there)
             } else {
-                if (quad == 0 && lane < C && group * C + lane < rows)
+                float* const mine = partial + (2ll * ((line.me << line.team_log2) + line.member) + (line.me == c.first[group] ? c.second[group] : 0)) * kPartial;
+                if (quad == 0 && lane < C)
                     __stcg(reinterpret_cast<float2*>(mine + (group * C + lane) * (D + 4) + D), make_float2(seen >> lane & 1u ? ref : kNoRef, sum));
-                #pragma unroll
-                for (int i = 0; i < C; ++i)
-                    if (group * C + i < rows && dim < D) __stcg(mine + (group * C + i) * (D + 4) + dim, __uint_as_float(raw[i]));
+                if (dim < D) {
+                    #pragma unroll
+                    for (int i = 0; i < C; ++i) __stcg(mine + (group * C + i) * (D + 4) + dim, __uint_as_float(raw[i]));
+                }
                 named_barrier(3 + kTileGroups, kTileSoftmax);
                 if (tid == 256) {
-                    c.joined = last_piece(counters + (share.first << line.team_log2) + line.member, share.last - share.first + 1);
+                    c.joined = last_piece(counters + (c.first[0] << line.team_log2) + line.member, c.last[0] - c.first[0] + 1);
                 }
                 named_barrier(3 + kTileGroups, kTileSoftmax);
                 if (c.joined) {
                     // 8 values of a row at a time, up to four partial rows on their way
-                    const float* const p0 = partial + share.place(line, share.first) * kPartial;
+                    const int first = c.first[group], n = c.last[group] - first + 1, items = rows * (D / 8);
+                    const float* const p0 = partial + (2ll * ((first << line.team_log2) + line.member) + c.second[group]) * kPartial;
                     const long long on = (2ll << line.team_log2) * kPartial;                 // between teams' places
-                    const int n = share.last - share.first + 1, items = rows * (D / 8);
-                    const float* const p1 = partial + share.place(line, share.first + 1) * kPartial;
+                    const float* const p1 = p0 - c.second[group] * kPartial + on;
                     #pragma unroll 1
                     for (int item = tid - 256; item < items; item += kTileSoftmax) {
                         const int r = item / (D / 8), d0 = (item - r * (D / 8)) * 8;
