@@ -84,13 +84,14 @@ struct TileLoader {
     }
 };
 
+template <int C>
 struct TileCtrl {
     unsigned long long k_full[2], s_full[2], s_free[2], v_full[2], p_full[2], pv_done[2], o_free, drain;
     uint32_t see[kTileGroups][64];                                          // per group and node: the rows that see it
     long long out[64];                                            // where a row's output goes (element offset)
     float neg_ref[64];
-    int tile_max[kTileGroups][4][32];
-    float sums[kTileGroups][4][32];
+    int tile_max[kTileGroups][4][C];
+    float sums[kTileGroups][4][C];
     unsigned long long vote[kTileGroups][2];                      // the warps of a group have looked at their scores; a reference has to go up
     int hot[kTileGroups][2];
     int first[kTileGroups], last[kTileGroups], second[kTileGroups];          // the unit's pieces
@@ -98,8 +99,8 @@ struct TileCtrl {
     int abort, joined;
 };
 
-__device__ __forceinline__ void tile_wait(uint32_t bar, uint32_t parity, TileCtrl& c, int* status) {
-    if (!mbar_try(bar, parity)) mbar_wait_slow(bar, parity, &c.abort, status);
+__device__ __forceinline__ void tile_wait(uint32_t bar, uint32_t parity, int* abort, int* status) {
+    if (!mbar_try(bar, parity)) mbar_wait_slow(bar, parity, abort, status);
 }
 // 128 threads agree on "any"
 __device__ __forceinline__ bool any_of_group(int id, bool x) {
@@ -179,12 +180,20 @@ __device__ __forceinline__ Extra extra_of(const KvqArgs& a, const Seq& s, int ro
     return x;
 }
 
+// Key e behind the prefix on its way to L2
+__device__ __forceinline__ void prefetch_extra(const KvqArgs& a, const Extra& x, int D, int b, int h, int e, const __nv_bfloat16* tree, const __nv_bfloat16* spec) {
+    if (e >= x.count) return;
+    const __nv_bfloat16* const src = (e < x.T ? tree : spec) + extra_offset(a, x, D, b, h, e);
+    prefetch_l2(src);
+    if (D > 64) prefetch_l2(src + D - 8);
+}
+
 template <int D, int N>
 __global__ void __launch_bounds__(kTileThreads, 1) msa_attention_kvq_tiles_kernel(const __grid_constant__ KvqArgs a) {
     using G = TileGeo<D, N>;
     constexpr int C = G::kRowsOfGroup;
     extern __shared__ __align__(1024) unsigned char smem_raw[];
-    __shared__ __align__(16) TileCtrl c;
+    __shared__ __align__(16) TileCtrl<C> c;
     __shared__ __align__(16) TileWalk<N> walks[3 + kTileGroups];    // K, V, softmax groups, MMAs
     const int tid = threadIdx.x, lane = tid & 31, warp = static_cast<int>(uniform(tid >> 5)), quad = warp & 3;
     const uint32_t smem = smem_u32(smem_raw);
@@ -219,7 +228,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) msa_attention_kvq_tiles_kerne
     tc_fence_after();
     const uint32_t tmem = uniform(c.tmem), lanes = static_cast<uint32_t>(32 * quad) << 16;
     // (a wait that runs out leaves the roles in step: everyone goes through the same tiles without waiting, and no output is written)
-    const auto wait = [&](unsigned long long& bar, uint32_t parity) { tile_wait(smem_u32(&bar), parity, c, status); };
+    const auto wait = [&](unsigned long long& bar, uint32_t parity) { tile_wait(smem_u32(&bar), parity, &c.abort, status); };
     // on to the next unit, all `threads` threads of a role together; id: their barrier
     const auto next_unit = [&](TileWalk<N>& w, bool leader, int id, int threads) {
         if (threads > 32) named_barrier(id, threads); else __syncwarp();
@@ -237,8 +246,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) msa_attention_kvq_tiles_kerne
             const Seq s = line.s;
             const int P = prefix_chunks<kTileOfKeys>(s.L), from = line.from, to = line.to, held = min(to, P), h = min(line.head0, a.n_heads - 1);
             const bool real = line.head0 < a.n_heads;
-            // (the ring's last stage has been read by all, and the unit before's rows once its last S is complete)
-            if (tau > 0) wait(c.s_full[(tau - 1) & 1], ((tau - 1) >> 1) & 1);
+            // (the ring's last stage has been read by all)
             const uint32_t tau0 = tau;
             TileLoader<D, N> loader(a, s, h, from, tid, a.k_codes);
             const long long words = (s.start + static_cast<long long>(from) * kTileOfKeys) * a.p_slot + h * a.p_head;
@@ -254,6 +262,8 @@ __global__ void __launch_bounds__(kTileThreads, 1) msa_attention_kvq_tiles_kerne
             };
             #pragma unroll 1
             for (int i = 0; i < G::kStages - 1; ++i) load(from + i);
+            // what lies behind the prefix comes to L2 meanwhile
+            if (to > P && real) prefetch_extra(a, extra_of(a, s, line.row0, N), D, line.b, h, key, a.k_tree, a.k_spec);
             // query rows, 16 bytes at a time (all of a thread's on their way at once), swizzled
             {
                 constexpr int kItems = N * (D / 8) / 128;
@@ -267,6 +277,8 @@ __global__ void __launch_bounds__(kTileThreads, 1) msa_attention_kvq_tiles_kerne
                         v[i] = *reinterpret_cast<const uint4*>((x.j < 0 ? a.q_main : a.q_spec) + row_offset(a, D, line.b, h, x) + 8 * at);
                     }
                 }
+                // the rows of the unit before have been read once its last S is complete
+                if (tau > 0) wait(c.s_full[(tau - 1) & 1], ((tau - 1) >> 1) & 1);
                 #pragma unroll
                 for (int i = 0; i < kItems; ++i) {
                     const int item = i * 128 + tid, r = item / (D / 8), at = item - r * (D / 8);
@@ -274,7 +286,6 @@ __global__ void __launch_bounds__(kTileThreads, 1) msa_attention_kvq_tiles_kerne
                 }
             }
             fence_async_smem();
-            const Extra x = extra_of(a, s, line.row0, N);
             #pragma unroll 1
             for (int k = from; k < to; ++k, ++tau) {
                 uint32_t w[G::kWords];
@@ -301,9 +312,12 @@ __global__ void __launch_bounds__(kTileThreads, 1) msa_attention_kvq_tiles_kerne
                 if (tau >= 2) wait(c.s_full[tau & 1], ((tau - 2) >> 1) & 1);
                 tc_fence_after();
                 const uint32_t dst = tmem + G::kTmemK + (tau & 1) * 64 + lanes;
-                const int e = (k - P) * kTileOfKeys + key;
                 const __nv_bfloat16* src = nullptr;
-                if (k >= held && real && e < x.count) src = (e < x.T ? a.k_tree : a.k_spec) + extra_offset(a, x, D, line.b, h, e);
+                if (k >= held && real) {
+                    const Extra x = extra_of(a, s, line.row0, N);
+                    const int e = (k - P) * kTileOfKeys + key;
+                    if (e < x.count) src = (e < x.T ? a.k_tree : a.k_spec) + extra_offset(a, x, D, line.b, h, e);
+                }
                 #pragma unroll
                 for (int i = 0; i < G::kWords; i += 8) {
                     uint32_t r[32];
@@ -354,7 +368,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) msa_attention_kvq_tiles_kerne
             };
             #pragma unroll 1
             for (int i = 0; i < G::kStages - 1; ++i) load(from + i);
-            const Extra x = extra_of(a, s, line.row0, N);
+            if (to > P && real) prefetch_extra(a, extra_of(a, s, line.row0, N), D, line.b, h, t, a.v_tree, a.v_spec);
             #pragma unroll 1
             for (int k = from; k < to; ++k, ++tau) {
                 const int st = (k - from) % G::kStages;
@@ -392,20 +406,37 @@ __global__ void __launch_bounds__(kTileThreads, 1) msa_attention_kvq_tiles_kerne
                 } else {
                     // bf16 rows in the order of the lanes: of 8 values the low codes' would be 0, 4, 1, 5, the high codes' 2, 6, 3, 7.  64 keys at
                     // a time, in the ring's place; a row's words are shared by two threads.
-                    if (tau >= 2) wait(c.pv_done[tau & 1], ((tau - 2) >> 1) & 1);
-                    tc_fence_after();
-                    #pragma unroll 1
-                    for (int half = 0; half < 2; ++half) {
-                        const int r = t >> 1, e = (k - P) * kTileOfKeys + 64 * half + r;
+                    const Extra x = extra_of(a, s, line.row0, N);
+                    const int r = t >> 1;
+                    const bool both = (k - P) * kTileOfKeys + 64 < x.count;      // (else the tile's upper half is empty)
+                    uint4 v[2 * G::kQuads];
+                    const auto fetch = [&](int half) {
+                        const int e = (k - P) * kTileOfKeys + 64 * half + r;
                         const __nv_bfloat16* src = nullptr;
                         if (real && e < x.count) src = (e < x.T ? a.v_tree : a.v_spec) + extra_offset(a, x, D, line.b, h, e);
-                        uint4 v[2 * G::kQuads];
                         #pragma unroll
                         for (int i = 0; i < 2 * G::kQuads; ++i) {
                             const int word = 2 * i + (t & 1);
                             v[i] = make_uint4(0u, 0u, 0u, 0u);
                             if (src && word < G::kWords) v[i] = *reinterpret_cast<const uint4*>(src + 8 * word);
                         }
+                    };
+                    fetch(0);
+                    if (tau >= 2) wait(c.pv_done[tau & 1], ((tau - 2) >> 1) & 1);
+                    tc_fence_after();
+                    #pragma unroll 1
+                    for (int half = 0; half < 2; ++half) {
+                        if (half > 0 && !both) {     // the weights there are zero; the values must be numbers
+                            if (mine) {
+                                uint32_t none[16];
+                                #pragma unroll
+                                for (int i = 0; i < 16; ++i) none[i] = 0u;
+                                tmem_store_lanes16(dst + 32, none);
+                                tmem_store_lanes16(dst + 32 + (16u << 16), none);
+                            }
+                            break;
+                        }
+                        if (half > 0) fetch(1);
                         named_barrier(2, 128);       // (what lay there has been read)
                         const uint32_t row = smem + G::oV + r * G::kRowOfV;
                         #pragma unroll
@@ -711,23 +742,23 @@ __global__ void __launch_bounds__(kTileThreads, 1) msa_attention_kvq_tiles_kerne
         }
     } else {
         // ---- MMAs ---------------------------------------------------------------------------
-        uint32_t unit = 0;
         const uint32_t base = uniform(smem);
         const uint64_t dq = desc_k_major(base + G::oQ), dp = desc_mn_major(base + G::oP, 0);
         const Line<N, kTileOfKeys, 0>& line = walks[2 + kTileGroups].line;
+        uint32_t unit = 0;
+        const auto product = [&](uint32_t t, bool first) {       // O^T (+)= V^T P^T of tile t
+            if (first && unit > 0) wait(c.o_free, (unit - 1) & 1);
+            wait(c.v_full[t & 1], (t >> 1) & 1);
+            wait(c.p_full[t & 1], (t >> 1) & 1);
+            tc_fence_after();
+            const uint64_t b = dp + (t & 1) * (G::kP >> 4);
+            const uint32_t va = tmem + G::kTmemV + (t & 1) * 64;
+            tc_mma_ts_steps(tmem + G::kTmemO, va, b, G::kIdescPV, first ? 0u : 1u);
+            tc_mma_ts_steps(tmem + G::kTmemO, va + 32, b + 4 * 128, G::kIdescPV, 1u);
+            tc_commit_e(smem_u32(&c.pv_done[t & 1]));
+        };
         while (next_unit(walks[2 + kTileGroups], lane == 0, 0, 32)) {
             const uint32_t tiles = uniform(static_cast<uint32_t>(line.to - line.from));
-            const auto product = [&](uint32_t t, bool first) {       // O^T (+)= V^T P^T of tile t
-                if (first && unit > 0) wait(c.o_free, (unit - 1) & 1);
-                wait(c.v_full[t & 1], (t >> 1) & 1);
-                wait(c.p_full[t & 1], (t >> 1) & 1);
-                tc_fence_after();
-                const uint64_t b = dp + (t & 1) * (G::kP >> 4);
-                const uint32_t va = tmem + G::kTmemV + (t & 1) * 64;
-                tc_mma_ts_steps(tmem + G::kTmemO, va, b, G::kIdescPV, first ? 0u : 1u);
-                tc_mma_ts_steps(tmem + G::kTmemO, va + 32, b + 4 * 128, G::kIdescPV, 1u);
-                tc_commit_e(smem_u32(&c.pv_done[t & 1]));
-            };
             #pragma unroll 1
             for (uint32_t i = 0; i < tiles; ++i, ++tau) {
                 wait(c.k_full[tau & 1], (tau >> 1) & 1);
