@@ -107,10 +107,10 @@ __device__ __forceinline__ Row row_of(int r, int T, int gamma) {
     return Row{t, s - t * gamma};
 }
 
-// Element offset of a row's vector in a main-stream or stream tensor
-__device__ __forceinline__ long long row_offset(const KvqArgs& a, int hd, int b, int h, const Row& r) {
-    const long long node = static_cast<long long>(b) * a.max_nodes + r.t;
-    return ((r.j < 0 ? node : node * a.gamma + r.j) * a.n_heads + h) * hd;
+// Element offset of row r's vector in the main-stream tensors (r < T) or in the streams' (rows there follow one another as they do here)
+__device__ __forceinline__ long long row_offset(const KvqArgs& a, int hd, int b, int h, int r, int T) {
+    const int nodes = b * a.max_nodes;               // (at most 65535 sequences' worth, see the entry point)
+    return ((r < T ? static_cast<long long>(nodes) + r : static_cast<long long>(nodes) * a.gamma + (r - T)) * a.n_heads + h) * hd;
 }
 
 constexpr float kNoRef = -FLT_MAX / 2;               // reference of a partial result that has seen no key
@@ -175,6 +175,11 @@ __device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1,
 __device__ __forceinline__ uint32_t pack2_f16(float lo, float hi) {
     uint32_t r;
     asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+__device__ __forceinline__ float round_f16(float x) {
+    float r;
+    asm("{\n\t.reg .b16 h;\n\tcvt.rn.f16.f32 h, %1;\n\tcvt.f32.f16 %0, h;\n\t}" : "=f"(r) : "f"(x));
     return r;
 }
 __device__ __forceinline__ uint32_t times16_bf16x2(uint32_t x) {
@@ -606,15 +611,12 @@ struct Extra {
 template <int D>
 __device__ __forceinline__ const __nv_bfloat16* query_row(const KvqArgs& a, int T, int rows, int b, int h, int r) {
     if (r >= rows || h >= a.n_heads) return nullptr;
-    const Row x = row_of(r, T, a.gamma);
-    return (x.j < 0 ? a.q_main : a.q_spec) + row_offset(a, D, b, h, x);
+    return (r < T ? a.q_main : a.q_spec) + row_offset(a, D, b, h, r, T);
 }
 
 // Where key e lies in k_tree / v_tree or k_spec / v_spec (elements)
 __device__ __forceinline__ long long extra_offset(const KvqArgs& a, const Extra& x, int D, int b, int h, int e) {
-    if (e < x.T) return row_offset(a, D, b, h, Row{e, -1});
-    const int s = e - x.T;
-    return row_offset(a, D, b, h, Row{x.t0 + s / x.gamma, s % x.gamma});
+    return row_offset(a, D, b, h, e < x.T ? e : e + x.t0 * x.gamma, x.T);
 }
 
 // Scores above their references of 16 keys behind the prefix, from `first` on; what a row does not see is -inf
@@ -958,7 +960,7 @@ __global__ void __launch_bounds__(kThreads, NG == 1 ? 3 : 2) msa_attention_kvq_r
                 join_row(o, m, l, stats[i * ROWS + r], *reinterpret_cast<const float4*>(src), *reinterpret_cast<const float4*>(src + 4));
             }
             if (whole) {
-                store_row<D>(a, row0 + r < s.T, row_offset(a, D, b, h0 + hd, row_of(row0 + r, s.T, a.gamma)), d0, o, m, l);
+                store_row<D>(a, row0 + r < s.T, row_offset(a, D, b, h0 + hd, row0 + r, s.T), d0, o, m, l);
             } else {
                 float* dst = place(line.me) + hr * (D + 4) + d0;
                 __stcg(reinterpret_cast<float4*>(dst), make_float4(o[0], o[1], o[2], o[3]));
@@ -991,7 +993,7 @@ __global__ void __launch_bounds__(kThreads, NG == 1 ? 3 : 2) msa_attention_kvq_r
                         for (int k = 0; k < 4; ++k)
                             if (i + k <= share.last) join_row(o, m, l, st[k], u[k], v[k]);
                     }
-                    store_row<D>(a, row0 + r < s.T, row_offset(a, D, b, h0 + hd, row_of(row0 + r, s.T, a.gamma)), d0, o, m, l);
+                    store_row<D>(a, row0 + r < s.T, row_offset(a, D, b, h0 + hd, row0 + r, s.T), d0, o, m, l);
                 }
             }
         }
@@ -1055,7 +1057,7 @@ static int32_t launch_kvq(const KvqPlan& k, const KvqArgs& args, int ctas, cudaS
 static int32_t kvq_check_shapes(const ss_kvq_attn_params* p) {
     if (!p) return SS_ERR_INVALID_ARG;
     const ss_kvq_cache& c = p->cache;
-    if (p->batch < 1 || c.n_heads < 1 || p->max_nodes < 1 || p->gamma < 0) return SS_ERR_INVALID_ARG;
+    if (p->batch < 1 || p->batch > 65535 || c.n_heads < 1 || p->max_nodes < 1 || p->gamma < 0) return SS_ERR_INVALID_ARG;
     if (c.head_dim != 64 && c.head_dim != 80 && c.head_dim != 128) return SS_ERR_UNSUPPORTED;
     if (p->max_nodes > SS_MAX_NODES || p->gamma > SS_MAX_GAMMA) return SS_ERR_UNSUPPORTED;
     return SS_OK;
