@@ -193,21 +193,22 @@ __device__ __forceinline__ float zero_over_16(uint32_t word) { return __uint_as_
 constexpr float kCode = 5.9604644775390625e-08f;                 // 2^-24: what a code counts in an MMA
 
 // The line of steps as one CTA sees it (every thread, or one warp of a role, works it out for itself)
-template <int ROWS, int CHUNK, int WARPS_LOG2>
+// START: what a unit costs before its first step, in steps, for the sake of an even deal.
+template <int ROWS, int CHUNK, int WARPS_LOG2, int START>
 struct Line {
     int heads_log2, team_log2, steps_log2;           // heads and chunks per step of a CTA, CTAs of a team
     int groups, me, member;                          // of heads; this CTA's team and its place there
     int pieces, whole_steps;
     long long total, share, rest;
     long long pos, end, base;                        // the piece's next step and its end; first step of sequence b
-    int b, steps, units, unit;                       // sequence; its units and their steps; the next unit
+    int b, steps, units, unit, start;                // sequence; its units and their steps; the next unit; steps that stand for a unit's start
     Seq s;
     // the unit at hand
-    long long unit0;
+    long long unit0;                                 // its first step's place in the line
     int from, to, head0, row0;                       // steps of it, its first head for this CTA and its first row
 
     __device__ __forceinline__ int steps_of(const Seq& q) const { return (q.chunks + (1 << steps_log2) - 1) >> steps_log2; }
-    __device__ __forceinline__ long long line_of(const Seq& q) const { return static_cast<long long>(steps_of(q)) * q.blocks * groups; }
+    __device__ __forceinline__ long long line_of(const Seq& q) const { return static_cast<long long>(q.blocks > 0 ? steps_of(q) + start : 0) * q.blocks * groups; }
     // first step of team i's piece
     __device__ __forceinline__ long long cut(int i) const {
         const int u = pieces > 0 ? i / pieces : 0, k = i - u * pieces;
@@ -227,6 +228,7 @@ struct Line {
         const Shape shape = shape_of<WARPS_LOG2>(a, chunks, blocks);
         heads_log2 = shape.heads, team_log2 = shape.team, steps_log2 = WARPS_LOG2 - shape.heads;
         groups = (a.n_heads + (1 << (heads_log2 + team_log2)) - 1) >> (heads_log2 + team_log2);
+        start = a.batch == 1 ? 0 : START;
         total = 0;
         #pragma unroll 1
         for (int b0 = 0; b0 < a.batch; b0 += 32)
@@ -273,19 +275,20 @@ struct Line {
             s = load_seq<ROWS, CHUNK>(a, b);
         }
         steps = steps_of(s), units = s.blocks * groups;
-        unit = static_cast<int>(divide(pos - base, steps));
+        unit = static_cast<int>(divide(pos - base, steps + start));
         return true;
     }
     // the unit at hand, or false at the end of the piece
     __device__ __forceinline__ bool next(const KvqArgs& a) {
         if (pos >= end) return false;
         while (unit >= units) {                      // on to the next sequence that has units
-            base += static_cast<long long>(units) * steps;
+            base += static_cast<long long>(units) * (steps + start);
             s = load_seq<ROWS, CHUNK>(a, ++b);
             steps = steps_of(s), units = s.blocks * groups, unit = 0;
         }
-        unit0 = base + static_cast<long long>(unit) * steps;
-        from = static_cast<int>(pos - unit0), to = static_cast<int>(min(end - unit0, static_cast<long long>(steps)));
+        unit0 = base + static_cast<long long>(unit) * (steps + start) + start;
+        from = static_cast<int>(max(pos - unit0, 0ll)), to = static_cast<int>(min(end - unit0, static_cast<long long>(steps)));
+        if (to <= from) return false;                // (the piece ends before the unit's first step)
         const int group = static_cast<int>(static_cast<uint32_t>(unit) / static_cast<uint32_t>(s.blocks));
         row0 = (unit - group * s.blocks) * ROWS;
         head0 = ((group << team_log2) + member) << heads_log2;
@@ -310,7 +313,7 @@ struct Pieces {
             #pragma unroll 1
             while (line.cut(last + 1) < line.unit0 + line.steps) ++last;
         }
-        second = at < line.unit0 ? 1 : 0;
+        second = at < line.unit0 - line.start ? 1 : 0;
     }
     template <typename L>
     __device__ __forceinline__ long long place(const L& line, int i) const { return 2ll * ((i << line.team_log2) + line.member) + (i == first ? second : 0); }
@@ -797,7 +800,7 @@ __global__ void __launch_bounds__(kThreads, NG == 1 ? 3 : 2) msa_attention_kvq_r
     wait_for_previous_kernel();
     release_next_kernel();
 
-    Line<ROWS, kChunk, kWarpsLog2> line;
+    Line<ROWS, kChunk, kWarpsLog2, 0> line;
     if (!line.begin(a, lane)) return;
     const int HW = 1 << line.heads_log2, KS = 1 << line.steps_log2;
     int* const counters = reinterpret_cast<int*>(a.ws + kWsHeaderBytes);

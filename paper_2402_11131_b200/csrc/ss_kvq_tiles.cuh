@@ -16,6 +16,8 @@
 
 namespace ss {
 
+// A unit's start and end take as long as some five tiles.
+constexpr int kTileStart = 5;
 constexpr int kTileOfKeys = 128, kTileGroups = 4, kTileSoftmax = 128 * kTileGroups, kTileThreads = 256 + kTileSoftmax + 32;
 
 template <int D, int N>
@@ -24,27 +26,27 @@ struct TileGeo {
     static constexpr int kPitch = D == 128 ? 64 : D == 80 ? 48 : 32;         // bytes of a key's codes in shared memory (16-byte aligned)
     static constexpr int kCopy = D == 80 ? 8 : 16, kPer = D / 2 / kCopy;     // asynchronous copies per key
     static constexpr int kWords = D / 8;
-        static constexpr int kQuads = (D + 31) / 32;                  // warps that have V lanes
+    static constexpr int kColumns = D / 2;                        // TMEM columns of a K tile
+    static constexpr int kQuads = (D + 31) / 32;                  // warps that have V lanes
     static constexpr int kCodes = kTileOfKeys * kPitch;
     static constexpr int kStages = 3, kParams = 8;
     static constexpr int kBoxes = D > 64 ? 2 : 1, kBox = N * 128;
     static constexpr int kRowOfV = 64 * kQuads;                   // bytes of a bf16 row in lane order
     static constexpr int kP = kTileOfKeys * 128;
-    static constexpr int oP = 0, oQ = oP + 2 * kP, oZ = oQ + kBoxes * kBox, oSums = oZ + N * 32, oK = oSums + N * 64, oV = oK + kStages * kCodes;
+    static constexpr int oP = 0, oQ = oP + 2 * kP, oK = oQ + kBoxes * kBox, oV = oK + kStages * kCodes;
     static constexpr int oKParams = oV + kStages * kCodes, oVParams = oKParams + kParams * kTileOfKeys * 8;
     static constexpr int kBytes = oVParams + kStages * kTileOfKeys * 4;
     static_assert(64 * kRowOfV <= kStages * kCodes, "half a tile of bf16 values takes the place of the ring");
-    static constexpr uint32_t kTmemK = 0, kTmemV = 144, kTmemS = 272, kTmemO = 272 + 2 * N;          // K: 72 columns a buffer, the last 8 for zero points
-    // fp32 sums, 128 lanes, N columns; S of fp16, P V of bf16 with P^T MN-major
-    static constexpr uint32_t kIdescS = (1u << 4) | (static_cast<uint32_t>(N >> 3) << 17) | ((128u >> 4) << 24);
-    static constexpr uint32_t kIdescPV = kIdescS | (1u << 7) | (1u << 10) | (1u << 16);
+    static constexpr uint32_t kTmemK = 0, kTmemV = 128, kTmemS = 256, kTmemO = 256 + 2 * N;
+    static constexpr uint32_t kIdesc = (1u << 4) | (1u << 7) | (1u << 10) | (static_cast<uint32_t>(N >> 3) << 17) | ((128u >> 4) << 24);
+    static constexpr uint32_t kIdescS = kIdesc, kIdescPV = kIdesc | (1u << 16);
 };
 
 // A role's place in the list of units: the role's first thread goes on, the others read.  In shared memory, since it is used between
 // units only and would cost every thread some 40 registers.
 template <int N>
 struct TileWalk {
-    Line<N, kTileOfKeys, 0> line;
+    Line<N, kTileOfKeys, 0, kTileStart> line;
     int more;
 };
 
@@ -94,8 +96,6 @@ struct TileCtrl {
     float sums[kTileGroups][4][C];
     unsigned long long vote[kTileGroups][2];                      // the warps of a group have looked at their scores; a reference has to go up
     int hot[kTileGroups][2];
-    float factor[4];                                              // of a unit (ring): what a unit of S is worth
-    uint32_t q_max[4];
     int first[kTileGroups], last[kTileGroups], second[kTileGroups];          // the unit's pieces
     uint32_t tmem;
     int abort, joined;
@@ -151,14 +151,6 @@ __device__ __forceinline__ void load_transposed_bytes(uint32_t addr, uint32_t& r
 }
 __device__ __forceinline__ void load_transposed_halves(uint32_t addr, uint32_t (&r)[4]) {
     asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
-}
-// two columns
-__device__ __forceinline__ void tmem_store2(uint32_t addr, uint32_t x, uint32_t y) {
-    asm volatile("tcgen05.st.sync.aligned.32x32b.x2.b32 [%0], {%1, %2};" ::"r"(addr), "r"(x), "r"(y) : "memory");
-}
-// K-major operand of 16 columns without a swizzle: 8 rows by 16 bytes are 128 bytes in a row, the second 16 bytes of the rows 128 further
-__device__ __forceinline__ uint64_t desc_16_columns(uint32_t addr) {
-    return static_cast<uint64_t>((addr & 0x3FFFFu) >> 4) | (static_cast<uint64_t>(128 >> 4) << 16) | (static_cast<uint64_t>(256 >> 4) << 32) | (1ull << 46);
 }
 // codes to bf16: 128 + c, which 128 + z is taken from
 __device__ __forceinline__ uint32_t code_plus_128(uint32_t x) {
@@ -222,7 +214,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) msa_attention_kvq_tiles_kerne
     wait_for_previous_kernel();
     release_next_kernel();
     if (warp < 3 + kTileGroups) {
-        Line<N, kTileOfKeys, 0> line;
+        Line<N, kTileOfKeys, 0, kTileStart> line;
         const bool any = line.begin(a, lane);
         if (lane == 0) walks[warp].line = line, walks[warp].more = any;
     }
@@ -251,14 +243,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) msa_attention_kvq_tiles_kerne
     if (warp < 4) {
         // ---- K ------------------------------------------------------------------------------
         const int key = tid;
-        uint32_t unit = 0;
-        float* const sums = reinterpret_cast<float*>(smem_raw + G::oSums);           // [row][16] of partial sums of x
-        #pragma unroll
-        for (int i = 0; i < 2; ++i) {                // the columns of the zero points' step that stay zero
-            const uint32_t none[8] = {};
-            tmem_store<8, 0>(tmem + G::kTmemK + i * 72 + 64 + lanes, none);
-        }
-        const Line<N, kTileOfKeys, 0>& line = walks[0].line;
+        const Line<N, kTileOfKeys, 0, kTileStart>& line = walks[0].line;
         while (next_unit(walks[0], tid == 0, 1, 128)) {
             const Seq s = line.s;
             const int P = prefix_chunks<kTileOfKeys>(s.L), from = line.from, to = line.to, held = min(to, P), h = min(line.head0, a.n_heads - 1);
@@ -281,58 +266,26 @@ __global__ void __launch_bounds__(kTileThreads, 1) msa_attention_kvq_tiles_kerne
             for (int i = 0; i < G::kStages - 1; ++i) load(from + i);
             // what lies behind the prefix comes to L2 meanwhile
             if (to > P && real) prefetch_extra(a, extra_of(a, s, line.row0, N), D, line.b, h, key, a.k_tree, a.k_spec);
-            // Query rows, 16 bytes at a time (all of a thread's on their way at once), as fp16: x = q 2^-e, e such that the block's largest
-            // |x| lies in [2^14, 2^15); dimensions that meet codes counting 16 times as much are taken as x / 16.
+            // query rows, 16 bytes at a time (all of a thread's on their way at once), swizzled
             {
                 constexpr int kItems = N * (D / 8) / 128;
                 uint4 v[kItems];
-                uint32_t top = 0u;
-                #pragma unroll
-                for (int i = 0; i < kItems; ++i) {
-                    const int item = i * 128 + tid, r = item / (D / 8), at = item - r * (D / 8), row = line.row0 + r;
-                    v[i] = make_uint4(0u, 0u, 0u, 0u);
-                    if (real && row < s.rows) v[i] = *reinterpret_cast<const uint4*>((row < s.T ? a.q_main : a.q_spec) + row_offset(a, D, line.b, h, row, s.T) + 8 * at);
-                }
-                #pragma unroll
-                for (int i = 0; i < kItems; ++i)
-                    top = __vmaxu2(top, __vmaxu2(__vmaxu2(v[i].x & 0x7fff7fffu, v[i].y & 0x7fff7fffu), __vmaxu2(v[i].z & 0x7fff7fffu, v[i].w & 0x7fff7fffu)));
-                top = __reduce_max_sync(0xffffffffu, max(top & 0xffffu, top >> 16));
-                if (lane == 0) c.q_max[quad] = top;
-                // the rows of the unit before have been read once its last S is complete
-                if (tau > 0) wait(c.s_full[(tau - 1) & 1], ((tau - 1) >> 1) & 1);
-                named_barrier(1, 128);
-                top = max(max(c.q_max[0], c.q_max[1]), max(c.q_max[2], c.q_max[3]));
-                const uint32_t eb = min(max(top >> 7, 24u), 247u) - 14u;         // (kept where 2^e and 2^-e are normal numbers)
-                const float down = __uint_as_float((254u - eb) << 23), down16 = down * 0.0625f;
-                if (tid == 0) c.factor[unit & 3] = __uint_as_float(eb << 23) * (a.scale * (1.f / kCode));
                 #pragma unroll
                 for (int i = 0; i < kItems; ++i) {
                     const int item = i * 128 + tid, r = item / (D / 8), at = item - r * (D / 8);
-                    const uint32_t u[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
-                    uint32_t h2[4];
-                    float sum = 0.f;
-                    #pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        const float x = __uint_as_float(u[q] << 16), y = __uint_as_float(u[q] & 0xffff0000u);
-                        h2[q] = pack2_f16(x * (q & 1 ? down16 : down), y * (q & 1 ? down16 : down));
-                        sum += x * down + y * down;
+                    v[i] = make_uint4(0u, 0u, 0u, 0u);
+                    if (real && line.row0 + r < s.rows) {
+                        const int row = line.row0 + r;
+                        v[i] = *reinterpret_cast<const uint4*>((row < s.T ? a.q_main : a.q_spec) + row_offset(a, D, line.b, h, row, s.T) + 8 * at);
                     }
-                    st_shared_v4(smem + G::oQ + (at >> 3) * G::kBox + r * 128 + (((at & 7) ^ (r & 7)) << 4), h2[0], h2[1], h2[2], h2[3]);
-                    sums[r * 16 + at] = sum;
                 }
-                named_barrier(1, 128);
-                // What zero points meet: -sum(x) in three fp16 terms.  z counts 2^-17 there, the terms 2^-7, as 2^-24 for codes.
-                if (tid < N) {
-                    float x = 0.f;
-                    #pragma unroll
-                    for (int i = 0; i < D / 8; ++i) x += sums[tid * 16 + i];
-                    x *= -0.0078125f;
-                    const float t0 = round_f16(x), t1 = round_f16(x - t0), t2 = (x - t0) - t1;
-                    const uint32_t row = smem + G::oZ + (tid >> 3) * 256 + (tid & 7) * 16;
-                    st_shared_v4(row, pack2_f16(t0, t1), pack2_f16(t2, 0.f), 0u, 0u);
-                    st_shared_v4(row + 128, 0u, 0u, 0u, 0u);
+                // the rows of the unit before have been read once its last S is complete
+                if (tau > 0) wait(c.s_full[(tau - 1) & 1], ((tau - 1) >> 1) & 1);
+                #pragma unroll
+                for (int i = 0; i < kItems; ++i) {
+                    const int item = i * 128 + tid, r = item / (D / 8), at = item - r * (D / 8);
+                    st_shared_v4(smem + G::oQ + (at >> 3) * G::kBox + r * 128 + (((at & 7) ^ (r & 7)) << 4), v[i].x, v[i].y, v[i].z, v[i].w);
                 }
-                ++unit;
             }
             fence_async_smem();
             #pragma unroll 1
@@ -354,62 +307,38 @@ __global__ void __launch_bounds__(kTileThreads, 1) msa_attention_kvq_tiles_kerne
                         const uint2 v = lds64(row + 32);
                         w[8] = v.x, w[9] = v.y;
                     }
-                    z = (lds32(params) >> 16 & 0xfu) << 7;
+                    z = code_plus_128(__byte_perm(lds32(params), 0u, 0x3232));
+                } else {
+                    asm volatile("st.shared.v2.u32 [%0], {%1, %1};" ::"r"(params), "r"(0x3f80u) : "memory");      // scales of 1
                 }
                 if (tau >= 2) wait(c.s_full[tau & 1], ((tau - 2) >> 1) & 1);
                 tc_fence_after();
-                const uint32_t dst = tmem + G::kTmemK + (tau & 1) * 72 + lanes;
-                if (k < held) {
-                    #pragma unroll
-                    for (int i = 0; i < G::kWords; i += 8) {
-                        uint32_t r[32];
-                        #pragma unroll
-                        for (int q = 0; q < 8; ++q) {
-                            if (i + q < G::kWords) {
-                                const uint32_t u = w[i + q] >> 8;
-                                r[4 * q] = low_codes(w[i + q]), r[4 * q + 1] = high_codes(w[i + q]), r[4 * q + 2] = low_codes(u), r[4 * q + 3] = high_codes(u);
-                            }
-                        }
-                        if (i + 8 <= G::kWords) tmem_store<32, 0>(dst + 4 * i, r);
-                        else tmem_store<8, 0>(dst + 4 * i, r);       // (80: the last two words)
-                    }
-                } else {
-                    // bf16 keys as fp16: k 2^-f with the largest in [2^10, 2^11), dimensions in the codes' manner; the scale is 2^(f - 24)
-                    const __nv_bfloat16* src = nullptr;
-                    if (real) {
-                        const Extra x = extra_of(a, s, line.row0, N);
-                        const int e = (k - P) * kTileOfKeys + key;
-                        if (e < x.count) src = (e < x.T ? a.k_tree : a.k_spec) + extra_offset(a, x, D, line.b, h, e);
-                    }
-                    uint32_t top = 0u;
-                    #pragma unroll 8
-                    for (int i = 0; i < G::kWords; ++i) {
-                        uint4 v = {};
-                        if (src) v = *reinterpret_cast<const uint4*>(src + 8 * i);
-                        top = __vmaxu2(top, __vmaxu2(__vmaxu2(v.x & 0x7fff7fffu, v.y & 0x7fff7fffu), __vmaxu2(v.z & 0x7fff7fffu, v.w & 0x7fff7fffu)));
-                    }
-                    const uint32_t fb = min(max(max(top & 0xffffu, top >> 16) >> 7, 60u), 250u) - 10u;
-                    const float down = __uint_as_float((254u - fb) << 23);
-                    const uint32_t scale = (fb - 24u) << 7;          // (a bf16 pattern)
-                    asm volatile("st.shared.v2.u32 [%0], {%1, %2};" ::"r"(params), "r"(scale), "r"(0x3f80u) : "memory");
-                    #pragma unroll
-                    for (int i = 0; i < G::kWords; i += 2) {
-                        uint32_t r[8];
-                        #pragma unroll
-                        for (int q = 0; q < 2; ++q) {
-                            uint4 v = {};
-                            if (src) v = *reinterpret_cast<const uint4*>(src + 8 * (i + q));
-                            const uint32_t u[4] = {v.x, v.y, v.z, v.w};
-                            #pragma unroll
-                            for (int n = 0; n < 4; ++n) {
-                                const float f = n & 1 ? down * 16.f : down;
-                                r[4 * q + n] = pack2_f16(__uint_as_float(u[n] << 16) * f, __uint_as_float(u[n] & 0xffff0000u) * f);
-                            }
-                        }
-                        tmem_store<8, 0>(dst + 4 * i, r);
-                    }
+                const uint32_t dst = tmem + G::kTmemK + (tau & 1) * 64 + lanes;
+                const __nv_bfloat16* src = nullptr;
+                if (k >= held && real) {
+                    const Extra x = extra_of(a, s, line.row0, N);
+                    const int e = (k - P) * kTileOfKeys + key;
+                    if (e < x.count) src = (e < x.T ? a.k_tree : a.k_spec) + extra_offset(a, x, D, line.b, h, e);
                 }
-                tmem_store2(dst + 64, z | z << 16, z);
+                #pragma unroll
+                for (int i = 0; i < G::kWords; i += 8) {
+                    uint32_t r[32];
+                    #pragma unroll
+                    for (int q = 0; q < 8; ++q) {
+                        if (i + q < G::kWords) {
+                            if (k < held) {
+                                #pragma unroll
+                                for (int n = 0; n < 4; ++n) r[4 * q + n] = sub_bf16x2(code_plus_128(w[i + q] >> (4 * n)), z);
+                            } else {
+                                uint4 v = {};
+                                if (src) v = *reinterpret_cast<const uint4*>(src + 8 * (i + q));
+                                r[4 * q] = v.x, r[4 * q + 1] = v.y, r[4 * q + 2] = v.z, r[4 * q + 3] = v.w;
+                            }
+                        }
+                    }
+                    if (i + 8 <= G::kWords) tmem_store<32, 0>(dst + 4 * i, r);
+                    else tmem_store<8, 0>(dst + 4 * i, r);           // (80: the last two words)
+                }
                 tmem_wait_st();
                 tc_fence_before();
                 mbar_arrive(smem_u32(&c.k_full[tau & 1]));
@@ -423,7 +352,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) msa_attention_kvq_tiles_kerne
         // keys in the order in which the columns of V^T follow one another: transposed byte 4 q + e of 16 keys goes to column q (e < 2) or
         // 4 + q, which hold keys 2 q, 2 q + 1 and 8 + 2 q, 8 + 2 q + 1
         const int from16 = (lane & 3) < 2 ? 2 * ((lane & 15) >> 2) + (lane & 3) : 8 + 2 * ((lane & 15) >> 2) + (lane & 3) - 2;
-        const Line<N, kTileOfKeys, 0>& line = walks[1].line;
+        const Line<N, kTileOfKeys, 0, kTileStart>& line = walks[1].line;
         while (next_unit(walks[1], t == 0, 2, 128)) {            // (the ring's last stage has been read by all)
             const Seq s = line.s;
             const int P = prefix_chunks<kTileOfKeys>(s.L), from = line.from, to = line.to, held = min(to, P), h = min(line.head0, a.n_heads - 1);
@@ -465,12 +394,12 @@ __global__ void __launch_bounds__(kTileThreads, 1) msa_attention_kvq_tiles_kerne
                                 load_transposed_bytes(codes + row * G::kPitch + place * 16, r0, r1);
                                 const uint2 p0 = lds64(words + 4 * key0), p1 = lds64(words + 4 * key0 + 32);
                                 const uint32_t z0 = code_plus_128(__byte_perm(p0.x, p0.y, 0x7632)), z1 = code_plus_128(__byte_perm(p1.x, p1.y, 0x7632));
-                                const uint32_t e0 = __byte_perm(r0, 0u, 0x4140), e1 = __byte_perm(r0, 0u, 0x4342);
-                                const uint32_t f0 = __byte_perm(r1, 0u, 0x4140), f1 = __byte_perm(r1, 0u, 0x4342);
-                                lo[4 * i] = sub_bf16x2(code_plus_128(e0), z0), lo[4 * i + 1] = sub_bf16x2(code_plus_128(f0), z0);
-                                lo[4 * i + 2] = sub_bf16x2(code_plus_128(e1), z1), lo[4 * i + 3] = sub_bf16x2(code_plus_128(f1), z1);
-                                hi[4 * i] = sub_bf16x2(code_plus_128(e0 >> 4), z0), hi[4 * i + 1] = sub_bf16x2(code_plus_128(f0 >> 4), z0);
-                                hi[4 * i + 2] = sub_bf16x2(code_plus_128(e1 >> 4), z1), hi[4 * i + 3] = sub_bf16x2(code_plus_128(f1 >> 4), z1);
+                                // a byte's low or high code beside 0x43: 128 + c in bf16
+                                const auto pair = [](uint32_t x, uint32_t sel) { return __byte_perm(x & 0x0f0f0f0fu, 0x43434343u, sel); };
+                                lo[4 * i] = sub_bf16x2(pair(r0, 0x4140), z0), lo[4 * i + 1] = sub_bf16x2(pair(r1, 0x4140), z0);
+                                lo[4 * i + 2] = sub_bf16x2(pair(r0, 0x4342), z1), lo[4 * i + 3] = sub_bf16x2(pair(r1, 0x4342), z1);
+                                hi[4 * i] = sub_bf16x2(pair(r0 >> 4, 0x4140), z0), hi[4 * i + 1] = sub_bf16x2(pair(r1 >> 4, 0x4140), z0);
+                                hi[4 * i + 2] = sub_bf16x2(pair(r0 >> 4, 0x4342), z1), hi[4 * i + 3] = sub_bf16x2(pair(r1 >> 4, 0x4342), z1);
                             }
                             tmem_store_lanes16(dst + 32 * half, lo);
                             tmem_store_lanes16(dst + 32 * half + (16u << 16), hi);
@@ -555,7 +484,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) msa_attention_kvq_tiles_kerne
         const uint32_t weights = smem + G::oP + key * 128;        // the key's row of P^T
         // TMEM lane to dimension
         const int byte = 16 * quad + (lane & 15), dim = 8 * (byte >> 2) + ((byte & 1) << 2) + ((byte >> 1) & 1) + ((lane >> 4) << 1);
-        const Line<N, kTileOfKeys, 0>& line = walks[2 + group].line;
+        const Line<N, kTileOfKeys, 0, kTileStart>& line = walks[2 + group].line;
         while (next_unit(walks[2 + group], key == 0, bar, 128)) {
             const Seq& s = line.s;
             const int L = s.L, P = prefix_chunks<kTileOfKeys>(L), from = line.from, to = line.to;
@@ -592,12 +521,12 @@ __global__ void __launch_bounds__(kTileThreads, 1) msa_attention_kvq_tiles_kerne
                 wait(c.s_full[tau & 1], parity);
                 tc_fence_after();
                 const uint2 params = lds64(smem + G::oKParams + ((tau % G::kParams) * kTileOfKeys + key) * 8);
-                const float sk = scale_of(params.x) * c.factor[unit & 3], sv = scale_of(params.y);
+                const float sk = scale_of(params.x) * a.scale, sv = scale_of(params.y);
                 // rows that see the key: all of them if it is a cached one; else those of its node's descendants; of a stream key, from its
                 // own row to its node's last
                 uint32_t vis = all;
                 if (k < P) {
-                    if ((k + 1) * kTileOfKeys > L && k * kTileOfKeys + key >= L) vis = 0u;
+                    if (k * kTileOfKeys + key >= L) vis = 0u;
                 } else {
                     const int e = (k - P) * kTileOfKeys + key;
                     vis = 0u;
@@ -608,7 +537,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) msa_attention_kvq_tiles_kerne
                         if (first < C && last >= 0) vis = (0xffffffffu >> (31 - min(last, 31))) & (0xffffffffu << max(first, 0));
                     }
                 }
-                const bool masked = (k + 1) * kTileOfKeys > L;
+                const bool masked = __any_sync(0xffffffffu, (vis & all) != all);
                 float d[C];
                 // scores above their references, in log2 units; -inf where the row does not see the key
                 const auto scores = [&]() {
@@ -815,8 +744,8 @@ __global__ void __launch_bounds__(kTileThreads, 1) msa_attention_kvq_tiles_kerne
     } else {
         // ---- MMAs ---------------------------------------------------------------------------
         const uint32_t base = uniform(smem);
-        const uint64_t dq = desc_k_major(base + G::oQ), dz = desc_16_columns(base + G::oZ), dp = desc_mn_major(base + G::oP, 0);
-        const Line<N, kTileOfKeys, 0>& line = walks[2 + kTileGroups].line;
+        const uint64_t dq = desc_k_major(base + G::oQ), dp = desc_mn_major(base + G::oP, 0);
+        const Line<N, kTileOfKeys, 0, kTileStart>& line = walks[2 + kTileGroups].line;
         uint32_t unit = 0;
         const auto product = [&](uint32_t t, bool first) {       // O^T (+)= V^T P^T of tile t
             if (first && unit > 0) wait(c.o_free, (unit - 1) & 1);
@@ -836,11 +765,10 @@ __global__ void __launch_bounds__(kTileThreads, 1) msa_attention_kvq_tiles_kerne
                 wait(c.k_full[tau & 1], (tau >> 1) & 1);
                 if (tau >= 2) wait(c.s_free[tau & 1], ((tau - 2) >> 1) & 1);
                 tc_fence_after();
-                const uint32_t ka = tmem + G::kTmemK + (tau & 1) * 72, sd = tmem + G::kTmemS + (tau & 1) * N;
+                const uint32_t ka = tmem + G::kTmemK + (tau & 1) * 64, sd = tmem + G::kTmemS + (tau & 1) * N;
                 tile_mma<4>(sd, ka, dq, G::kIdescS, 0u);
                 if constexpr (D == 128) tile_mma<4>(sd, ka + 32, dq + (G::kBox >> 4), G::kIdescS, 1u);
                 if constexpr (D == 80) tile_mma<1>(sd, ka + 32, dq + (G::kBox >> 4), G::kIdescS, 1u);
-                tile_mma<1>(sd, ka + 64, dz, G::kIdescS, 1u);
                 tc_commit_e(smem_u32(&c.s_full[tau & 1]));
                 if (lane == 0) mbar_arrive(smem_u32(&c.s_full[tau & 1]));            // (passes on what the K warps have written: the keys' scales)
                 if (i > 0) product(tau - 1, i == 1);
