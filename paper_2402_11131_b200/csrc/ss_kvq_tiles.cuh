@@ -2,23 +2,26 @@
 //
 // S^T = K Q^T and O^T = V^T P^T with 128 keys (dimensions) as the 128 lanes of TMEM and the N <= 64 query rows as columns: what
 // grows with the rows is the cheap side, and codes go from registers to TMEM as A operands, never through shared memory.
-//   K: the thread of a key turns the key's codes into bf16 c - z (exact), one TMEM lane; its scale multiplies the lane's scores.
+//   K: the thread of a key turns the key's codes into bf16 128 + c (a mask and an or), one TMEM lane; one more step of the product, whose
+//      operands are 128 + z and -sum(q) in three bf16 terms, leaves sum q (c - z); the key's scale multiplies the lane's scores.
 //   V: transposing loads (ldmatrix, 16 keys by 16 bytes) give a thread four keys' codes of two dimensions; a TMEM lane is a dimension.
 //      The scale is part of the weight that meets it.
 // Lane 32 w + x of V^T and O^T (w < D / 32) holds, for x < 16, the low codes of byte 16 w + x of a row, else the high codes of
 // byte 16 w + x - 16.
 //
-// 25 warps: 0..3 K, 4..7 V, 8..23 softmax (four groups of four, each a quarter of the rows, thread = key), 24 issues the MMAs.  Two
-// buffers each for K, V, S and P, so that the five work on different tiles.  Nothing but the order of tiles is shared: every role
-// walks the same list of units.
+// 26 warps: 0..3 copy the codes of K and V and turn K's into operands, 4..7 V's, 8..23 softmax (four groups of four, each a quarter of
+// the rows, thread = key), 24 issues the MMAs, 25..27 prepare: they walk the list of units one ahead of the others, who find a
+// unit's query rows and what else they need to know of it in shared memory.  Two buffers each for K, V, S, P and the query rows, so that
+// the roles work on different tiles and units.
 #pragma once
 #include "ss_tcgen05.cuh"
 
 namespace ss {
 
-// A unit's start and end take as long as some five tiles.
-constexpr int kTileStart = 5;
-constexpr int kTileOfKeys = 128, kTileGroups = 4, kTileSoftmax = 128 * kTileGroups, kTileThreads = 256 + kTileSoftmax + 32;
+// A unit's start and end take as long as some four tiles.
+constexpr int kTileStart = 4;
+constexpr int kTileOfKeys = 128, kTileGroups = 4, kTileSoftmax = 128 * kTileGroups, kTilePrepare = 96, kTileThreads = 256 + kTileSoftmax + 32 + kTilePrepare;
+constexpr int kTileWarpsOfUnit = (kTileThreads - kTilePrepare) / 32;             // that use a unit's plan
 
 template <int D, int N>
 struct TileGeo {
@@ -26,28 +29,32 @@ struct TileGeo {
     static constexpr int kPitch = D == 128 ? 64 : D == 80 ? 48 : 32;         // bytes of a key's codes in shared memory (16-byte aligned)
     static constexpr int kCopy = D == 80 ? 8 : 16, kPer = D / 2 / kCopy;     // asynchronous copies per key
     static constexpr int kWords = D / 8;
-    static constexpr int kColumns = D / 2;                        // TMEM columns of a K tile
-    static constexpr int kQuads = (D + 31) / 32;                  // warps that have V lanes
+        static constexpr int kQuads = (D + 31) / 32;                  // warps that have V lanes
     static constexpr int kCodes = kTileOfKeys * kPitch;
-    static constexpr int kStages = 3, kParams = 8;
+    static constexpr int kStages = 4, kParams = 8;
     static constexpr int kBoxes = D > 64 ? 2 : 1, kBox = N * 128;
     static constexpr int kRowOfV = 64 * kQuads;                   // bytes of a bf16 row in lane order
     static constexpr int kP = kTileOfKeys * 128;
-    static constexpr int oP = 0, oQ = oP + 2 * kP, oK = oQ + kBoxes * kBox, oV = oK + kStages * kCodes;
-    static constexpr int oKParams = oV + kStages * kCodes, oVParams = oKParams + kParams * kTileOfKeys * 8;
-    static constexpr int kBytes = oVParams + kStages * kTileOfKeys * 4;
-    static_assert(64 * kRowOfV <= kStages * kCodes, "half a tile of bf16 values takes the place of the ring");
-    static constexpr uint32_t kTmemK = 0, kTmemV = 128, kTmemS = 256, kTmemO = 256 + 2 * N;
-    static constexpr uint32_t kIdesc = (1u << 4) | (1u << 7) | (1u << 10) | (static_cast<uint32_t>(N >> 3) << 17) | ((128u >> 4) << 24);
-    static constexpr uint32_t kIdescS = kIdesc, kIdescPV = kIdesc | (1u << 16);
+    static constexpr int oP = 0, oQ = oP + 2 * kP, oZ = oQ + kBoxes * kBox, kRowsOfUnit = kBoxes * kBox + N * 32, oSums = oQ + 2 * kRowsOfUnit, oK = oSums + N * 64, oV = oK + kStages * kCodes;
+    static constexpr int oRows = oV + kStages * kCodes;           // 64 rows of bf16 values in the order of the lanes
+    static constexpr int oKParams = oRows + 64 * kRowOfV, oVParams = oKParams + kParams * kTileOfKeys * 4;
+    static constexpr int kBytes = oVParams + kParams * kTileOfKeys * 4;
+    static constexpr uint32_t kTmemK = 0, kTmemV = 144, kTmemS = 272, kTmemO = 272 + 2 * N;          // K: 72 columns a buffer, the last 8 for zero points
+    // bf16 operands, fp32 sums, 128 lanes, N columns; P^T is MN-major
+    static constexpr uint32_t kIdescS = (1u << 4) | (1u << 7) | (1u << 10) | (static_cast<uint32_t>(N >> 3) << 17) | ((128u >> 4) << 24);
+    static constexpr uint32_t kIdescPV = kIdescS | (1u << 16);
 };
 
-// A role's place in the list of units: the role's first thread goes on, the others read.  In shared memory, since it is used between
-// units only and would cost every thread some 40 registers.
-template <int N>
-struct TileWalk {
-    Line<N, kTileOfKeys, 0, kTileStart> line;
-    int more;
+// What the roles have to know of a unit
+struct TileUnit {
+    int L, T, prefix, from, to;                      // of the sequence; tiles of cached slots, and those of this piece
+    int head, real, row0, rows, b;                   // real: there is such a head; rows: of the block
+    int whole, first, last, second, me, member, team;            // see Pieces
+    int done;                                        // no unit: the list is at its end
+    long long start;
+    Extra extra;
+    long long out[64];                               // where a row's output goes (element offset)
+    unsigned long long see[64];                      // per node: the rows that see it
 };
 
 // Asynchronous copies of a tile's codes by 128 threads, 16 (8) bytes each, from a pointer that walks along with the tiles.  Slots behind
@@ -56,29 +63,32 @@ template <int D, int N>
 struct TileLoader {
     using G = TileGeo<D, N>;
     static constexpr bool kEven = 128 % G::kPer == 0;
-    const unsigned char* at;                         // of the next tile: the thread's first copy (80: key 0)
+    long long at;                                    // of the next tile: the thread's first copy (80: key 0), in either array of codes
     int left;                                        // slots from there on
-    __device__ __forceinline__ TileLoader(const KvqArgs& a, const Seq& s, int h, int tile, int t, const unsigned char* codes) {
-        const long long slot = s.start + static_cast<long long>(tile) * kTileOfKeys + (kEven ? t / G::kPer : 0);
-        at = codes + slot * a.slot_stride + h * a.head_stride + (kEven ? t % G::kPer * G::kCopy : 0);
-        left = s.L - tile * kTileOfKeys;
+    __device__ __forceinline__ TileLoader(const KvqArgs& a, const TileUnit& u, int tile, int t) {
+        const long long slot = u.start + static_cast<long long>(tile) * kTileOfKeys + (kEven ? t / G::kPer : 0);
+        at = slot * a.slot_stride + u.head * a.head_stride + (kEven ? t % G::kPer * G::kCopy : 0);
+        left = u.L - tile * kTileOfKeys;
     }
     __device__ __forceinline__ uint32_t place(int row, int column) const {
         return row * G::kPitch + (D == 128 ? column ^ ((row >> 1) & 3) : D == 64 ? column ^ ((row >> 2) & 1) : column) * G::kCopy;
     }
-    __device__ __forceinline__ void next(const KvqArgs& a, uint32_t stage, int t) {
+    __device__ __forceinline__ void next(const KvqArgs& a, uint32_t k_stage, uint32_t v_stage, int t) {
         if (kEven && left >= kTileOfKeys) {
             // (the swizzle is the same for all of the thread's rows: they are a multiple of 8 apart)
-            const uint32_t dst = stage + place(t / G::kPer, t % G::kPer);
+            const uint32_t dst = place(t / G::kPer, t % G::kPer);
             #pragma unroll
-            for (int i = 0; i < G::kPer; ++i)
-                copy_async<G::kCopy>(dst + i * (128 / G::kPer) * G::kPitch, at + i * (128 / G::kPer) * a.slot_stride);
+            for (int i = 0; i < G::kPer; ++i) copy_async<G::kCopy>(k_stage + dst + i * (128 / G::kPer) * G::kPitch, a.k_codes + at + i * (128 / G::kPer) * a.slot_stride);
+            #pragma unroll
+            for (int i = 0; i < G::kPer; ++i) copy_async<G::kCopy>(v_stage + dst + i * (128 / G::kPer) * G::kPitch, a.v_codes + at + i * (128 / G::kPer) * a.slot_stride);
         } else {
             const int last = left - 1;
             #pragma unroll 1
             for (int i = 0; i < G::kPer; ++i) {
                 const int item = i * 128 + t, row = item / G::kPer, column = item - row * G::kPer;
-                copy_async<G::kCopy>(stage + place(row, column), at + (kEven ? (min(row, last) - t / G::kPer) * a.slot_stride : min(row, last) * a.slot_stride + column * G::kCopy));
+                const long long from = at + (kEven ? (min(row, last) - t / G::kPer) * a.slot_stride : min(row, last) * a.slot_stride + column * G::kCopy);
+                copy_async<G::kCopy>(k_stage + place(row, column), a.k_codes + from);
+                copy_async<G::kCopy>(v_stage + place(row, column), a.v_codes + from);
             }
         }
         at += kTileOfKeys * a.slot_stride;
@@ -89,16 +99,16 @@ struct TileLoader {
 template <int C>
 struct TileCtrl {
     unsigned long long k_full[2], s_full[2], s_free[2], v_full[2], p_full[2], pv_done[2], o_free, drain;
-    uint32_t see[kTileGroups][64];                                          // per group and node: the rows that see it
-    long long out[64];                                            // where a row's output goes (element offset)
+    unsigned long long codes_full[4], codes_free[4];              // V's codes
+    unsigned long long plan_full[2], rows_full[2], plan_free[2];
+    unsigned long long vote[kTileGroups][2];                      // the warps of a group have looked at their scores
+    TileUnit unit[2];
     float neg_ref[64];
     int tile_max[kTileGroups][4][C];
     float sums[kTileGroups][4][C];
-    unsigned long long vote[kTileGroups][2];                      // the warps of a group have looked at their scores; a reference has to go up
-    int hot[kTileGroups][2];
-    int first[kTileGroups], last[kTileGroups], second[kTileGroups];          // the unit's pieces
+    int hot[kTileGroups][2];                                      // a reference has to go up
     uint32_t tmem;
-    int abort, joined;
+    int abort, joined, any;
 };
 
 __device__ __forceinline__ void tile_wait(uint32_t bar, uint32_t parity, int* abort, int* status) {
@@ -152,6 +162,14 @@ __device__ __forceinline__ void load_transposed_bytes(uint32_t addr, uint32_t& r
 __device__ __forceinline__ void load_transposed_halves(uint32_t addr, uint32_t (&r)[4]) {
     asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
 }
+// two columns
+__device__ __forceinline__ void tmem_store2(uint32_t addr, uint32_t x, uint32_t y) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x2.b32 [%0], {%1, %2};" ::"r"(addr), "r"(x), "r"(y) : "memory");
+}
+// K-major operand of 16 columns without a swizzle: 8 rows by 16 bytes are 128 bytes in a row, the second 16 bytes of the rows 128 further
+__device__ __forceinline__ uint64_t desc_16_columns(uint32_t addr) {
+    return static_cast<uint64_t>((addr & 0x3FFFFu) >> 4) | (static_cast<uint64_t>(128 >> 4) << 16) | (static_cast<uint64_t>(256 >> 4) << 32) | (1ull << 46);
+}
 // codes to bf16: 128 + c, which 128 + z is taken from
 __device__ __forceinline__ uint32_t code_plus_128(uint32_t x) {
     uint32_t r;
@@ -196,31 +214,32 @@ __global__ void __launch_bounds__(kTileThreads, 1) msa_attention_kvq_tiles_kerne
     constexpr int C = G::kRowsOfGroup;
     extern __shared__ __align__(1024) unsigned char smem_raw[];
     __shared__ __align__(16) TileCtrl<C> c;
-    __shared__ __align__(16) TileWalk<N> walks[3 + kTileGroups];    // K, V, softmax groups, MMAs
     const int tid = threadIdx.x, lane = tid & 31, warp = static_cast<int>(uniform(tid >> 5)), quad = warp & 3;
     const uint32_t smem = smem_u32(smem_raw);
     int* const status = reinterpret_cast<int*>(a.ws);
+    constexpr int kMmaWarp = kTileWarpsOfUnit - 1, kPlanWarp = kMmaWarp + 1;
     if (tid == 0) {
         c.abort = 0;
         for (int i = 0; i < 2; ++i) {
             mbar_init(smem_u32(&c.k_full[i]), 128), mbar_init(smem_u32(&c.v_full[i]), 128);
             mbar_init(smem_u32(&c.s_free[i]), kTileSoftmax), mbar_init(smem_u32(&c.p_full[i]), kTileSoftmax);
             mbar_init(smem_u32(&c.s_full[i]), 2), mbar_init(smem_u32(&c.pv_done[i]), 1);
+            mbar_init(smem_u32(&c.plan_full[i]), 1), mbar_init(smem_u32(&c.rows_full[i]), 1), mbar_init(smem_u32(&c.plan_free[i]), kTileWarpsOfUnit);
         }
+        for (int i = 0; i < G::kStages; ++i) mbar_init(smem_u32(&c.codes_full[i]), 128), mbar_init(smem_u32(&c.codes_free[i]), 128);
         for (int i = 0; i < 2 * kTileGroups; ++i) mbar_init(smem_u32(&c.vote[i >> 1][i & 1]), 4), c.hot[i >> 1][i & 1] = 0;
         mbar_init(smem_u32(&c.o_free), kTileSoftmax), mbar_init(smem_u32(&c.drain), 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     wait_for_previous_kernel();
     release_next_kernel();
-    if (warp < 3 + kTileGroups) {
-        Line<N, kTileOfKeys, 0, kTileStart> line;
+    Line<N, kTileOfKeys, 0, kTileStart> line;                    // (the planning warp's)
+    if (warp == kPlanWarp) {
         const bool any = line.begin(a, lane);
-        if (lane == 0) walks[warp].line = line, walks[warp].more = any;
+        if (lane == 0) c.any = any;
     }
     __syncthreads();
-    if (walks[0].more == 0) return;
-    constexpr int kMmaWarp = kTileThreads / 32 - 1;
+    if (c.any == 0) return;
     if (warp == kMmaWarp) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&c.tmem)) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
@@ -231,73 +250,62 @@ __global__ void __launch_bounds__(kTileThreads, 1) msa_attention_kvq_tiles_kerne
     const uint32_t tmem = uniform(c.tmem), lanes = static_cast<uint32_t>(32 * quad) << 16;
     // (a wait that runs out leaves the roles in step: everyone goes through the same tiles without waiting, and no output is written)
     const auto wait = [&](unsigned long long& bar, uint32_t parity) { tile_wait(smem_u32(&bar), parity, &c.abort, status); };
-    // on to the next unit, all `threads` threads of a role together; id: their barrier
-    const auto next_unit = [&](TileWalk<N>& w, bool leader, int id, int threads) {
-        if (threads > 32) named_barrier(id, threads); else __syncwarp();
-        if (leader) w.more = w.line.next(a);
-        if (threads > 32) named_barrier(id, threads); else __syncwarp();
-        return w.more != 0;
+    // units one after another: the plan of unit n, and back to the planning warp when a warp is done with it
+    const auto plan_of = [&](uint32_t n) -> const TileUnit& {
+        wait(c.plan_full[n & 1], (n >> 1) & 1);
+        return c.unit[n & 1];
+    };
+    const auto plan_used = [&](uint32_t n) {
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&c.plan_free[n & 1]));
     };
     uint32_t tau = 0;                                // tiles so far, over all units: buffer tau & 1, phase (tau >> 1) & 1
 
     if (warp < 4) {
         // ---- K ------------------------------------------------------------------------------
         const int key = tid;
-        const Line<N, kTileOfKeys, 0, kTileStart>& line = walks[0].line;
-        while (next_unit(walks[0], tid == 0, 1, 128)) {
-            const Seq s = line.s;
-            const int P = prefix_chunks<kTileOfKeys>(s.L), from = line.from, to = line.to, held = min(to, P), h = min(line.head0, a.n_heads - 1);
-            const bool real = line.head0 < a.n_heads;
-            // (the ring's last stage has been read by all)
-            const uint32_t tau0 = tau;
-            TileLoader<D, N> loader(a, s, h, from, tid, a.k_codes);
-            const long long words = (s.start + static_cast<long long>(from) * kTileOfKeys) * a.p_slot + h * a.p_head;
+        uint32_t unit = 0, copied = 0;               // units; tiles of codes copied or on their way
+        #pragma unroll
+        for (int i = 0; i < 2; ++i) {                // the columns of the zero points' step that stay zero
+            const uint32_t none[8] = {};
+            tmem_store<8, 0>(tmem + G::kTmemK + i * 72 + 64 + lanes, none);
+        }
+        for (;; ++unit) {
+            const TileUnit& u = plan_of(unit);
+            if (u.done) break;
+            const int from = u.from, to = u.to, held = min(to, u.prefix);
+            const bool real = u.real;
+            const uint32_t tau0 = tau, copied0 = copied;
+            TileLoader<D, N> loader(a, u, from, tid);
+            const uint32_t* words = a.k_params + (u.start + static_cast<long long>(from) * kTileOfKeys) * a.p_slot + u.head * a.p_head;
+            const long long v_words = a.v_params - a.k_params;
+            named_barrier(1, 128);                   // (the ring's last stage has been read by all)
             const auto load = [&](int k) {           // codes, scales and zero points of tile k
                 if (k < held) {
-                    loader.next(a, smem + G::oK + ((k - from) % G::kStages) * G::kCodes, tid);
-                    const long long p = words + (static_cast<long long>(k - from) * kTileOfKeys + min(key, s.L - 1 - k * kTileOfKeys)) * a.p_slot;
-                    const uint32_t dst = smem + G::oKParams + (((tau0 + (k - from)) % G::kParams) * kTileOfKeys + key) * 8;
-                    copy_async<4>(dst, a.k_params + p);
-                    copy_async<4>(dst + 4, a.v_params + p);
+                    const uint32_t n = copied0 + (k - from), stage = n % G::kStages;
+                    if (n >= G::kStages) wait(c.codes_free[stage], ((n - G::kStages) / G::kStages) & 1);
+                    loader.next(a, smem + G::oK + stage * G::kCodes, smem + G::oV + stage * G::kCodes, tid);
+                    const long long p = (static_cast<long long>(k - from) * kTileOfKeys + min(key, u.L - 1 - k * kTileOfKeys)) * a.p_slot;
+                    const uint32_t dst = (((tau0 + (k - from)) % G::kParams) * kTileOfKeys + key) * 4;
+                    copy_async<4>(smem + G::oKParams + dst, words + p);
+                    copy_async<4>(smem + G::oVParams + dst, words + v_words + p);
+                    asm volatile("cp.async.mbarrier.arrive.noinc.shared.b64 [%0];" ::"r"(smem_u32(&c.codes_full[stage])) : "memory");
                 }
                 copy_commit();
             };
             #pragma unroll 1
             for (int i = 0; i < G::kStages - 1; ++i) load(from + i);
-            // what lies behind the prefix comes to L2 meanwhile
-            if (to > P && real) prefetch_extra(a, extra_of(a, s, line.row0, N), D, line.b, h, key, a.k_tree, a.k_spec);
-            // query rows, 16 bytes at a time (all of a thread's on their way at once), swizzled
-            {
-                constexpr int kItems = N * (D / 8) / 128;
-                uint4 v[kItems];
-                #pragma unroll
-                for (int i = 0; i < kItems; ++i) {
-                    const int item = i * 128 + tid, r = item / (D / 8), at = item - r * (D / 8);
-                    v[i] = make_uint4(0u, 0u, 0u, 0u);
-                    if (real && line.row0 + r < s.rows) {
-                        const int row = line.row0 + r;
-                        v[i] = *reinterpret_cast<const uint4*>((row < s.T ? a.q_main : a.q_spec) + row_offset(a, D, line.b, h, row, s.T) + 8 * at);
-                    }
-                }
-                // the rows of the unit before have been read once its last S is complete
-                if (tau > 0) wait(c.s_full[(tau - 1) & 1], ((tau - 1) >> 1) & 1);
-                #pragma unroll
-                for (int i = 0; i < kItems; ++i) {
-                    const int item = i * 128 + tid, r = item / (D / 8), at = item - r * (D / 8);
-                    st_shared_v4(smem + G::oQ + (at >> 3) * G::kBox + r * 128 + (((at & 7) ^ (r & 7)) << 4), v[i].x, v[i].y, v[i].z, v[i].w);
-                }
-            }
-            fence_async_smem();
             #pragma unroll 1
             for (int k = from; k < to; ++k, ++tau) {
                 uint32_t w[G::kWords];
                 uint32_t z = 0u;
-                const uint32_t params = smem + G::oKParams + ((tau % G::kParams) * kTileOfKeys + key) * 8;
+                const uint32_t params = ((tau % G::kParams) * kTileOfKeys + key) * 4;
                 if (k < held) {
                     copy_wait<G::kStages - 2>();
                     named_barrier(1, 128);
                     load(k + G::kStages - 1);
-                    const uint32_t row = smem + G::oK + ((k - from) % G::kStages) * G::kCodes + key * G::kPitch;
+                    const uint32_t row = smem + G::oK + (copied % G::kStages) * G::kCodes + key * G::kPitch;
+                    ++copied;
                     #pragma unroll
                     for (int i = 0; i < G::kWords / 4; ++i) {
                         const uint4 v = lds128(row + 16 * (D == 128 ? i ^ ((key >> 1) & 3) : D == 64 ? i ^ ((key >> 2) & 1) : i));
@@ -307,44 +315,54 @@ __global__ void __launch_bounds__(kTileThreads, 1) msa_attention_kvq_tiles_kerne
                         const uint2 v = lds64(row + 32);
                         w[8] = v.x, w[9] = v.y;
                     }
-                    z = code_plus_128(__byte_perm(lds32(params), 0u, 0x3232));
-                } else {
-                    asm volatile("st.shared.v2.u32 [%0], {%1, %1};" ::"r"(params), "r"(0x3f80u) : "memory");      // scales of 1
+                    z = code_plus_128(__byte_perm(lds32(smem + G::oKParams + params), 0u, 0x3232));
                 }
                 if (tau >= 2) wait(c.s_full[tau & 1], ((tau - 2) >> 1) & 1);
                 tc_fence_after();
-                const uint32_t dst = tmem + G::kTmemK + (tau & 1) * 64 + lanes;
-                const __nv_bfloat16* src = nullptr;
-                if (k >= held && real) {
-                    const Extra x = extra_of(a, s, line.row0, N);
-                    const int e = (k - P) * kTileOfKeys + key;
-                    if (e < x.count) src = (e < x.T ? a.k_tree : a.k_spec) + extra_offset(a, x, D, line.b, h, e);
-                }
-                #pragma unroll
-                for (int i = 0; i < G::kWords; i += 8) {
-                    uint32_t r[32];
+                const uint32_t dst = tmem + G::kTmemK + (tau & 1) * 72 + lanes;
+                if (k < held) {
                     #pragma unroll
-                    for (int q = 0; q < 8; ++q) {
-                        if (i + q < G::kWords) {
-                            if (k < held) {
+                    for (int i = 0; i < G::kWords; i += 8) {
+                        uint32_t r[32];
+                        #pragma unroll
+                        for (int q = 0; q < 8; ++q) {
+                            if (i + q < G::kWords) {
                                 #pragma unroll
-                                for (int n = 0; n < 4; ++n) r[4 * q + n] = sub_bf16x2(code_plus_128(w[i + q] >> (4 * n)), z);
-                            } else {
-                                uint4 v = {};
-                                if (src) v = *reinterpret_cast<const uint4*>(src + 8 * (i + q));
-                                r[4 * q] = v.x, r[4 * q + 1] = v.y, r[4 * q + 2] = v.z, r[4 * q + 3] = v.w;
+                                for (int n = 0; n < 4; ++n) r[4 * q + n] = code_plus_128(w[i + q] >> (4 * n));
                             }
                         }
+                        if (i + 8 <= G::kWords) tmem_store<32, 0>(dst + 4 * i, r);
+                        else tmem_store<8, 0>(dst + 4 * i, r);       // (80: the last two words)
                     }
-                    if (i + 8 <= G::kWords) tmem_store<32, 0>(dst + 4 * i, r);
-                    else tmem_store<8, 0>(dst + 4 * i, r);           // (80: the last two words)
+                } else {
+                    const __nv_bfloat16* src = nullptr;
+                    if (real) {
+                        const int e = (k - u.prefix) * kTileOfKeys + key;
+                        if (e < u.extra.count) src = (e < u.T ? a.k_tree : a.k_spec) + extra_offset(a, u.extra, D, u.b, u.head, e);
+                    }
+                    asm volatile("st.shared.u32 [%0], %1;" ::"r"(smem + G::oKParams + params), "r"(0x3f80u) : "memory");      // scales of 1
+                    asm volatile("st.shared.u32 [%0], %1;" ::"r"(smem + G::oVParams + params), "r"(0x3f80u) : "memory");
+                    #pragma unroll
+                    for (int i = 0; i < G::kWords; i += 8) {
+                        uint32_t r[32];
+                        #pragma unroll
+                        for (int q = 0; q < 8; ++q) {
+                            uint4 v = {};
+                            if (src && i + q < G::kWords) v = *reinterpret_cast<const uint4*>(src + 8 * (i + q));
+                            r[4 * q] = v.x, r[4 * q + 1] = v.y, r[4 * q + 2] = v.z, r[4 * q + 3] = v.w;
+                        }
+                        if (i + 8 <= G::kWords) tmem_store<32, 0>(dst + 4 * i, r);
+                        else tmem_store<8, 0>(dst + 4 * i, r);
+                    }
                 }
+                tmem_store2(dst + 64, z, z & 0xffffu);
                 tmem_wait_st();
                 tc_fence_before();
                 mbar_arrive(smem_u32(&c.k_full[tau & 1]));
             }
-            copy_wait<0>();
+            plan_used(unit);
         }
+        copy_wait<0>();
     } else if (warp < 8) {
         // ---- V ------------------------------------------------------------------------------
         const int t = tid - 128;
@@ -352,37 +370,22 @@ __global__ void __launch_bounds__(kTileThreads, 1) msa_attention_kvq_tiles_kerne
         // keys in the order in which the columns of V^T follow one another: transposed byte 4 q + e of 16 keys goes to column q (e < 2) or
         // 4 + q, which hold keys 2 q, 2 q + 1 and 8 + 2 q, 8 + 2 q + 1
         const int from16 = (lane & 3) < 2 ? 2 * ((lane & 15) >> 2) + (lane & 3) : 8 + 2 * ((lane & 15) >> 2) + (lane & 3) - 2;
-        const Line<N, kTileOfKeys, 0, kTileStart>& line = walks[1].line;
-        while (next_unit(walks[1], t == 0, 2, 128)) {            // (the ring's last stage has been read by all)
-            const Seq s = line.s;
-            const int P = prefix_chunks<kTileOfKeys>(s.L), from = line.from, to = line.to, held = min(to, P), h = min(line.head0, a.n_heads - 1);
-            const bool real = line.head0 < a.n_heads;
-            TileLoader<D, N> loader(a, s, h, from, t, a.v_codes);
-            const long long words = (s.start + static_cast<long long>(from) * kTileOfKeys) * a.p_slot + h * a.p_head;
-            const auto load = [&](int k) {
-                if (k < held) {
-                    const int st = (k - from) % G::kStages;
-                    loader.next(a, smem + G::oV + st * G::kCodes, t);
-                    copy_async<4>(smem + G::oVParams + (st * kTileOfKeys + t) * 4,
-                                  a.v_params + words + (static_cast<long long>(k - from) * kTileOfKeys + min(t, s.L - 1 - k * kTileOfKeys)) * a.p_slot);
-                }
-                copy_commit();
-            };
-            #pragma unroll 1
-            for (int i = 0; i < G::kStages - 1; ++i) load(from + i);
-            if (to > P && real) prefetch_extra(a, extra_of(a, s, line.row0, N), D, line.b, h, t, a.v_tree, a.v_spec);
+        uint32_t unit = 0, used = 0;                 // units; tiles of codes used
+        for (;; ++unit) {
+            const TileUnit& u = plan_of(unit);
+            if (u.done) break;
+            const int from = u.from, to = u.to, held = min(to, u.prefix);
             #pragma unroll 1
             for (int k = from; k < to; ++k, ++tau) {
-                const int st = (k - from) % G::kStages;
                 const uint32_t dst = tmem + G::kTmemV + (tau & 1) * 64 + lanes;
                 if (k < held) {
-                    copy_wait<G::kStages - 2>();
-                    named_barrier(2, 128);
-                    load(k + G::kStages - 1);
+                    const uint32_t st = used % G::kStages;
+                    wait(c.codes_full[st], (used / G::kStages) & 1);
+                    ++used;
                     if (tau >= 2) wait(c.pv_done[tau & 1], ((tau - 2) >> 1) & 1);
                     tc_fence_after();
                     if (mine) {
-                        const uint32_t codes = smem + G::oV + st * G::kCodes, words = smem + G::oVParams + st * kTileOfKeys * 4 + 8 * (lane & 3);
+                        const uint32_t codes = smem + G::oV + st * G::kCodes, words = smem + G::oVParams + (tau % G::kParams) * kTileOfKeys * 4 + 8 * (lane & 3);
                         #pragma unroll
                         for (int half = 0; half < 2; ++half) {
                             uint32_t lo[16], hi[16];
@@ -405,17 +408,17 @@ __global__ void __launch_bounds__(kTileThreads, 1) msa_attention_kvq_tiles_kerne
                             tmem_store_lanes16(dst + 32 * half + (16u << 16), hi);
                         }
                     }
+                    mbar_arrive(smem_u32(&c.codes_free[st]));
                 } else {
                     // bf16 rows in the order of the lanes: of 8 values the low codes' would be 0, 4, 1, 5, the high codes' 2, 6, 3, 7.  64 keys at
-                    // a time, in the ring's place; a row's words are shared by two threads.
-                    const Extra x = extra_of(a, s, line.row0, N);
+                    // a time; a row's words are shared by two threads.
                     const int r = t >> 1;
-                    const bool both = (k - P) * kTileOfKeys + 64 < x.count;      // (else the tile's upper half is empty)
+                    const bool both = (k - u.prefix) * kTileOfKeys + 64 < u.extra.count;      // (else the tile's upper half is empty)
                     uint4 v[2 * G::kQuads];
                     const auto fetch = [&](int half) {
-                        const int e = (k - P) * kTileOfKeys + 64 * half + r;
+                        const int e = (k - u.prefix) * kTileOfKeys + 64 * half + r;
                         const __nv_bfloat16* src = nullptr;
-                        if (real && e < x.count) src = (e < x.T ? a.v_tree : a.v_spec) + extra_offset(a, x, D, line.b, h, e);
+                        if (u.real && e < u.extra.count) src = (e < u.T ? a.v_tree : a.v_spec) + extra_offset(a, u.extra, D, u.b, u.head, e);
                         #pragma unroll
                         for (int i = 0; i < 2 * G::kQuads; ++i) {
                             const int word = 2 * i + (t & 1);
@@ -440,7 +443,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) msa_attention_kvq_tiles_kerne
                         }
                         if (half > 0) fetch(1);
                         named_barrier(2, 128);       // (what lay there has been read)
-                        const uint32_t row = smem + G::oV + r * G::kRowOfV;
+                        const uint32_t row = smem + G::oRows + r * G::kRowOfV;
                         #pragma unroll
                         for (int i = 0; i < 2 * G::kQuads; ++i) {
                             // bytes: 64 to a quad, low ones first, 8 to a word; 16-byte places swizzled by the key
@@ -459,7 +462,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) msa_attention_kvq_tiles_kerne
                                     const int kk = 16 * i + 8 * (lane >> 4) + (lane & 7);          // matrices: dims 0..7, 8..15 of 8 keys, then of 8 more
                                     const int at = 64 * quad + 32 * high + 16 * ((lane >> 3) & 1);
                                     uint32_t q[4];
-                                    load_transposed_halves(smem + G::oV + kk * G::kRowOfV + (((at >> 4) ^ (kk & 3)) << 4), q);
+                                    load_transposed_halves(smem + G::oRows + kk * G::kRowOfV + (((at >> 4) ^ (kk & 3)) << 4), q);
                                     q16[4 * i] = q[0], q16[4 * i + 1] = q[1], q16[4 * i + 2] = q[2], q16[4 * i + 3] = q[3];
                                 }
                                 tmem_store_lanes16(dst + 32 * half + (high ? 16u << 16 : 0u), q16);
@@ -471,7 +474,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) msa_attention_kvq_tiles_kerne
                 tc_fence_before();
                 mbar_arrive(smem_u32(&c.v_full[tau & 1]));
             }
-            copy_wait<0>();
+            plan_used(unit);
         }
     } else if (warp < kMmaWarp) {
         // ---- softmax ------------------------------------------------------------------------
@@ -484,32 +487,11 @@ __global__ void __launch_bounds__(kTileThreads, 1) msa_attention_kvq_tiles_kerne
         const uint32_t weights = smem + G::oP + key * 128;        // the key's row of P^T
         // TMEM lane to dimension
         const int byte = 16 * quad + (lane & 15), dim = 8 * (byte >> 2) + ((byte & 1) << 2) + ((byte >> 1) & 1) + ((lane >> 4) << 1);
-        const Line<N, kTileOfKeys, 0, kTileStart>& line = walks[2 + group].line;
-        while (next_unit(walks[2 + group], key == 0, bar, 128)) {
-            const Seq& s = line.s;
-            const int L = s.L, P = prefix_chunks<kTileOfKeys>(L), from = line.from, to = line.to;
-            const Extra x = extra_of(a, s, line.row0, N);
-            {
-                const int n = group * C + lane, r = line.row0 + n;
-                unsigned long long see = 0;
-                long long out = 0;
-                if (lane < C && r < s.rows && line.head0 < a.n_heads) {
-                    see = a.trees[line.b].anc_mask[row_of(r, s.T, a.gamma).t];
-                    out = row_offset(a, D, line.b, line.head0, r, s.T);
-                }
-                uint32_t own = 0u;
-                #pragma unroll
-                for (int i = 0; i < 16; ++i) {       // nodes 16 quad ..
-                    const uint32_t rows = __ballot_sync(0xffffffffu, see >> (16 * quad + i) & 1ull);
-                    if (lane == i) own = rows;
-                }
-                if (lane < 16) c.see[group][16 * quad + lane] = own;
-                if (quad == 0 && lane < C) c.out[n] = out, c.neg_ref[n] = 0.f;
-                if (key == 96) {
-                    const Pieces share(line);
-                    c.first[group] = share.first, c.last[group] = share.last, c.second[group] = share.second;
-                }
-            }
+        for (;; ++unit) {
+            const TileUnit& u = plan_of(unit);
+            if (u.done) break;
+            const int L = u.L, P = u.prefix, from = u.from, to = u.to;
+            if (quad == 0 && lane < C) c.neg_ref[group * C + lane] = 0.f;
             named_barrier(bar, 128);
             float l[C];
             #pragma unroll
@@ -520,24 +502,24 @@ __global__ void __launch_bounds__(kTileThreads, 1) msa_attention_kvq_tiles_kerne
                 const uint32_t parity = (tau >> 1) & 1;
                 wait(c.s_full[tau & 1], parity);
                 tc_fence_after();
-                const uint2 params = lds64(smem + G::oKParams + ((tau % G::kParams) * kTileOfKeys + key) * 8);
-                const float sk = scale_of(params.x) * a.scale, sv = scale_of(params.y);
+                const uint32_t params = ((tau % G::kParams) * kTileOfKeys + key) * 4;
+                const float sk = scale_of(lds32(smem + G::oKParams + params)) * a.scale, sv = scale_of(lds32(smem + G::oVParams + params));
                 // rows that see the key: all of them if it is a cached one; else those of its node's descendants; of a stream key, from its
                 // own row to its node's last
                 uint32_t vis = all;
                 if (k < P) {
-                    if (k * kTileOfKeys + key >= L) vis = 0u;
+                    if ((k + 1) * kTileOfKeys > L && k * kTileOfKeys + key >= L) vis = 0u;
                 } else {
                     const int e = (k - P) * kTileOfKeys + key;
                     vis = 0u;
-                    if (e < x.T) {
-                        vis = c.see[group][e];
-                    } else if (e < x.count) {
-                        const int own = e - x.T + x.t0 * x.gamma, first = x.T + own - x.row0 - group * C, last = first + x.gamma - 1 - own % x.gamma;
+                    if (e < u.T) {
+                        vis = static_cast<uint32_t>(u.see[e] >> (group * C)) & all;
+                    } else if (e < u.extra.count) {
+                        const int own = e - u.T + u.extra.t0 * u.extra.gamma, first = u.T + own - u.row0 - group * C, last = first + u.extra.gamma - 1 - own % u.extra.gamma;
                         if (first < C && last >= 0) vis = (0xffffffffu >> (31 - min(last, 31))) & (0xffffffffu << max(first, 0));
                     }
                 }
-                const bool masked = __any_sync(0xffffffffu, (vis & all) != all);
+                const bool masked = (k + 1) * kTileOfKeys > L;
                 float d[C];
                 // scores above their references, in log2 units; -inf where the row does not see the key
                 const auto scores = [&]() {
@@ -662,13 +644,13 @@ __global__ void __launch_bounds__(kTileThreads, 1) msa_attention_kvq_tiles_kerne
             tc_fence_before();
             mbar_arrive(smem_u32(&c.o_free));
             const bool ok = *const_cast<volatile int*>(&c.abort) == 0;
-            const int rows = line.head0 < a.n_heads ? min(N, s.rows - line.row0) : 0;
-            if (line.whole()) {
+            const int rows = u.real ? u.rows : 0, mains = u.T - u.row0;       // rows, and how many of them are main-stream ones
+            if (u.whole) {
                 const float f = 1.f / sum;
                 if (quad == 0 && lane < C && ok && group * C + lane < rows) {
                     const int n = group * C + lane;
-                    float* lse = line.row0 + n < s.T ? a.lse_main : a.lse_spec;
-                    if (lse != nullptr) lse[c.out[n] / D] = (ref + log2f(sum)) * 0.6931471805599453f;
+                    float* lse = n < mains ? a.lse_main : a.lse_spec;
+                    if (lse != nullptr) lse[u.out[n] / D] = (ref + log2f(sum)) * 0.6931471805599453f;
                 }
                 // to rows of dimensions, by way of the group's part of the first buffer of P: a TMEM lane's rows lie where a key's weights do
                 #pragma unroll
@@ -692,12 +674,12 @@ __global__ void __launch_bounds__(kTileThreads, 1) msa_attention_kvq_tiles_kerne
                     for (int i = 0; i < 4; ++i) {
                         const int mi = m0 + i, wi = mi / (C / 8), n = group * C + 8 * (mi - wi * (C / 8)) + (lane >> 2);
                         if (n < rows && ok)
-                            *reinterpret_cast<uint32_t*>((line.row0 + n < s.T ? a.o_main : a.o_spec) + c.out[n] + 8 * wi + 2 * (lane & 3)) = q[i];
+                            *reinterpret_cast<uint32_t*>((n < mains ? a.o_main : a.o_spec) + u.out[n] + 8 * wi + 2 * (lane & 3)) = q[i];
                     }
                 }
                 named_barrier(bar, 128);             // (the next unit's weights go there)
             } else {
-                float* const mine = partial + (2ll * ((line.me << line.team_log2) + line.member) + (line.me == c.first[group] ? c.second[group] : 0)) * kPartial;
+                float* const mine = partial + (2ll * blockIdx.x + (u.me == u.first ? u.second : 0)) * kPartial;
                 if (quad == 0 && lane < C)
                     __stcg(reinterpret_cast<float2*>(mine + (group * C + lane) * (D + 4) + D), make_float2(seen >> lane & 1u ? ref : kNoRef, sum));
                 if (dim < D) {
@@ -706,15 +688,15 @@ __global__ void __launch_bounds__(kTileThreads, 1) msa_attention_kvq_tiles_kerne
                 }
                 named_barrier(3 + kTileGroups, kTileSoftmax);
                 if (tid == 256) {
-                    c.joined = last_piece(counters + (c.first[0] << line.team_log2) + line.member, c.last[0] - c.first[0] + 1);
+                    c.joined = last_piece(counters + (u.first << u.team) + u.member, u.last - u.first + 1);
                 }
                 named_barrier(3 + kTileGroups, kTileSoftmax);
                 if (c.joined) {
                     // 8 values of a row at a time, up to four partial rows on their way
-                    const int first = c.first[group], n = c.last[group] - first + 1, items = rows * (D / 8);
-                    const float* const p0 = partial + (2ll * ((first << line.team_log2) + line.member) + c.second[group]) * kPartial;
-                    const long long on = (2ll << line.team_log2) * kPartial;                 // between teams' places
-                    const float* const p1 = p0 - c.second[group] * kPartial + on;
+                    const int n = u.last - u.first + 1, items = rows * (D / 8);
+                    const float* const p0 = partial + (2ll * ((u.first << u.team) + u.member) + u.second) * kPartial;
+                    const long long on = (2ll << u.team) * kPartial;         // between teams' places
+                    const float* const p1 = p0 - u.second * kPartial + on;
                     #pragma unroll 1
                     for (int item = tid - 256; item < items; item += kTileSoftmax) {
                         const int r = item / (D / 8), d0 = (item - r * (D / 8)) * 8;
@@ -734,18 +716,16 @@ __global__ void __launch_bounds__(kTileThreads, 1) msa_attention_kvq_tiles_kerne
                             for (int q = 0; q < 4; ++q)
                                 if (i + q < n) join_row(o, m, sm, st[q], u[q], v[q]);
                         }
-                        if (ok) store_row<D>(a, line.row0 + r < s.T, c.out[r], d0, o, m, sm);
+                        if (ok) store_row<D>(a, r < mains, u.out[r], d0, o, m, sm);
                     }
-                    named_barrier(3 + kTileGroups, kTileSoftmax);           // (all groups read all rows' places)
                 }
             }
-            ++unit;
+            plan_used(unit);
         }
-    } else {
+    } else if (warp == kMmaWarp) {
         // ---- MMAs ---------------------------------------------------------------------------
         const uint32_t base = uniform(smem);
-        const uint64_t dq = desc_k_major(base + G::oQ), dp = desc_mn_major(base + G::oP, 0);
-        const Line<N, kTileOfKeys, 0, kTileStart>& line = walks[2 + kTileGroups].line;
+        const uint64_t dq = desc_k_major(base + G::oQ), dz = desc_16_columns(base + G::oZ), dp = desc_mn_major(base + G::oP, 0);
         uint32_t unit = 0;
         const auto product = [&](uint32_t t, bool first) {       // O^T (+)= V^T P^T of tile t
             if (first && unit > 0) wait(c.o_free, (unit - 1) & 1);
@@ -758,26 +738,117 @@ __global__ void __launch_bounds__(kTileThreads, 1) msa_attention_kvq_tiles_kerne
             tc_mma_ts_steps(tmem + G::kTmemO, va + 32, b + 4 * 128, G::kIdescPV, 1u);
             tc_commit_e(smem_u32(&c.pv_done[t & 1]));
         };
-        while (next_unit(walks[2 + kTileGroups], lane == 0, 0, 32)) {
-            const uint32_t tiles = uniform(static_cast<uint32_t>(line.to - line.from));
+        for (;; ++unit) {
+            const TileUnit& u = plan_of(unit);
+            if (u.done) break;
+            const uint32_t tiles = uniform(static_cast<uint32_t>(u.to - u.from));
+            const uint64_t rows = (unit & 1) * (G::kRowsOfUnit >> 4);
+            wait(c.rows_full[unit & 1], (unit >> 1) & 1);
             #pragma unroll 1
             for (uint32_t i = 0; i < tiles; ++i, ++tau) {
                 wait(c.k_full[tau & 1], (tau >> 1) & 1);
                 if (tau >= 2) wait(c.s_free[tau & 1], ((tau - 2) >> 1) & 1);
                 tc_fence_after();
-                const uint32_t ka = tmem + G::kTmemK + (tau & 1) * 64, sd = tmem + G::kTmemS + (tau & 1) * N;
-                tile_mma<4>(sd, ka, dq, G::kIdescS, 0u);
-                if constexpr (D == 128) tile_mma<4>(sd, ka + 32, dq + (G::kBox >> 4), G::kIdescS, 1u);
-                if constexpr (D == 80) tile_mma<1>(sd, ka + 32, dq + (G::kBox >> 4), G::kIdescS, 1u);
+                const uint32_t ka = tmem + G::kTmemK + (tau & 1) * 72, sd = tmem + G::kTmemS + (tau & 1) * N;
+                tile_mma<4>(sd, ka, dq + rows, G::kIdescS, 0u);
+                if constexpr (D == 128) tile_mma<4>(sd, ka + 32, dq + rows + (G::kBox >> 4), G::kIdescS, 1u);
+                if constexpr (D == 80) tile_mma<1>(sd, ka + 32, dq + rows + (G::kBox >> 4), G::kIdescS, 1u);
+                tile_mma<1>(sd, ka + 64, dz + rows, G::kIdescS, 1u);
                 tc_commit_e(smem_u32(&c.s_full[tau & 1]));
                 if (lane == 0) mbar_arrive(smem_u32(&c.s_full[tau & 1]));            // (passes on what the K warps have written: the keys' scales)
                 if (i > 0) product(tau - 1, i == 1);
             }
             product(tau - 1, tiles == 1);
-            ++unit;
+            plan_used(unit);
         }
         tc_commit_e(smem_u32(&c.drain));
         mbar_drain(smem_u32(&c.drain), 0);           // (nothing is in flight when TMEM goes back)
+    } else {
+        // ---- preparing ----------------------------------------------------------------------
+        const int t = tid - 32 * kPlanWarp, place = warp - kPlanWarp;
+        float* const sums = reinterpret_cast<float*>(smem_raw + G::oSums);           // [row][16] of partial sums of x
+        constexpr int kItems = (N * (D / 8) + kTilePrepare - 1) / kTilePrepare, kBatch = 6;
+        for (uint32_t unit = 0;; ++unit) {
+            TileUnit& u = c.unit[unit & 1];
+            const uint32_t rows_at = smem + G::oQ + (unit & 1) * G::kRowsOfUnit;
+            if (place == 0) {
+                const bool more = line.next(a);
+                // (a unit's rows are free when all are done with the plan: its last S is complete then)
+                if (unit >= 2) wait(c.plan_free[unit & 1], ((unit - 2) >> 1) & 1);
+                if (lane == 0) {
+                    u.done = !more;
+                    if (more) {
+                        const Seq& s = line.s;
+                        const Pieces share(line);
+                        u.L = s.L, u.T = s.T, u.prefix = prefix_chunks<kTileOfKeys>(s.L), u.from = line.from, u.to = line.to, u.start = s.start;
+                        u.head = min(line.head0, a.n_heads - 1), u.real = line.head0 < a.n_heads, u.row0 = line.row0, u.rows = min(N, s.rows - line.row0), u.b = line.b;
+                        u.whole = line.whole(), u.first = share.first, u.last = share.last, u.second = share.second;
+                        u.me = line.me, u.member = line.member, u.team = line.team_log2;
+                        u.extra = extra_of(a, s, line.row0, N);
+                    }
+                }
+            }
+            named_barrier(4 + kTileGroups, kTilePrepare);
+            if (t == 0) mbar_arrive(smem_u32(&c.plan_full[unit & 1]));
+            if (u.done) break;
+            // what lies behind the prefix comes to L2 meanwhile
+            const int rows = u.rows, T = u.T, row0 = u.row0, h = u.head, b = u.b;
+            if (u.to > u.prefix) {
+                for (int e = t; e < kTileOfKeys; e += kTilePrepare) {
+                    prefetch_extra(a, u.extra, D, b, h, e, a.k_tree, a.k_spec);
+                    prefetch_extra(a, u.extra, D, b, h, e, a.v_tree, a.v_spec);
+                }
+            }
+            // query rows, 16 bytes at a time, some of a thread's on their way at once
+            #pragma unroll 1
+            for (int i = 0; i < kItems; i += kBatch) {
+                uint4 v[kBatch];
+                #pragma unroll
+                for (int q = 0; q < kBatch; ++q) {
+                    const int item = (i + q) * kTilePrepare + t, r = item / (D / 8), at = item - r * (D / 8), row = row0 + r;
+                    v[q] = make_uint4(0u, 0u, 0u, 0u);
+                    if (r < rows) v[q] = *reinterpret_cast<const uint4*>((row < T ? a.q_main : a.q_spec) + row_offset(a, D, b, h, row, T) + 8 * at);
+                }
+                #pragma unroll
+                for (int q = 0; q < kBatch; ++q) {
+                    const int item = (i + q) * kTilePrepare + t, r = item / (D / 8), at = item - r * (D / 8);
+                    if (item >= N * (D / 8)) break;
+                    const uint32_t pair[4] = {v[q].x, v[q].y, v[q].z, v[q].w};
+                    float sum = 0.f;
+                    #pragma unroll
+                    for (int n = 0; n < 4; ++n) sum += __uint_as_float(pair[n] << 16) + __uint_as_float(pair[n] & 0xffff0000u);
+                    st_shared_v4(rows_at + (at >> 3) * G::kBox + r * 128 + (((at & 7) ^ (r & 7)) << 4), v[q].x, v[q].y, v[q].z, v[q].w);
+                    sums[r * 16 + at] = sum;
+                }
+            }
+            named_barrier(4 + kTileGroups, kTilePrepare);
+            // what 128 + z meets
+            if (t < N) {
+                float x = 0.f;
+                #pragma unroll
+                for (int i = 0; i < D / 8; ++i) x += sums[t * 16 + i];
+                x = -x;
+                const float t0 = round_bf16(x), t1 = round_bf16(x - t0), t2 = (x - t0) - t1;
+                const uint32_t row = rows_at + G::kBoxes * G::kBox + (t >> 3) * 256 + (t & 7) * 16;
+                st_shared_v4(row, pack2_bf16(t0, t1), pack2_bf16(t2, 0.f), 0u, 0u);
+                st_shared_v4(row + 128, 0u, 0u, 0u, 0u);
+                u.out[t] = t < rows ? row_offset(a, D, b, h, row0 + t, T) : 0;
+            }
+            // the rows that see a node: every warp takes a third of the nodes
+            unsigned long long see[2] = {};
+            #pragma unroll
+            for (int half = 0; half < (N + 31) / 32; ++half) {
+                const int n = 32 * half + lane;
+                if (n < rows) see[half] = a.trees[b].anc_mask[row_of(row0 + n, T, a.gamma).t];
+            }
+            for (int e = place; e < T; e += 3) {
+                const uint32_t lo = __ballot_sync(0xffffffffu, see[0] >> e & 1ull), hi = N > 32 ? __ballot_sync(0xffffffffu, see[1] >> e & 1ull) : 0u;
+                if (lane == 0) u.see[e] = static_cast<unsigned long long>(hi) << 32 | lo;
+            }
+            fence_async_smem();
+            named_barrier(4 + kTileGroups, kTilePrepare);
+            if (t == 0) mbar_arrive(smem_u32(&c.rows_full[unit & 1]));           // (the query rows, and with them `out` and `see`)
+        }
     }
     tc_fence_before();
     __syncthreads();
