@@ -383,7 +383,8 @@ int32_t ss_kvq_read(const ss_kvq_cache* cache, const ss_kvq_rows* rows, const in
  * rounds p); sums, statistics and both products accumulate in fp32.
  * The keys of all heads are dealt out evenly over the GPU, whatever the lengths; a head that several CTAs share leaves partial
  * rows in the workspace, and the last of them to finish joins them in key order: results do not depend on the order of arrival,
- * and no CTA waits for another.
+ * and no CTA waits for another.  The workspace holds the counters of arrivals, zero between calls, and those rows: calls of
+ * different shapes may share one that is large enough for each, in stream order, but it is not one of another entry point's.
  * A sequence with kv_len[b] over its capacity, with slots outside the slab or without nodes is skipped (its outputs are not
  * written); for the first two the status word is set to SS_ERR_CAPACITY.
  * Errors (nothing launched): SS_ERR_INVALID_ARG, SS_ERR_UNSUPPORTED, SS_ERR_WORKSPACE, SS_ERR_CUDA. */

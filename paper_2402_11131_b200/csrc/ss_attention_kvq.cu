@@ -327,6 +327,10 @@ __device__ __forceinline__ void store_row(const KvqArgs& a, bool main, long long
     if (d0 == 0 && lse != nullptr) lse[off / D] = (m + log2f(l)) * 0.6931471805599453f;
 }
 
+// A workspace: the header, the counters (one per CTA, zero between calls), the partial rows.  The counters' room does not depend on
+// the call: calls of other shapes on the same workspace leave their partial rows elsewhere.
+constexpr int kCounterBytes = 4096;
+
 // One more piece of a unit is in the workspace: true for the last of `n`, who joins them and leaves the counter at zero.  Called by one
 // thread behind a barrier of those that wrote: the operation releases their partial rows and acquires the others'.
 __device__ __forceinline__ bool last_piece(int* counter, int n) {
@@ -800,7 +804,7 @@ __global__ void __launch_bounds__(kThreads, NG == 1 ? 3 : 2) msa_attention_kvq_r
     if (!line.begin(a, lane)) return;
     const int HW = 1 << line.heads_log2, KS = 1 << line.steps_log2;
     int* const counters = reinterpret_cast<int*>(a.ws + kWsHeaderBytes);
-    float* const partial = reinterpret_cast<float*>(a.ws + kWsHeaderBytes + (4ull * gridDim.x + 255) / 256 * 256);
+    float* const partial = reinterpret_cast<float*>(a.ws + kWsHeaderBytes + kCounterBytes);
     const int my_head = warp & (HW - 1), slice = warp >> line.heads_log2;
 
     while (line.next(a)) {
@@ -1018,7 +1022,7 @@ static KvqPlan kvq_plan(const ss_kvq_attn_params& p) {
     KvqPlan k{0, rows <= 8 ? 1 : 2, 0, 0};
     if (rows > 16) k.tile = rows <= 32 ? 32 : 64;
     k.block = k.tile > 0 ? k.tile : 8 * k.groups;
-    k.ctas = sm_count() * (k.tile > 0 ? 1 : k.groups == 1 ? 3 : 2);
+    k.ctas = std::min(sm_count() * (k.tile > 0 ? 1 : k.groups == 1 ? 3 : 2), kCounterBytes / 4);
     return k;
 }
 
@@ -1026,7 +1030,7 @@ static size_t kvq_workspace(const ss_kvq_attn_params& p) {
     const KvqPlan k = kvq_plan(p);
     const size_t ctas = static_cast<size_t>(k.ctas), d = static_cast<size_t>(p.cache.head_dim);
     const size_t floats = k.tile > 0 ? k.tile * (d + 4) : static_cast<size_t>(partial_floats(p.cache.head_dim, k.block));
-    return kWsHeaderBytes + (4 * ctas + 255) / 256 * 256 + 2 * ctas * floats * sizeof(float);
+    return kWsHeaderBytes + kCounterBytes + 2 * ctas * floats * sizeof(float);
 }
 
 template <typename Kernel>

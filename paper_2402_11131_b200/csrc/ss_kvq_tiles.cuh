@@ -482,7 +482,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) msa_attention_kvq_tiles_kerne
         constexpr uint32_t all = C == 32 ? 0xffffffffu : (1u << C) - 1u;
         uint32_t unit = 0;
         int* const counters = reinterpret_cast<int*>(a.ws + kWsHeaderBytes);
-        float* const partial = reinterpret_cast<float*>(a.ws + kWsHeaderBytes + (4ull * gridDim.x + 255) / 256 * 256);
+        float* const partial = reinterpret_cast<float*>(a.ws + kWsHeaderBytes + kCounterBytes);
         constexpr int kPartial = N * (D + 4);
         const uint32_t weights = smem + G::oP + key * 128;        // the key's row of P^T
         // TMEM lane to dimension

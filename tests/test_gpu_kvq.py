@@ -376,6 +376,38 @@ def test_attention_beyond_32_bit_offsets(api):
     assert ((x.o_main[0].cpu().double() - o).abs() <= tol).all()
 
 
+def test_calls_of_other_shapes_share_a_workspace(api):
+    """Grids, partial rows and kernels of different sizes in turn on one workspace, eagerly and as two captured graphs."""
+    xs = [Layer(api, 1, 1, 64, [150], [2], 0, seed=31), Layer(api, 2, 8, 128, [3000, 900], [40, 40], 0, seed=32),
+          Layer(api, 1, 2, 80, [700], [64], 1, seed=33), Layer(api, 1, 32, 128, [2000], [1], 0, seed=34),
+          Layer(api, 3, 2, 128, [400, 33, 5000], [14, 14, 14], 0, seed=35), Layer(api, 1, 1, 128, [90], [30], 0, seed=36)]
+    ws = max((x.workspace() for x in xs), key=lambda w: w.numel())
+    for order in ([0, 1, 2, 3, 4, 5], [5, 3, 1, 0, 4, 2], [1, 5, 0, 4, 3, 2]):
+        for i in order:
+            xs[i].fresh()
+            xs[i].run(ws)
+        for x in xs:
+            x.check()
+    params = [x.params(ws) for x in xs]
+    graphs = []
+    for part in (params[:3], params[3:]):
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            for p in part:
+                api.ss_msa_attention_kvq(p)
+    for _ in range(3):
+        for x in xs:                                          # (in place: the graphs hold these tensors)
+            for t in (x.o_main, x.o_spec, x.lse_main, x.lse_spec):
+                if t is not None:
+                    t.fill_(77.0)
+        graphs[0].replay()
+        graphs[1].replay()
+        torch.cuda.synchronize()
+        for x in xs:
+            x.check()
+    assert api.ss_status(ws) == 0
+
+
 def test_captured_calls_and_another_stream(api):
     """Write, attention and read in a graph on a side stream, replayed with other contents of the same buffers."""
     x = Layer(api, 3, 4, 128, [40, 300, 129], [9, 9, 9], 2, seed=12)
