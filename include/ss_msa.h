@@ -343,7 +343,8 @@ typedef struct ss_kvq_cache {
 } ss_kvq_cache;
 
 /* bf16 rows outside the cache: layer l, sequence b, row r, head h at k + l * layer_stride + b * batch_stride + r * row_stride +
- * h * head_stride (elements, multiples of 8; bases 16-byte aligned), head_dim values next to each other. */
+ * h * head_stride (elements, multiples of 8; bases 16-byte aligned), head_dim values next to each other.  At most 65535 sequences
+ * and 2^30 rows. */
 typedef struct ss_kvq_rows {
     void* k;
     void* v;
@@ -361,7 +362,8 @@ typedef struct ss_kvq_rows {
  *   status   a workspace whose word 0 receives SS_ERR_CAPACITY, or NULL
  * A sequence whose rows do not fit (kv_len + n_rows over its capacity, or slots outside the slab) is skipped and keeps its
  * length.  Slots of other rows are not touched.  One launch, two where kv_len_out overlaps an input.
- * Errors (nothing launched): SS_ERR_INVALID_ARG, SS_ERR_UNSUPPORTED (head_dim not in {64, 80, 128}), SS_ERR_CUDA. */
+ * Errors (nothing launched): SS_ERR_INVALID_ARG, SS_ERR_UNSUPPORTED (head_dim not in {64, 80, 128}, more than 65535 heads, strides
+ * that are no multiples, kv_len_out over an input and more than 1024 sequences), SS_ERR_CUDA. */
 int32_t ss_kvq_write(const ss_kvq_rows* rows, const ss_kvq_cache* cache, const int64_t* kv_start, const int32_t* kv_len_in,
                      const int32_t* n_rows, const int32_t* path, const int32_t* kv_capacity, int32_t* kv_len_out, void* status,
                      void* stream);

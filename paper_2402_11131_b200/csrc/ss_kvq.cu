@@ -1,23 +1,27 @@
 // Rows into and out of a cache held in 4 bits (format and layout: ss_msa.h).  Compiled without fast-math: scales and codes are
 // defined bit by bit.
 //
-// Both kernels stream: HBM bounds them.  A thread holds 16 values (32 bytes of bf16, 8 bytes of codes), so a row of a head is
-// 4, 5 or 8 neighbouring lanes, which find the row's extremes with three exchanges.
+// Both kernels stream: HBM bounds them.  A thread holds 16 values, 8 at dimension 8 at and 8 at D / 2 + 8 at: a row of a head is 4, 5
+// or 8 neighbouring lanes that read (or write) runs of 16 bytes next to each other, and find the row's extremes with three exchanges.
 //
-// The arithmetic of the scale.  s is the smallest bf16 with 15 s >= hi - lo.  Directed rounding composes: a sum rounded up to
-// fp32, its quotient rounded up to fp32 and that rounded up to bf16 is the exact quotient rounded up to bf16, because 15 s is
-// itself an fp32 number.  (Everything is divided by 16 first, exactly, so that hi - lo does not overflow.)
+// The arithmetic of the scale.  s is the smallest bf16 with 15 s >= hi - lo.  15 s is an fp32 number, so that is 15 s >= t with t the
+// sum rounded up to fp32.  (Everything is divided by 16 first, exactly, so that hi - lo does not overflow.)  t * (1 + 2^-22) 16 / 15
+// cut to bf16 is that s or the bf16 below: it is not below the quotient's cut, and above it only where the bf16 above is s.
 // The arithmetic of the codes.  x and s have 8 significant bits, so x / s either lies exactly between two whole numbers or is at
 // least 2^-13 of itself away from there (the midpoints are (2k + 1) / 2 with 2k + 1 <= 31, and 255 * 31 < 2^13).  x * (1 / s) with
 // 1 / s enlarged by 2^-16 is off by less than that and on the far side of the midpoint where the quotient is exactly one, so that
-// one fused multiply-add with 1.5 * 2^23, whose sum has no fraction bits left, rounds as if the quotient were exact.
+// one fused multiply-add with 1.5 * 2^23 + z, whose sum has no fraction bits left, rounds as if the quotient were exact; the sum's low
+// 16 bits are round(x / s) + z, clamped two at a time.
 #include <cuda_bf16.h>
+
+#include <climits>
 
 #include "ss_common.cuh"
 
 namespace ss {
 
 constexpr int kKvqThreads = 256;
+constexpr int kKvqCtas = 4;                         // resident on an SM: 64 registers a thread
 constexpr float kRoundMagic = 12582912.f;          // 1.5 * 2^23
 
 struct KvqGeo {
@@ -29,66 +33,64 @@ struct KvqGeo {
     int n_heads, max_rows, layers;
 };
 
+// Two at a time; NaN where one of the operands is
 __device__ __forceinline__ uint32_t max_bf16x2(uint32_t a, uint32_t b) {
     uint32_t r;
-    asm("max.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
     return r;
 }
 
-// x / s rounded to the nearest whole number, from the middle away from zero, as the low bits of the result (inv: 1 / s enlarged)
-__device__ __forceinline__ uint32_t rounded_bits(float x, float inv) { return __float_as_uint(__fmaf_rn(x, inv, kRoundMagic)); }
+__device__ __forceinline__ uint32_t min_bf16x2(uint32_t a, uint32_t b) {
+    uint32_t r;
+    asm("min.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+
+__device__ __forceinline__ float rcp_approx(float x) {
+    float r;
+    asm("rcp.approx.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
 
 // A row of D values over D / 16 neighbouring lanes, 16 values each: returns the row's word of scale and zero point and this lane's
-// 16 codes.  All 32 lanes take part; `base` is the first lane of the row, `at` this lane's place in it.
+// two words of codes.  All 32 lanes take part; `base` is the first lane of the row, `at` this lane's place in it.
 template <int D>
-__device__ __forceinline__ uint32_t quantise_row(const uint4 (&x)[2], int base, int at, uint2* codes) {
+__device__ __forceinline__ uint32_t quantise_row(const uint4 (&x)[2], int base, int at, uint32_t (&codes)[2]) {
     constexpr int G = D / 16;
     const uint32_t w[8] = {x[0].x, x[0].y, x[0].z, x[0].w, x[1].x, x[1].y, x[1].z, x[1].w};
-    // largest value and largest negated value, with zero among them; bits of the largest magnitude
-    uint32_t hi2 = 0u, lo2 = 0u, mag = 0u;
+    // largest and smallest value, with zero among them
+    uint32_t hi2 = 0u, lo2 = 0u;
     #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        hi2 = max_bf16x2(hi2, w[i]);
-        lo2 = max_bf16x2(lo2, w[i] ^ 0x80008000u);
-        mag = __vmaxu2(mag, w[i] & 0x7fff7fffu);
-    }
-    uint32_t ext = max_bf16x2(__byte_perm(hi2, lo2, 0x5410), __byte_perm(hi2, lo2, 0x7632));    // low half: hi, high half: -lo
-    mag = max(mag & 0xffffu, mag >> 16);
+    for (int i = 0; i < 8; ++i) hi2 = max_bf16x2(hi2, w[i]), lo2 = min_bf16x2(lo2, w[i]);
+    uint32_t ext = max_bf16x2(__byte_perm(hi2, lo2, 0x5410) & 0x7fff7fffu, __byte_perm(hi2, lo2, 0x7632) & 0x7fff7fffu);   // low half: hi, high half: -lo
     #pragma unroll
     for (int step = 0; step < 3; ++step) {
         const int shift = step == 0 ? 1 : step == 1 ? 2 : (G == 8 ? 4 : 1);     // (after 1 + 2 + 1 a lane has seen all of 4 or 5)
         int from = at + shift;
         if (from >= G) from -= G;
         ext = max_bf16x2(ext, __shfl_sync(0xffffffffu, ext, base + from));
-        mag = max(mag, __shfl_sync(0xffffffffu, mag, base + from));
     }
     const float hi = __uint_as_float(ext << 16), nlo = __uint_as_float(ext & 0xffff0000u);
-    const float up = __fdiv_ru(__fadd_ru(hi * 0.0625f, nlo * 0.0625f), 0.9375f);
-    uint32_t sb = (__float_as_uint(up) + 0xffffu) >> 16;          // (up is not negative)
+    const bool bad = !(hi < INFINITY && nlo < INFINITY);          // an infinity or a NaN in the row
+    const float t = __fadd_ru(hi * 0.0625f, nlo * 0.0625f);
+    uint32_t sb = __float_as_uint(__fmul_rn(t, 1.06666692f)) >> 16;
+    if (__uint_as_float(sb << 16) * 0.9375f < t) ++sb;
     sb = max(sb, 0x0380u);                                        // 2^-120
     const float s = __uint_as_float(sb << 16);
-    const float inv = __fmul_rn(__frcp_rn(s), 1.0000152587890625f);
-    const bool bad = mag >= 0x7f80u;                              // an infinity or a NaN in the row
-    const uint32_t z = bad ? 0u : (rounded_bits(nlo, inv) & 0xfu);   // (at most 15: nlo <= 15 s)
-    // rounded(x / s) + z in the low bits of 1.5 * 2^23 + .., clamped as an fp32 number
-    const float zf = static_cast<float>(z), top = kRoundMagic + 15.f;
-    uint32_t c[16];
-    #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const float a = __uint_as_float(rounded_bits(__uint_as_float(w[i] << 16), inv)) + zf;
-        const float b = __uint_as_float(rounded_bits(__uint_as_float(w[i] & 0xffff0000u), inv)) + zf;
-        c[2 * i] = __float_as_uint(fminf(fmaxf(a, kRoundMagic), top)) & 0xfu;
-        c[2 * i + 1] = __float_as_uint(fminf(fmaxf(b, kRoundMagic), top)) & 0xfu;
-    }
-    uint32_t out[2];
+    const float inv = __fmul_rn(rcp_approx(s), 1.0000152587890625f);
+    const uint32_t z = bad ? 0u : (__float_as_uint(__fmaf_rn(nlo, inv, kRoundMagic)) & 0xfu);   // (at most 15: nlo <= 15 s)
+    const float from = kRoundMagic + static_cast<float>(z);
     #pragma unroll
     for (int h = 0; h < 2; ++h) {
         uint32_t v = 0u;
         #pragma unroll
-        for (int i = 0; i < 4; ++i) v |= (c[8 * h + 2 * i] << (4 * i)) | (c[8 * h + 2 * i + 1] << (16 + 4 * i));
-        out[h] = bad ? 0u : v;
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t a = __float_as_uint(__fmaf_rn(__uint_as_float(w[4 * h + i] << 16), inv, from));
+            const uint32_t b = __float_as_uint(__fmaf_rn(__uint_as_float(w[4 * h + i] & 0xffff0000u), inv, from));
+            v |= __vimin_s16x2_relu(__byte_perm(a, b, 0x5410), 0x000f000fu) << (4 * i);
+        }
+        codes[h] = bad ? 0u : v;
     }
-    *codes = make_uint2(out[0], out[1]);
     return (bad ? 0x7fffu : sb) | (z << 16);
 }
 
@@ -99,19 +101,42 @@ __device__ __forceinline__ bool write_run(const KvqGeo& g, const int64_t* kv_sta
     *L = kv_len_in[b];
     *n = n_rows != nullptr ? max(0, min(n_rows[b], limit)) : min(g.max_rows, limit);
     *slot0 = kv_start[b] + *L;
-    const bool fits = *L >= 0 && *slot0 >= 0 && *slot0 + *n <= g.total_slots &&
-                      (kv_capacity == nullptr || static_cast<long long>(*L) + *n <= kv_capacity[b]);
+    const bool fits = *L >= 0 && *n <= INT_MAX - *L && *slot0 >= 0 && *slot0 + *n <= g.total_slots &&
+                      (kv_capacity == nullptr || *L + *n <= kv_capacity[b]);
     return fits;
 }
 
+// A warp's unit of work is a few neighbouring slots of one head, D / 16 lanes for each: a head's scales lie slot after slot, and
+// written head after head they would cost a sector per word.
 template <int D>
-__global__ void __launch_bounds__(kKvqThreads)
+struct Unit {
+    static constexpr int G = D / 16, SLOTS = 32 / G, WARPS = kKvqThreads / 32;
+};
+
+// Units in order from unit `first` on, `by` apart: divisions at the start only.  (r: blocks of slots.  There are at most 2^30 slots and
+// steps of some 2^17 units: no overflow.)
+struct Walk {
+    int r, h, dr, dh, n_heads;
+    __device__ __forceinline__ Walk(int heads, int first, int by) : n_heads(heads) {
+        r = first / heads, h = first - r * heads;
+        dr = by / heads, dh = by - dr * heads;
+    }
+    __device__ __forceinline__ void step() {
+        r += dr, h += dh;
+        if (h >= n_heads) h -= n_heads, ++r;
+    }
+};
+
+template <int D>
+__global__ void __launch_bounds__(kKvqThreads, kKvqCtas)
 kvq_write_kernel(const __grid_constant__ KvqGeo g, const int64_t* __restrict__ kv_start, const int32_t* __restrict__ kv_len_in,
                  const int32_t* __restrict__ n_rows, const int32_t* __restrict__ path, const int32_t* __restrict__ kv_capacity,
                  int32_t* __restrict__ kv_len_out, void* __restrict__ status) {
-    constexpr int G = D / 16, ROWS = 32 / G, WARPS = kKvqThreads / 32;
+    using U = Unit<D>;
+    constexpr int G = U::G;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int sub = min(lane / G, ROWS - 1), base = sub * G, at = lane < ROWS * G ? lane - base : 0;
+    const int sub = min(lane / G, U::SLOTS - 1), base = sub * G, at = lane < U::SLOTS * G ? lane - base : 0;
+    const bool mine = lane < U::SLOTS * G;
     const int layer = blockIdx.y >> 1, b = blockIdx.z;
     const bool is_v = blockIdx.y & 1;
     wait_for_previous_kernel();
@@ -124,28 +149,38 @@ kvq_write_kernel(const __grid_constant__ KvqGeo g, const int64_t* __restrict__ k
         if (kv_len_out != nullptr) kv_len_out[b] = fits ? L + n : L;
     }
     if (!fits) return;
-    const unsigned char* rows = (is_v ? g.v_rows : g.k_rows) + layer * g.r_layer + b * g.r_batch;
-    unsigned char* codes = (is_v ? g.v_codes : g.k_codes) + layer * g.layer_stride + slot0 * g.slot_stride;
+    const int* const nodes = path == nullptr ? nullptr : path + static_cast<long long>(b) * SS_PATH_STRIDE;
+    const unsigned char* rows = (is_v ? g.v_rows : g.k_rows) + layer * g.r_layer + b * g.r_batch + 16 * at;
+    unsigned char* codes = (is_v ? g.v_codes : g.k_codes) + layer * g.layer_stride + slot0 * g.slot_stride + 4 * at;
     uint32_t* params = (is_v ? g.v_params : g.k_params) + layer * g.p_layer + slot0 * g.p_slot;
-    const long long items = static_cast<long long>(n) * g.n_heads, step = static_cast<long long>(gridDim.x) * WARPS * ROWS;
-    for (long long i0 = (static_cast<long long>(blockIdx.x) * WARPS + warp) * ROWS; i0 < items; i0 += step) {
-        const long long i = i0 + sub;
-        const int r = static_cast<int>(i / g.n_heads), h = static_cast<int>(i - static_cast<long long>(r) * g.n_heads);
+    // the next unit's rows are on their way while these are turned into codes
+    Walk unit(g.n_heads, blockIdx.x * U::WARPS + warp, gridDim.x * U::WARPS);
+    const auto fetch = [&](uint4 (&x)[2]) {
+        const int r = unit.r * U::SLOTS + sub;
         int src = r;
-        if (path != nullptr && i < items) src = path[static_cast<long long>(b) * SS_PATH_STRIDE + r];
-        const bool live = i < items && lane < ROWS * G && src >= 0 && src < g.max_rows;
-        uint4 x[2] = {};
+        if (nodes != nullptr && r < n) src = nodes[r];
+        const bool live = mine && r < n && src >= 0 && src < g.max_rows;
         if (live) {
-            const uint4* p = reinterpret_cast<const uint4*>(rows + src * g.r_row + h * g.r_head) + 2 * at;
-            x[0] = __ldcs(p);
-            x[1] = __ldcs(p + 1);
+            const uint4* p = reinterpret_cast<const uint4*>(rows + src * g.r_row + unit.h * g.r_head);
+            x[0] = __ldcs(p), x[1] = __ldcs(p + G);
         }
-        uint2 c;
-        const uint32_t word = quantise_row<D>(x, base, at, &c);
+        return live;
+    };
+    uint4 x[2] = {};
+    bool live = fetch(x);
+    while (unit.r * U::SLOTS < n) {
+        const int r = unit.r * U::SLOTS + sub, h = unit.h;
+        unit.step();
+        uint4 next[2] = {};
+        const bool next_live = fetch(next);
+        uint32_t c[2];
+        const uint32_t word = quantise_row<D>(x, base, at, c);
         if (live) {
-            *reinterpret_cast<uint2*>(codes + r * g.slot_stride + h * g.head_stride + 8 * at) = c;
+            uint32_t* const to = reinterpret_cast<uint32_t*>(codes + r * g.slot_stride + h * g.head_stride);
+            to[0] = c[0], to[G] = c[1];
             if (at == 0) params[r * g.p_slot + h * g.p_head] = word;
         }
+        x[0] = next[0], x[1] = next[1], live = next_live;
     }
 }
 
@@ -167,42 +202,55 @@ __device__ __forceinline__ uint32_t pack_values(float lo, float hi) {
 }
 
 template <int D>
-__global__ void __launch_bounds__(kKvqThreads)
+__global__ void __launch_bounds__(kKvqThreads, kKvqCtas)
 kvq_read_kernel(const __grid_constant__ KvqGeo g, const int64_t* __restrict__ kv_start, const int32_t* __restrict__ first,
                 const int32_t* __restrict__ n_rows) {
-    constexpr int G = D / 16, ROWS = kKvqThreads / G;
-    const int sub = threadIdx.x / G, at = threadIdx.x - sub * G;
-    const int layer = blockIdx.y >> 1, b = blockIdx.z;
-    const bool is_v = blockIdx.y & 1;
+    using U = Unit<D>;
+    constexpr int G = U::G, AHEAD = 4;                // units on their way at a time
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int sub = min(lane / G, U::SLOTS - 1), at = lane - sub * G;
+    const bool mine = lane < U::SLOTS * G;
     wait_for_previous_kernel();
     release_next_kernel();
+    const int layer = blockIdx.y >> 1, b = blockIdx.z;
+    const bool is_v = blockIdx.y & 1;
     const int n = n_rows != nullptr ? min(n_rows[b], g.max_rows) : g.max_rows;
     const long long slot0 = kv_start[b] + (first != nullptr ? first[b] : 0);
-    const unsigned char* codes = (is_v ? g.v_codes : g.k_codes) + layer * g.layer_stride;
+    const unsigned char* codes = (is_v ? g.v_codes : g.k_codes) + layer * g.layer_stride + 4 * at;
     const uint32_t* params = (is_v ? g.v_params : g.k_params) + layer * g.p_layer;
-    unsigned char* rows = (is_v ? g.v_rows : g.k_rows) + layer * g.r_layer + b * g.r_batch;
-    if (sub >= ROWS) return;
-    const long long items = static_cast<long long>(max(n, 0)) * g.n_heads, step = static_cast<long long>(gridDim.x) * ROWS;
-    for (long long i = static_cast<long long>(blockIdx.x) * ROWS + sub; i < items; i += step) {
-        const int r = static_cast<int>(i / g.n_heads), h = static_cast<int>(i - static_cast<long long>(r) * g.n_heads);
-        const long long slot = slot0 + r;
-        if (slot < 0 || slot >= g.total_slots) continue;
-        const uint2 c = __ldcs(reinterpret_cast<const uint2*>(codes + slot * g.slot_stride + h * g.head_stride + 8 * at));
-        const uint32_t p = params[slot * g.p_slot + h * g.p_head];
-        const float s = __uint_as_float(p << 16);
-        const int z = (p >> 16) & 0xf;
-        uint32_t out[8];
+    unsigned char* rows = (is_v ? g.v_rows : g.k_rows) + layer * g.r_layer + b * g.r_batch + 16 * at;
+    Walk unit(g.n_heads, blockIdx.x * U::WARPS + warp, gridDim.x * U::WARPS);
+    while (unit.r * U::SLOTS < n) {
+        uint32_t c[AHEAD][2], p[AHEAD];
+        unsigned char* to[AHEAD];
         #pragma unroll
-        for (int w = 0; w < 2; ++w) {
-            const uint32_t v = w ? c.y : c.x;
-            #pragma unroll
-            for (int j = 0; j < 4; ++j)
-                out[4 * w + j] = pack_values(s * static_cast<float>(static_cast<int>((v >> (4 * j)) & 0xf) - z),
-                                             s * static_cast<float>(static_cast<int>((v >> (16 + 4 * j)) & 0xf) - z));
+        for (int k = 0; k < AHEAD; ++k) {
+            const int r = unit.r * U::SLOTS + sub;
+            const long long slot = slot0 + r;
+            const bool live = mine && r < n && slot >= 0 && slot < g.total_slots;
+            to[k] = live ? rows + r * g.r_row + unit.h * g.r_head : nullptr;
+            if (live) {
+                const uint32_t* const from = reinterpret_cast<const uint32_t*>(codes + slot * g.slot_stride + unit.h * g.head_stride);
+                c[k][0] = __ldcs(from), c[k][1] = __ldcs(from + G);
+                p[k] = params[slot * g.p_slot + unit.h * g.p_head];
+            }
+            unit.step();
         }
-        uint4* dst = reinterpret_cast<uint4*>(rows + r * g.r_row + h * g.r_head) + 2 * at;
-        __stcs(dst, make_uint4(out[0], out[1], out[2], out[3]));
-        __stcs(dst + 1, make_uint4(out[4], out[5], out[6], out[7]));
+        #pragma unroll
+        for (int k = 0; k < AHEAD; ++k) {
+            if (to[k] == nullptr) continue;
+            const float s = __uint_as_float(p[k] << 16);
+            const int z = (p[k] >> 16) & 0xf;
+            #pragma unroll
+            for (int w = 0; w < 2; ++w) {
+                uint32_t out[4];
+                #pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    out[j] = pack_values(s * static_cast<float>(static_cast<int>((c[k][w] >> (4 * j)) & 0xf) - z),
+                                         s * static_cast<float>(static_cast<int>((c[k][w] >> (16 + 4 * j)) & 0xf) - z));
+                __stcs(reinterpret_cast<uint4*>(to[k]) + w * G, make_uint4(out[0], out[1], out[2], out[3]));
+            }
+        }
     }
 }
 
@@ -210,7 +258,7 @@ static int32_t make_geo(const ss_kvq_rows* rows, const ss_kvq_cache* cache, KvqG
     if (!rows || !cache || (rows->max_rows > 0 && (!rows->k || !rows->v))) return SS_ERR_INVALID_ARG;
     const int32_t st = kvq_check_cache(*cache);
     if (st != SS_OK) return st;
-    if (rows->batch < 1 || rows->batch > 65535 || rows->max_rows < 0 || cache->n_layers > 32767) return SS_ERR_INVALID_ARG;
+    if (rows->batch < 1 || rows->batch > 65535 || rows->max_rows < 0 || rows->max_rows > 1 << 30 || cache->n_layers > 32767) return SS_ERR_INVALID_ARG;
     if ((rows->layer_stride | rows->batch_stride | rows->row_stride | rows->head_stride) & 7) return SS_ERR_UNSUPPORTED;
     if (!aligned16(rows->k) || !aligned16(rows->v)) return SS_ERR_INVALID_ARG;
     *g = KvqGeo{static_cast<unsigned char*>(cache->k_codes), static_cast<unsigned char*>(cache->v_codes), cache->k_params, cache->v_params,
@@ -221,11 +269,16 @@ static int32_t make_geo(const ss_kvq_rows* rows, const ss_kvq_cache* cache, KvqG
     return SS_OK;
 }
 
-// CTAs along x: enough for the longest run (the lengths are on the device), at most some sixteen CTAs per SM in all
-static dim3 grid_for(const KvqGeo& g, int batch, long long max_rows, int per_cta) {
-    const long long want = (max_rows * g.n_heads + per_cta - 1) / per_cta, others = 2ll * g.layers * batch;
-    const long long most = std::max(1ll, 16ll * sm_count() / others);
-    return dim3(static_cast<unsigned>(std::max(1ll, std::min(want, most))), static_cast<unsigned>(2 * g.layers), static_cast<unsigned>(batch));
+// CTAs along x, for the longest run (the lengths are on the device).  The start of a CTA costs as much as several steps, so it gets
+// eight of them before there are more (a user's accepted path into 32 layers and back 6.8 us; with one step each 10.7, with two 8.2);
+// and where runs are long there are up to 32 CTAs per SM, eight times what is resident, so that the shorter runs' end early (up to 8:
+// 570 us for the prompts of four users, up to 32: 480).  Sharing the sum of the runs out evenly was slower, whether each CTA
+// took a stretch (550) or all went side by side (740): finding one's place and starting anew in every run costs more than it evens out.
+static dim3 grid_for(const KvqGeo& g, int batch, long long max_rows, int head_dim) {
+    const long long slots = head_dim == 128 ? Unit<128>::SLOTS : head_dim == 80 ? Unit<80>::SLOTS : Unit<64>::SLOTS, warps = kKvqThreads / 32;
+    const long long chunks = ((max_rows + slots - 1) / slots * g.n_heads + warps - 1) / warps, planes = 2ll * g.layers * batch;
+    const long long most = 32ll * sm_count() / planes;
+    return dim3(static_cast<unsigned>(std::max(1ll, std::min((chunks + 7) / 8, most))), static_cast<unsigned>(2 * g.layers), static_cast<unsigned>(batch));
 }
 
 }  // namespace ss
@@ -247,9 +300,8 @@ extern "C" int32_t ss_kvq_write(const ss_kvq_rows* rows, const ss_kvq_cache* cac
     if (overlap && rows->batch > 1024) return SS_ERR_UNSUPPORTED;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     const auto kernel = cache->head_dim == 128 ? ss::kvq_write_kernel<128> : cache->head_dim == 80 ? ss::kvq_write_kernel<80> : ss::kvq_write_kernel<64>;
-    const int per_cta = ss::kKvqThreads / 32 * (32 / (cache->head_dim / 16));
     const long long most = path != nullptr ? std::min<long long>(rows->max_rows, SS_PATH_STRIDE) : rows->max_rows;
-    if (ss::launch_after_previous(kernel, ss::grid_for(g, rows->batch, most, per_cta), dim3(ss::kKvqThreads), s, g, kv_start, kv_len_in,
+    if (ss::launch_after_previous(kernel, ss::grid_for(g, rows->batch, most, cache->head_dim), dim3(ss::kKvqThreads), s, g, kv_start, kv_len_in,
                                   n_rows, path, kv_capacity, overlap ? nullptr : kv_len_out, status) != cudaSuccess)
         return SS_ERR_CUDA;
     if (!overlap) return SS_OK;
@@ -265,7 +317,7 @@ extern "C" int32_t ss_kvq_read(const ss_kvq_cache* cache, const ss_kvq_rows* row
     if (!kv_start) return SS_ERR_INVALID_ARG;
     if (rows->max_rows == 0) return SS_OK;
     const auto kernel = cache->head_dim == 128 ? ss::kvq_read_kernel<128> : cache->head_dim == 80 ? ss::kvq_read_kernel<80> : ss::kvq_read_kernel<64>;
-    const int per_cta = ss::kKvqThreads / (cache->head_dim / 16);
-    return ss::launch_after_previous(kernel, ss::grid_for(g, rows->batch, rows->max_rows, per_cta), dim3(ss::kKvqThreads),
-                                     static_cast<cudaStream_t>(stream), g, kv_start, first, n_rows) == cudaSuccess ? SS_OK : SS_ERR_CUDA;
+    return ss::launch_after_previous(kernel, ss::grid_for(g, rows->batch, rows->max_rows, cache->head_dim), dim3(ss::kKvqThreads),
+                                     static_cast<cudaStream_t>(stream), g, kv_start, first, n_rows) == cudaSuccess
+               ? SS_OK : SS_ERR_CUDA;
 }

@@ -162,6 +162,36 @@ def test_write_lengths_in_place_and_sequences_that_do_not_fit(api):
     assert out.tolist() == [1, 2, 3, 4, 5]
 
 
+@pytest.mark.parametrize("d,H", [(64, 3), (80, 5), (128, 13)])
+def test_write_and_read_of_long_runs(api, d, H):
+    """Runs of many steps of a CTA, beside short ones, and a head count that no CTA's warps divide."""
+    B, layers, M = 3, 2, 2900
+    cache = api.empty_kvq_cache(layers, 6000, H, d)
+    starts, n_rows = _i64([0, 2950, 3100]), _i32([M, 1, 2603])
+    k, v = _rows((layers, B, M, H, d), d), _rows((layers, B, M, H, d), d + 1)
+    out = _i32([0] * B)
+    api.ss_kvq_write(k, v, cache, starts, _i32([0, 0, 0]), n_rows, None, None, out)
+    assert out.tolist() == n_rows.tolist()
+    back = [torch.full_like(k, 7.0) for _ in "kv"]
+    api.ss_kvq_read(cache, back[0], back[1], starts, None, n_rows)
+    for b, n in enumerate(n_rows.tolist()):
+        for x, got in ((k, back[0]), (v, back[1])):
+            # within half a step of the value's own scale where nothing was clamped, a step anywhere; the value is rounded to bf16 once
+            want = x[:, b, :n].double()
+            s = (want.amax(-1).clamp(min=0) - want.amin(-1).clamp(max=0)) / 15 * (1 + 2.0 ** -7)
+            err = (got[:, b, :n].double() - want).abs()
+            assert (err <= (s * (1 + 16 * 2.0 ** -8))[..., None]).all()
+            assert (got[:, b, n:] == 7.0).all()
+    # the same rows one call per sequence give the same cache
+    other = api.empty_kvq_cache(layers, 6000, H, d)
+    for b, n in enumerate(n_rows.tolist()):
+        for at in range(0, n, 701):
+            m = min(701, n - at)
+            api.ss_kvq_write(k[:, b:b + 1, at:at + m], v[:, b:b + 1, at:at + m], other, starts[b:b + 1], _i32([at]), None, None, None, None)
+    for a, c in zip(cache.tensors, other.tensors):
+        assert torch.equal(a, c)
+
+
 def test_read_leaves_what_is_not_asked_for(api):
     d, H = 80, 3
     cache = api.empty_kvq_cache(2, 50, H, d)

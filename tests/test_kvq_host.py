@@ -77,6 +77,17 @@ def test_calls_refuse_rows_they_cannot_read(lib, kw, code):
     assert lib.ss_kvq_read(C.byref(c), C.byref(r), P, None, None, None) == code
 
 
+def test_calls_refuse_sizes_beyond_their_index_arithmetic(lib):
+    for c, r, code in ((_fake_cache(n_heads=65536), _fake_rows(), api.SS_ERR_UNSUPPORTED),
+                       (_fake_cache(), _fake_rows(max_rows=(1 << 30) + 1), api.SS_ERR_INVALID_ARG)):
+        assert lib.ss_kvq_write(C.byref(r), C.byref(c), P, P, None, None, None, None, None, None) == code
+        assert lib.ss_kvq_read(C.byref(c), C.byref(r), P, None, None, None) == code
+    assert lib.ss_msa_attention_kvq(C.byref(_fake_params(cache=_fake_cache(n_heads=65536))), None) == api.SS_ERR_UNSUPPORTED
+    # lengths updated in place are one CTA's work
+    c, r = _fake_cache(), _fake_rows(batch=1025)
+    assert lib.ss_kvq_write(C.byref(r), C.byref(c), P, P, None, None, None, P, None, None) == api.SS_ERR_UNSUPPORTED
+
+
 def test_write_and_read_refuse_missing_arguments(lib):
     c, r = _fake_cache(), _fake_rows()
     bad = api.SS_ERR_INVALID_ARG
