@@ -188,6 +188,11 @@ __device__ __forceinline__ float scale_of(uint32_t word) { return __uint_as_floa
 __device__ __forceinline__ float zero_over_16(uint32_t word) { return __uint_as_float(((word & 0xf0000u) << 3) | 0x3f800000u); }     // 1 + z / 16
 constexpr float kCode = 5.9604644775390625e-08f;                 // 2^-24: what a code counts in an MMA
 
+// Pieces of a lone sequence's unit.  What joining p pieces takes grows with p, what the steps of one take falls as 1 / p: the best p grows
+// as the root of the steps.  (Two heads with 20,000 keys, one row: 14.1 us, in as many pieces as there are CTAs 22.7, with twice the
+// root as the limit 14.9.)  Two steps are not worth a join at all (7.6 against 8.5 us).
+__device__ __forceinline__ int most_pieces(int steps) { return steps < 3 ? 1 : static_cast<int>(3.f * sqrtf(static_cast<float>(steps))); }
+
 // The line of steps as one CTA sees it (every thread, or one warp of a role, works it out for itself)
 // START: what a unit costs before its first step, in steps, for the sake of an even deal.
 template <int ROWS, int CHUNK, int WARPS_LOG2, int START>
@@ -237,7 +242,7 @@ struct Line {
             const int n = __shfl_sync(0xffffffffu, mine.blocks, 0) * groups;
             whole_steps = __shfl_sync(0xffffffffu, steps_of(mine), 0);
             pieces = static_cast<int>(static_cast<uint32_t>(teams) / static_cast<uint32_t>(n));
-            if (pieces > 0) teams = static_cast<long long>(pieces) * n;
+            if (pieces > 0) pieces = min(pieces, most_pieces(whole_steps)), teams = static_cast<long long>(pieces) * n;
         }
         me = static_cast<int>(blockIdx.x) >> team_log2, member = static_cast<int>(blockIdx.x) - (me << team_log2);
         if (me >= teams) return false;
@@ -978,22 +983,23 @@ __global__ void __launch_bounds__(kThreads, NG == 1 ? 3 : 2) msa_attention_kvq_r
             }
             __syncthreads();
             if (joined) {
+                constexpr int kJoinAhead = NG == 1 ? 8 : 4;                   // partial rows that a thread has on their way
                 #pragma unroll 1
                 for (int item = tid; item < items; item += kThreads) {
                     const int hr = item / (D / 8), d0 = (item - hr * (D / 8)) * 8, hd = hr / rows, r = hr - hd * rows;
                     float m = kNoRef, l = 0.f, o[8] = {};
                     #pragma unroll 1
-                    for (int i = share.first; i <= share.last; i += 4) {          // (four partial rows on their way at a time)
-                        float2 st[4];
-                        float4 u[4], v[4];
+                    for (int i = share.first; i <= share.last; i += kJoinAhead) {
+                        float2 st[kJoinAhead];
+                        float4 u[kJoinAhead], v[kJoinAhead];
                         #pragma unroll
-                        for (int k = 0; k < 4; ++k) {
+                        for (int k = 0; k < kJoinAhead; ++k) {
                             const float* src = place(min(i + k, share.last)) + hr * (D + 4);
                             st[k] = __ldcg(reinterpret_cast<const float2*>(src + D));
                             u[k] = __ldcg(reinterpret_cast<const float4*>(src + d0)), v[k] = __ldcg(reinterpret_cast<const float4*>(src + d0) + 1);
                         }
                         #pragma unroll
-                        for (int k = 0; k < 4; ++k)
+                        for (int k = 0; k < kJoinAhead; ++k)
                             if (i + k <= share.last) join_row(o, m, l, st[k], u[k], v[k]);
                     }
                     store_row<D>(a, row0 + r < s.T, row_offset(a, D, b, h0 + hd, row0 + r, s.T), d0, o, m, l);
