@@ -381,14 +381,17 @@ int32_t ss_kvq_read(const ss_kvq_cache* cache, const ss_kvq_rows* rows, const in
  *   q_main, o_main, k_tree, v_tree        bf16 [batch][max_nodes][n_heads][head_dim]
  *   q_spec, k_spec, v_spec, o_spec        bf16 [batch][max_nodes][gamma][n_heads][head_dim]
  *   lse_main, lse_spec                    optional, as there
- * Scores are s_k * sm_scale * <q, c - z>, the weights p * s_v meet V's (c - z) as bf16 (rounded once, as ss_msa_attention
- * rounds p); sums, statistics and both products accumulate in fp32.
+ * Scores are s_k * sm_scale * <q, c - z>.  The weights p * s_v meet V's codes rounded once to 16 bits: with at most 16 query rows
+ * per head (max_nodes * (1 + gamma)) to fp16 under a power of two that follows the largest s_v (11 bits, down to 2^-31 of it), with more to bf16, as
+ * ss_msa_attention rounds p.  Sums, statistics and both products accumulate in fp32.
  * The keys of all heads are dealt out evenly over the GPU, whatever the lengths; a head that several CTAs share leaves partial
  * rows in the workspace, and the last of them to finish joins them in key order: results do not depend on the order of arrival,
  * and no CTA waits for another.  The workspace holds the counters of arrivals, zero between calls, and those rows: calls of
  * different shapes may share one that is large enough for each, in stream order, but it is not one of another entry point's.
  * A sequence with kv_len[b] over its capacity, with slots outside the slab or without nodes is skipped (its outputs are not
- * written); for the first two the status word is set to SS_ERR_CAPACITY.
+ * written); for the first two the status word is set to SS_ERR_CAPACITY.  SS_ERR_DEVICE_TIMEOUT there means that a wait between the warps of
+ * a CTA ran out (about a second): outputs are not written and the workspace is to be zero-filled.
+ * Limits: 65535 sequences and heads, SS_MAX_NODES nodes, SS_MAX_GAMMA streams, head_dim 64, 80 or 128.
  * Errors (nothing launched): SS_ERR_INVALID_ARG, SS_ERR_UNSUPPORTED, SS_ERR_WORKSPACE, SS_ERR_CUDA. */
 typedef struct ss_kvq_attn_params {
     int32_t batch, gamma, max_nodes, layer;

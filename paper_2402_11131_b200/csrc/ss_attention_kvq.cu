@@ -356,7 +356,12 @@ __device__ __forceinline__ void join_row(float (&o)[8], float& m, float& l, cons
 
 // ---- the kernel ---------------------------------------------------------------------------------
 // S^T = K Q^T and O^T = V^T P^T on mma.sync m16n8k16 with the keys (the dimensions) as the 16 rows of A and NG groups of 8 query
-// rows as N: a CTA of 8 warps, each with an online softmax of its own over every eighth chunk of the CTA's piece of a unit.
+// rows as N: a CTA of 4 warps, each with an online softmax of its own over its chunks of the CTA's piece of a unit, its codes on their way
+// through a ring of its own in shared memory.
+// What bounds it: with one row the bytes (64 users with up to 8191 keys: 229 us for 178 of HBM), from some eight rows on, and in long
+// sequences, the instructions that make fragments of codes and weights of scores, which is why codes are taken as they lie
+// (below: a mask, no conversion) and why keys are the wide side of the products.  Short calls are a chain of latencies: lengths, codes,
+// a few steps, partial rows and their join.
 //
 // Fragments, for lane 4 g + c.  Which key is row g of A, and which dimensions are the columns that c holds, is free as long as both
 // operands agree; the choice here lets a lane read runs of codes and turn them into fragments in place:
@@ -370,7 +375,7 @@ struct KvqGeometry {
     static constexpr int kRowBytes = D / 2;
     static constexpr int kWordsK = kMain / 32;                   // words of 8 codes per lane and key
     static constexpr int kWordsV = kMain / 64;
-    static constexpr int kSteps = D / 16, kTiles = D / 16;
+    static constexpr int kTiles = D / 16;
     static constexpr int kCopy = D == 80 ? 8 : 16;               // bytes per asynchronous copy
     static constexpr int kCodeBytes = kChunk * kRowBytes;
     static constexpr int kStageBytes = 2 * kCodeBytes + 2 * kChunk * 4;
@@ -1025,6 +1030,11 @@ struct KvqPlan {
 };
 static KvqPlan kvq_plan(const ss_kvq_attn_params& p) {
     const int rows = q_rows(p);
+    // Up to 8 rows the rows are one group: three CTAs per SM, and nothing is spent on the second group's padding (16 users with 512 to 4096
+    // keys, a row each: 43 us, with two groups 50; 32 heads of 50,000 keys, 8 rows: 57 and 64; 2048 keys: 14.4 and 11.9, the other way round).
+    // From 17 rows on tcgen05 is faster at all lengths (32 rows: 16 users 86 us, by two groups of 16 rows 121; 50,000 keys 107 and 125;
+    // 512 keys 12.9 and 14.3), up to 16 it is slower in all but short sequences (12 rows: 84 and 64 us; 105 and 68; 512 keys 12.1 and 12.6).
+    // 32 rows in the kernel for 64 cost a sixth (102 us).
     KvqPlan k{0, rows <= 8 ? 1 : 2, 0, 0};
     if (rows > 16) k.tile = rows <= 32 ? 32 : 64;
     k.block = k.tile > 0 ? k.tile : 8 * k.groups;

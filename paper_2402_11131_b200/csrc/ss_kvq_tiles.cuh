@@ -9,10 +9,19 @@
 // Lane 32 w + x of V^T and O^T (w < D / 32) holds, for x < 16, the low codes of byte 16 w + x of a row, else the high codes of
 // byte 16 w + x - 16.
 //
-// 26 warps: 0..3 copy the codes of K and V and turn K's into operands, 4..7 V's, 8..23 softmax (four groups of four, each a quarter of
+// 28 warps: 0..3 copy the codes of K and V and turn K's into operands, 4..7 V's, 8..23 softmax (four groups of four, each a quarter of
 // the rows, thread = key), 24 issues the MMAs, 25..27 prepare: they walk the list of units one ahead of the others, who find a
 // unit's query rows and what else they need to know of it in shared memory.  Two buffers each for K, V, S, P and the query rows, so that
 // the roles work on different tiles and units.
+//
+// What bounds it: each role's chain of latencies per tile (loads, conversion, TMEM round trip, hand-over), some 1800 to 2300 cycles of 128 keys
+// by 64 rows whatever the role, where the MMAs need 300 and the exponentials 512: 16 users with 512 to 4096 keys 107 us for 27.5 of HBM.
+// On the way there: one softmax group per 32 rows 143 us, four 130; weights without a vote on the references 118 (a sum per tile
+// decides) against 112; a unit's start counted in the deal of work 112 for 131; own warps for what comes before a unit 107.
+// Rounding: keys and values are whole numbers below 2^8 in bf16, exactly; queries enter as they are; a weight p s_v is rounded once to
+// bf16 (2^-8 of itself), as the bf16 attention rounds p.  The sums of q (128 + c) are larger than those of q (c - z) by some 143 over
+// |c - z|: fp32 accumulators lose 2^-24 of them per step of 16, 10^-4 of a score unit for normal queries and keys, a tenth of what the
+// weights' rounding does.
 #pragma once
 #include "ss_tcgen05.cuh"
 
@@ -29,7 +38,7 @@ struct TileGeo {
     static constexpr int kPitch = D == 128 ? 64 : D == 80 ? 48 : 32;         // bytes of a key's codes in shared memory (16-byte aligned)
     static constexpr int kCopy = D == 80 ? 8 : 16, kPer = D / 2 / kCopy;     // asynchronous copies per key
     static constexpr int kWords = D / 8;
-        static constexpr int kQuads = (D + 31) / 32;                  // warps that have V lanes
+    static constexpr int kQuads = (D + 31) / 32;                  // warps that have V lanes
     static constexpr int kCodes = kTileOfKeys * kPitch;
     static constexpr int kStages = 4, kParams = 8;
     static constexpr int kBoxes = D > 64 ? 2 : 1, kBox = N * 128;
@@ -113,12 +122,6 @@ struct TileCtrl {
 
 __device__ __forceinline__ void tile_wait(uint32_t bar, uint32_t parity, int* abort, int* status) {
     if (!mbar_try(bar, parity)) mbar_wait_slow(bar, parity, abort, status);
-}
-// 128 threads agree on "any"
-__device__ __forceinline__ bool any_of_group(int id, bool x) {
-    uint32_t r;
-    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %2, 0;\n\tbar.red.or.pred q, %1, 128, p;\n\tselp.u32 %0, 1, 0, q;\n\t}" : "=r"(r) : "r"(id), "r"(static_cast<uint32_t>(x)) : "memory");
-    return r != 0u;
 }
 template <int C>
 __device__ __forceinline__ void tmem_load(uint32_t addr, uint32_t (&r)[C]) {
@@ -208,6 +211,59 @@ __device__ __forceinline__ void prefetch_extra(const KvqArgs& a, const Extra& x,
     if (D > 64) prefetch_l2(src + D - 8);
 }
 
+// A unit's query rows as THREADS threads put them into shared memory at `rows_at`, what 128 + z meets, and which rows see which node.
+// BATCH: loads of a thread on their way at once; `sums`: [row][16] partial sums
+template <int D, int N, int THREADS, int BATCH>
+static __device__ __noinline__ void prepare_rows(const KvqArgs& a, TileUnit& u, uint32_t rows_at, float* sums, int t, int bar) {
+    using G = TileGeo<D, N>;
+    constexpr int kItems = (N * (D / 8) + THREADS - 1) / THREADS;
+    const int rows = u.rows, T = u.T, row0 = u.row0, h = u.head, b = u.b, lane = t & 31;
+    // the rows that see a node: every warp takes its share of the nodes
+    unsigned long long see[2] = {};
+    #pragma unroll
+    for (int half = 0; half < (N + 31) / 32; ++half) {
+        const int n = 32 * half + lane;
+        if (n < rows) see[half] = a.trees[b].anc_mask[row_of(row0 + n, T, a.gamma).t];
+    }
+    #pragma unroll 1
+    for (int i = 0; i < kItems; i += BATCH) {
+        uint4 v[BATCH];
+        #pragma unroll
+        for (int q = 0; q < BATCH; ++q) {
+            const int item = (i + q) * THREADS + t, r = item / (D / 8), at = item - r * (D / 8), row = row0 + r;
+            v[q] = make_uint4(0u, 0u, 0u, 0u);
+            if (r < rows) v[q] = *reinterpret_cast<const uint4*>((row < T ? a.q_main : a.q_spec) + row_offset(a, D, b, h, row, T) + 8 * at);
+        }
+        #pragma unroll
+        for (int q = 0; q < BATCH; ++q) {
+            const int item = (i + q) * THREADS + t, r = item / (D / 8), at = item - r * (D / 8);
+            if (item >= N * (D / 8)) break;
+            const uint32_t pair[4] = {v[q].x, v[q].y, v[q].z, v[q].w};
+            float sum = 0.f;
+            #pragma unroll
+            for (int n = 0; n < 4; ++n) sum += __uint_as_float(pair[n] << 16) + __uint_as_float(pair[n] & 0xffff0000u);
+            st_shared_v4(rows_at + (at >> 3) * G::kBox + r * 128 + (((at & 7) ^ (r & 7)) << 4), v[q].x, v[q].y, v[q].z, v[q].w);
+            sums[r * 16 + at] = sum;
+        }
+    }
+    for (int e = t >> 5; e < T; e += THREADS / 32) {
+        const uint32_t lo = __ballot_sync(0xffffffffu, see[0] >> e & 1ull), hi = N > 32 ? __ballot_sync(0xffffffffu, see[1] >> e & 1ull) : 0u;
+        if (lane == 0) u.see[e] = static_cast<unsigned long long>(hi) << 32 | lo;
+    }
+    named_barrier(bar, THREADS);
+    if (t < N) {
+        float x = 0.f;
+        #pragma unroll
+        for (int i = 0; i < D / 8; ++i) x += sums[t * 16 + i];
+        x = -x;
+        const float t0 = round_bf16(x), t1 = round_bf16(x - t0), t2 = (x - t0) - t1;
+        const uint32_t row = rows_at + G::kBoxes * G::kBox + (t >> 3) * 256 + (t & 7) * 16;
+        st_shared_v4(row, pack2_bf16(t0, t1), pack2_bf16(t2, 0.f), 0u, 0u);
+        st_shared_v4(row + 128, 0u, 0u, 0u, 0u);
+        u.out[t] = t < rows ? row_offset(a, D, b, h, row0 + t, T) : 0;
+    }
+}
+
 template <int D, int N>
 __global__ void __launch_bounds__(kTileThreads, 1) msa_attention_kvq_tiles_kernel(const __grid_constant__ KvqArgs a) {
     using G = TileGeo<D, N>;
@@ -231,22 +287,37 @@ __global__ void __launch_bounds__(kTileThreads, 1) msa_attention_kvq_tiles_kerne
         mbar_init(smem_u32(&c.o_free), kTileSoftmax), mbar_init(smem_u32(&c.drain), 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    wait_for_previous_kernel();
-    release_next_kernel();
-    Line<N, kTileOfKeys, 0, kTileStart> line;                    // (the planning warp's)
-    if (warp == kPlanWarp) {
-        const bool any = line.begin(a, lane);
-        if (lane == 0) c.any = any;
-    }
-    __syncthreads();
-    if (c.any == 0) return;
     if (warp == kMmaWarp) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&c.tmem)) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
     }
+    wait_for_previous_kernel();
+    release_next_kernel();
+    Line<N, kTileOfKeys, 0, kTileStart> line;                    // (the planning warp's)
+    const auto make_plan = [&](TileUnit& u, bool more) {         // of the unit that the line is at
+        if (lane != 0) return;
+        u.done = !more;
+        if (!more) return;
+        const Seq& s = line.s;
+        const Pieces share(line);
+        u.L = s.L, u.T = s.T, u.prefix = prefix_chunks<kTileOfKeys>(s.L), u.from = line.from, u.to = line.to, u.start = s.start;
+        u.head = min(line.head0, a.n_heads - 1), u.real = line.head0 < a.n_heads, u.row0 = line.row0, u.rows = min(N, s.rows - line.row0), u.b = line.b;
+        u.whole = line.whole(), u.first = share.first, u.last = share.last, u.second = share.second;
+        u.me = line.me, u.member = line.member, u.team = line.team_log2;
+        u.extra = extra_of(a, s, line.row0, N);
+    };
+    if (warp == kPlanWarp) {
+        const bool any = line.begin(a, lane);
+        if (lane == 0) c.any = any;
+        if (any) make_plan(c.unit[0], line.next(a));
+    }
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
+    if (c.any == 0) {
+        if (warp == kMmaWarp) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(c.tmem));
+        return;
+    }
     const uint32_t tmem = uniform(c.tmem), lanes = static_cast<uint32_t>(32 * quad) << 16;
     // (a wait that runs out leaves the roles in step: everyone goes through the same tiles without waiting, and no output is written)
     const auto wait = [&](unsigned long long& bar, uint32_t parity) { tile_wait(smem_u32(&bar), parity, &c.abort, status); };
@@ -487,6 +558,13 @@ __global__ void __launch_bounds__(kTileThreads, 1) msa_attention_kvq_tiles_kerne
         const uint32_t weights = smem + G::oP + key * 128;        // the key's row of P^T
         // TMEM lane to dimension
         const int byte = 16 * quad + (lane & 15), dim = 8 * (byte >> 2) + ((byte & 1) << 2) + ((byte >> 1) & 1) + ((lane >> 4) << 1);
+        if (!plan_of(0).done) {
+            // (partial sums where the weights will be)
+            prepare_rows<D, N, kTileSoftmax, 2>(a, c.unit[0], smem + G::oQ, reinterpret_cast<float*>(smem_raw + G::oP), tid - 256, 3 + kTileGroups);
+            fence_async_smem();
+            named_barrier(3 + kTileGroups, kTileSoftmax);
+            if (tid == 256) mbar_arrive(smem_u32(&c.rows_full[0]));
+        }
         for (;; ++unit) {
             const TileUnit& u = plan_of(unit);
             if (u.done) break;
@@ -767,84 +845,29 @@ __global__ void __launch_bounds__(kTileThreads, 1) msa_attention_kvq_tiles_kerne
         // ---- preparing ----------------------------------------------------------------------
         const int t = tid - 32 * kPlanWarp, place = warp - kPlanWarp;
         float* const sums = reinterpret_cast<float*>(smem_raw + G::oSums);           // [row][16] of partial sums of x
-        constexpr int kItems = (N * (D / 8) + kTilePrepare - 1) / kTilePrepare, kBatch = 6;
         for (uint32_t unit = 0;; ++unit) {
             TileUnit& u = c.unit[unit & 1];
             const uint32_t rows_at = smem + G::oQ + (unit & 1) * G::kRowsOfUnit;
             if (place == 0) {
-                const bool more = line.next(a);
-                // (a unit's rows are free when all are done with the plan: its last S is complete then)
-                if (unit >= 2) wait(c.plan_free[unit & 1], ((unit - 2) >> 1) & 1);
-                if (lane == 0) {
-                    u.done = !more;
-                    if (more) {
-                        const Seq& s = line.s;
-                        const Pieces share(line);
-                        u.L = s.L, u.T = s.T, u.prefix = prefix_chunks<kTileOfKeys>(s.L), u.from = line.from, u.to = line.to, u.start = s.start;
-                        u.head = min(line.head0, a.n_heads - 1), u.real = line.head0 < a.n_heads, u.row0 = line.row0, u.rows = min(N, s.rows - line.row0), u.b = line.b;
-                        u.whole = line.whole(), u.first = share.first, u.last = share.last, u.second = share.second;
-                        u.me = line.me, u.member = line.member, u.team = line.team_log2;
-                        u.extra = extra_of(a, s, line.row0, N);
-                    }
+                if (unit > 0) {                      // (the first unit's plan is there)
+                    const bool more = line.next(a);
+                    // (a unit's rows are free when all are done with the plan: its last S is complete then)
+                    if (unit >= 2) wait(c.plan_free[unit & 1], ((unit - 2) >> 1) & 1);
+                    make_plan(u, more);
                 }
             }
             named_barrier(4 + kTileGroups, kTilePrepare);
             if (t == 0) mbar_arrive(smem_u32(&c.plan_full[unit & 1]));
             if (u.done) break;
             // what lies behind the prefix comes to L2 meanwhile
-            const int rows = u.rows, T = u.T, row0 = u.row0, h = u.head, b = u.b;
             if (u.to > u.prefix) {
                 for (int e = t; e < kTileOfKeys; e += kTilePrepare) {
-                    prefetch_extra(a, u.extra, D, b, h, e, a.k_tree, a.k_spec);
-                    prefetch_extra(a, u.extra, D, b, h, e, a.v_tree, a.v_spec);
+                    prefetch_extra(a, u.extra, D, u.b, u.head, e, a.k_tree, a.k_spec);
+                    prefetch_extra(a, u.extra, D, u.b, u.head, e, a.v_tree, a.v_spec);
                 }
             }
-            // query rows, 16 bytes at a time, some of a thread's on their way at once
-            #pragma unroll 1
-            for (int i = 0; i < kItems; i += kBatch) {
-                uint4 v[kBatch];
-                #pragma unroll
-                for (int q = 0; q < kBatch; ++q) {
-                    const int item = (i + q) * kTilePrepare + t, r = item / (D / 8), at = item - r * (D / 8), row = row0 + r;
-                    v[q] = make_uint4(0u, 0u, 0u, 0u);
-                    if (r < rows) v[q] = *reinterpret_cast<const uint4*>((row < T ? a.q_main : a.q_spec) + row_offset(a, D, b, h, row, T) + 8 * at);
-                }
-                #pragma unroll
-                for (int q = 0; q < kBatch; ++q) {
-                    const int item = (i + q) * kTilePrepare + t, r = item / (D / 8), at = item - r * (D / 8);
-                    if (item >= N * (D / 8)) break;
-                    const uint32_t pair[4] = {v[q].x, v[q].y, v[q].z, v[q].w};
-                    float sum = 0.f;
-                    #pragma unroll
-                    for (int n = 0; n < 4; ++n) sum += __uint_as_float(pair[n] << 16) + __uint_as_float(pair[n] & 0xffff0000u);
-                    st_shared_v4(rows_at + (at >> 3) * G::kBox + r * 128 + (((at & 7) ^ (r & 7)) << 4), v[q].x, v[q].y, v[q].z, v[q].w);
-                    sums[r * 16 + at] = sum;
-                }
-            }
-            named_barrier(4 + kTileGroups, kTilePrepare);
-            // what 128 + z meets
-            if (t < N) {
-                float x = 0.f;
-                #pragma unroll
-                for (int i = 0; i < D / 8; ++i) x += sums[t * 16 + i];
-                x = -x;
-                const float t0 = round_bf16(x), t1 = round_bf16(x - t0), t2 = (x - t0) - t1;
-                const uint32_t row = rows_at + G::kBoxes * G::kBox + (t >> 3) * 256 + (t & 7) * 16;
-                st_shared_v4(row, pack2_bf16(t0, t1), pack2_bf16(t2, 0.f), 0u, 0u);
-                st_shared_v4(row + 128, 0u, 0u, 0u, 0u);
-                u.out[t] = t < rows ? row_offset(a, D, b, h, row0 + t, T) : 0;
-            }
-            // the rows that see a node: every warp takes a third of the nodes
-            unsigned long long see[2] = {};
-            #pragma unroll
-            for (int half = 0; half < (N + 31) / 32; ++half) {
-                const int n = 32 * half + lane;
-                if (n < rows) see[half] = a.trees[b].anc_mask[row_of(row0 + n, T, a.gamma).t];
-            }
-            for (int e = place; e < T; e += 3) {
-                const uint32_t lo = __ballot_sync(0xffffffffu, see[0] >> e & 1ull), hi = N > 32 ? __ballot_sync(0xffffffffu, see[1] >> e & 1ull) : 0u;
-                if (lane == 0) u.see[e] = static_cast<unsigned long long>(hi) << 32 | lo;
-            }
+            if (unit == 0) continue;                 // (the softmax warps, idle then, fetch the first unit's rows in a third of the time)
+            prepare_rows<D, N, kTilePrepare, 6>(a, u, rows_at, sums, t, 4 + kTileGroups);
             fence_async_smem();
             named_barrier(4 + kTileGroups, kTilePrepare);
             if (t == 0) mbar_arrive(smem_u32(&c.rows_full[unit & 1]));           // (the query rows, and with them `out` and `see`)
