@@ -217,10 +217,15 @@ struct Line {
     }
     // false: nothing for this CTA.  All lanes of a warp come here.
     __device__ __forceinline__ bool begin(const KvqArgs& a, int lane) {
+        const bool lone = a.batch == 1;              // (every lane has it: no sums, no searches)
         long long chunks = 0, blocks = 0;            // of all sequences, for one head
         Seq mine;                                    // the lane's sequence of the first 32
+        if (lone) {
+            mine = load_seq<ROWS, CHUNK>(a, 0);
+            chunks = static_cast<long long>(mine.chunks) * mine.blocks, blocks = mine.blocks;
+        }
         #pragma unroll 1
-        for (int b0 = 0; b0 < a.batch; b0 += 32) {
+        for (int b0 = 0; b0 < (lone ? 0 : a.batch); b0 += 32) {
             const Seq q = b0 + lane < a.batch ? load_seq<ROWS, CHUNK>(a, b0 + lane) : Seq{};
             if (b0 == 0) mine = q;
             chunks += warp_sum(static_cast<long long>(q.chunks) * q.blocks);
@@ -229,18 +234,18 @@ struct Line {
         const Shape shape = shape_of<WARPS_LOG2>(a, chunks, blocks);
         heads_log2 = shape.heads, team_log2 = shape.team, steps_log2 = WARPS_LOG2 - shape.heads;
         groups = (a.n_heads + (1 << (heads_log2 + team_log2)) - 1) >> (heads_log2 + team_log2);
-        start = a.batch == 1 ? 0 : START;
-        total = 0;
+        start = lone ? 0 : START;
+        total = lone ? line_of(mine) : 0;
         #pragma unroll 1
-        for (int b0 = 0; b0 < a.batch; b0 += 32)
+        for (int b0 = 0; b0 < (lone ? 0 : a.batch); b0 += 32)
             total += warp_sum(b0 + lane < a.batch ? line_of(b0 == 0 ? mine : load_seq<ROWS, CHUNK>(a, b0 + lane)) : 0);
         long long teams = min(static_cast<long long>(gridDim.x >> team_log2), total);
         // one sequence with fewer units than teams: every unit in the same number of pieces, so that all heads' pieces read the same slots
         // at the same time
         pieces = whole_steps = 0;
-        if (a.batch == 1 && total > 0) {
-            const int n = __shfl_sync(0xffffffffu, mine.blocks, 0) * groups;
-            whole_steps = __shfl_sync(0xffffffffu, steps_of(mine), 0);
+        if (lone && total > 0) {
+            const int n = mine.blocks * groups;
+            whole_steps = steps_of(mine);
             pieces = static_cast<int>(static_cast<uint32_t>(teams) / static_cast<uint32_t>(n));
             if (pieces > 0) pieces = min(pieces, most_pieces(whole_steps)), teams = static_cast<long long>(pieces) * n;
         }
@@ -252,7 +257,7 @@ struct Line {
         // the sequence that holds the piece's first step
         base = 0, b = 0;
         #pragma unroll 1
-        for (int b0 = 0; b0 < a.batch; b0 += 32) {
+        for (int b0 = 0; b0 < (lone ? 0 : a.batch); b0 += 32) {
             const long long own = b0 + lane < a.batch ? line_of(b0 == 0 ? mine : load_seq<ROWS, CHUNK>(a, b0 + lane)) : 0;
             long long upto = own;
             #pragma unroll
@@ -269,7 +274,9 @@ struct Line {
             }
             base += __shfl_sync(0xffffffffu, upto, 31);
         }
-        if (b < 32) {                                // (a lane has it)
+        if (lone) {
+            s = mine;
+        } else if (b < 32) {                         // (a lane has it)
             s.L = __shfl_sync(0xffffffffu, mine.L, b), s.T = __shfl_sync(0xffffffffu, mine.T, b), s.rows = __shfl_sync(0xffffffffu, mine.rows, b);
             s.blocks = __shfl_sync(0xffffffffu, mine.blocks, b), s.chunks = __shfl_sync(0xffffffffu, mine.chunks, b), s.start = __shfl_sync(0xffffffffu, mine.start, b);
         } else {
