@@ -751,7 +751,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) msa_attention_kvq_tiles_kerne
                     #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         const int mi = m0 + i, wi = mi / (C / 8), n = group * C + 8 * (mi - wi * (C / 8)) + (lane >> 2);
-                        if (n < rows && ok)
+                        if (n < rows && wi < D / 8 && ok)        // (80: ten words of eight rows are no multiple of four matrices)
                             *reinterpret_cast<uint32_t*>((n < mains ? a.o_main : a.o_spec) + u.out[n] + 8 * wi + 2 * (lane & 3)) = q[i];
                     }
                 }

@@ -307,6 +307,32 @@ def test_attention_over_lengths_and_trees(api, d, nodes, gamma):
 
 
 @pytest.mark.parametrize("d", [64, 80, 128])
+@pytest.mark.parametrize("nodes,gamma", [(17, 0), (20, 0), (32, 0), (8, 2), (6, 4), (11, 1), (5, 3)])
+def test_attention_of_blocks_of_up_to_32_rows(api, d, nodes, gamma):
+    B = len(LENGTHS)
+    counts = [nodes if b % 3 else max(1, nodes - b) for b in range(B)]
+    x = Layer(api, B, 3, d, LENGTHS, counts, gamma, seed=2 * d + nodes)
+    x.run()
+    x.check()
+
+
+@pytest.mark.parametrize("d", [64, 80, 128])
+@pytest.mark.parametrize("rows", [1, 7, 8, 9, 16, 17, 19, 32, 33, 50, 64])
+@pytest.mark.parametrize("length", [5, 112, 900])
+def test_attention_writes_its_rows_and_nothing_else(api, d, rows, length):
+    """One sequence (whole heads, and heads in pieces), odd heads; what lies around the outputs is left as it was."""
+    x = Layer(api, 1, 5, d, [length], [rows], 0, seed=rows + length)
+    room = torch.full((x.o_main.numel() + 2048,), 77.0, dtype=torch.bfloat16, device="cuda")
+    room_lse = torch.full((x.lse_main.numel() + 2048,), 77.0, device="cuda")
+    x.o_main = room[1024:-1024].view(x.o_main.shape)
+    x.lse_main = room_lse[1024:-1024].view(x.lse_main.shape)
+    x.run()
+    x.check()
+    for t in (room, room_lse):
+        assert (t[:1024] == 77.0).all() and (t[-1024:] == 77.0).all()
+
+
+@pytest.mark.parametrize("d", [64, 80, 128])
 @pytest.mark.parametrize("H,length,nodes,gamma,order", [(32, 2048, 1, 0, "slots"), (1, 5000, 4, 0, "heads"), (2, 3001, 64, 0, "slots"),
                                                         (7, 1000, 40, 1, "heads"), (32, 517, 16, 3, "slots"), (40, 100, 64, 4, "heads"),
                                                         (148, 33, 2, 0, "slots"), (1, 1, 1, 0, "slots"), (1, 0, 1, 0, "heads")])
