@@ -1,7 +1,9 @@
 // Rows into and out of a cache held in 4 bits (format and layout: ss_msa.h).  Compiled without fast-math: scales and codes are
 // defined bit by bit.
 //
-// Both kernels stream: HBM bounds them.  A thread holds 16 values, 8 at dimension 8 at and 8 at D / 2 + 8 at: a row of a head is 4, 5
+// Both kernels stream: HBM bounds them, with the instructions per value (13 of a write, 78 % of the issue slots) close behind.  Four
+// users' prompts into eight layers, 8240 rows of 32 x 128 each: written in 252 us (1.32 GB, 5.2 TB/s), read back in 220 (1.31 GB, 6.0 TB/s).
+// One layer of 2048 slots is read in 7.9 us, 4 of them the launch and one trip to memory.  A thread holds 16 values, 8 at dimension 8 at and 8 at D / 2 + 8 at: a row of a head is 4, 5
 // or 8 neighbouring lanes that read (or write) runs of 16 bytes next to each other, and find the row's extremes with three exchanges.
 //
 // The arithmetic of the scale.  s is the smallest bf16 with 15 s >= hi - lo.  15 s is an fp32 number, so that is 15 s >= t with t the
@@ -121,9 +123,24 @@ struct Walk {
         r = first / heads, h = first - r * heads;
         dr = by / heads, dh = by - dr * heads;
     }
-    __device__ __forceinline__ void step() {
+    // true: on to other slots
+    __device__ __forceinline__ bool step() {
         r += dr, h += dh;
-        if (h >= n_heads) h -= n_heads, ++r;
+        const bool on = h >= n_heads;
+        if (on) h -= n_heads, ++r;
+        return on;
+    }
+};
+
+// Where a lane's row of the unit lies, for strides of a slot and of a head: sums along the walk, not products
+struct Trail {
+    long long at, by, wrap;
+    __device__ __forceinline__ Trail(const Walk& w, int slots, int sub, long long slot_stride, long long head_stride)
+        : at((static_cast<long long>(w.r) * slots + sub) * slot_stride + w.h * head_stride), by(static_cast<long long>(w.dr) * slots * slot_stride + w.dh * head_stride),
+          wrap(slots * slot_stride - w.n_heads * head_stride) {}
+    __device__ __forceinline__ void step(bool on) {
+        at += by;
+        if (on) at += wrap;
     }
 };
 
@@ -153,34 +170,49 @@ kvq_write_kernel(const __grid_constant__ KvqGeo g, const int64_t* __restrict__ k
     const unsigned char* rows = (is_v ? g.v_rows : g.k_rows) + layer * g.r_layer + b * g.r_batch + 16 * at;
     unsigned char* codes = (is_v ? g.v_codes : g.k_codes) + layer * g.layer_stride + slot0 * g.slot_stride + 4 * at;
     uint32_t* params = (is_v ? g.v_params : g.k_params) + layer * g.p_layer + slot0 * g.p_slot;
-    // the next unit's rows are on their way while these are turned into codes
     Walk unit(g.n_heads, blockIdx.x * U::WARPS + warp, gridDim.x * U::WARPS);
+    Trail row_at(unit, U::SLOTS, sub, g.r_row, g.r_head), code_at(unit, U::SLOTS, sub, g.slot_stride, g.head_stride), word_at(unit, U::SLOTS, sub, g.p_slot, g.p_head);
+    // (lanes without a row have its last contents: a row's lanes have one or none together)
     const auto fetch = [&](uint4 (&x)[2]) {
         const int r = unit.r * U::SLOTS + sub;
-        int src = r;
-        if (nodes != nullptr && r < n) src = nodes[r];
-        const bool live = mine && r < n && src >= 0 && src < g.max_rows;
-        if (live) {
-            const uint4* p = reinterpret_cast<const uint4*>(rows + src * g.r_row + unit.h * g.r_head);
-            x[0] = __ldcs(p), x[1] = __ldcs(p + G);
+        bool live = mine && r < n;
+        const unsigned char* src = rows + row_at.at;
+        if (nodes == nullptr) {
+            live = live && r < g.max_rows;
+        } else if (live) {
+            const int node = nodes[r];
+            live = node >= 0 && node < g.max_rows;
+            src = rows + node * g.r_row + unit.h * g.r_head;
         }
+        if (live) x[0] = __ldcs(reinterpret_cast<const uint4*>(src)), x[1] = __ldcs(reinterpret_cast<const uint4*>(src) + G);
         return live;
     };
-    uint4 x[2] = {};
-    bool live = fetch(x);
-    while (unit.r * U::SLOTS < n) {
-        const int r = unit.r * U::SLOTS + sub, h = unit.h;
-        unit.step();
-        uint4 next[2] = {};
-        const bool next_live = fetch(next);
+    const auto store = [&](const uint4 (&x)[2], bool live, unsigned char* to, uint32_t* word_to) {
         uint32_t c[2];
         const uint32_t word = quantise_row<D>(x, base, at, c);
         if (live) {
-            uint32_t* const to = reinterpret_cast<uint32_t*>(codes + r * g.slot_stride + h * g.head_stride);
-            to[0] = c[0], to[G] = c[1];
-            if (at == 0) params[r * g.p_slot + h * g.p_head] = word;
+            reinterpret_cast<uint32_t*>(to)[0] = c[0], reinterpret_cast<uint32_t*>(to)[G] = c[1];
+            if (at == 0) *word_to = word;
         }
-        x[0] = next[0], x[1] = next[1], live = next_live;
+    };
+    // two units' rows in turn: the next ones are on their way while these are turned into codes
+    uint4 x[2] = {}, y[2] = {};
+    bool live = fetch(x);
+    while (unit.r * U::SLOTS < n) {
+        unsigned char* to = codes + code_at.at;
+        uint32_t* word_to = params + word_at.at;
+        const auto step = [&] {
+            const bool on = unit.step();
+            row_at.step(on), code_at.step(on), word_at.step(on);
+        };
+        step();
+        const bool more = fetch(y);
+        store(x, live, to, word_to);
+        if (unit.r * U::SLOTS >= n) break;
+        to = codes + code_at.at, word_to = params + word_at.at;
+        step();
+        live = fetch(x);
+        store(y, more, to, word_to);
     }
 }
 
@@ -196,9 +228,15 @@ __global__ void kvq_len_kernel(const __grid_constant__ KvqGeo g, const int64_t* 
     if (b < batch) kv_len_out[b] = fits ? L + n : L;
 }
 
-__device__ __forceinline__ uint32_t pack_values(float lo, float hi) {
-    const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
-    return *reinterpret_cast<const uint32_t*>(&v);
+__device__ __forceinline__ uint32_t sub_bf16x2(uint32_t a, uint32_t b) {
+    uint32_t r;
+    asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+__device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b) {
+    uint32_t r;
+    asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
 }
 
 template <int D>
@@ -206,7 +244,7 @@ __global__ void __launch_bounds__(kKvqThreads, kKvqCtas)
 kvq_read_kernel(const __grid_constant__ KvqGeo g, const int64_t* __restrict__ kv_start, const int32_t* __restrict__ first,
                 const int32_t* __restrict__ n_rows) {
     using U = Unit<D>;
-    constexpr int G = U::G, AHEAD = 4;                // units on their way at a time
+    constexpr int G = U::G, AHEAD = D == 80 ? 3 : 4;  // units on their way at a time (as many as 64 registers hold)
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int sub = min(lane / G, U::SLOTS - 1), at = lane - sub * G;
     const bool mine = lane < U::SLOTS * G;
@@ -219,35 +257,37 @@ kvq_read_kernel(const __grid_constant__ KvqGeo g, const int64_t* __restrict__ kv
     const unsigned char* codes = (is_v ? g.v_codes : g.k_codes) + layer * g.layer_stride + 4 * at;
     const uint32_t* params = (is_v ? g.v_params : g.k_params) + layer * g.p_layer;
     unsigned char* rows = (is_v ? g.v_rows : g.k_rows) + layer * g.r_layer + b * g.r_batch + 16 * at;
+    codes += slot0 * g.slot_stride, params += slot0 * g.p_slot;
+    // rows whose slots lie in the slab
+    const int lo = static_cast<int>(min(max(-slot0, 0ll), static_cast<long long>(max(n, 0)))), hi = static_cast<int>(max(min(g.total_slots - slot0, static_cast<long long>(n)), 0ll));
     Walk unit(g.n_heads, blockIdx.x * U::WARPS + warp, gridDim.x * U::WARPS);
-    while (unit.r * U::SLOTS < n) {
+    Trail row_at(unit, U::SLOTS, sub, g.r_row, g.r_head), code_at(unit, U::SLOTS, sub, g.slot_stride, g.head_stride), word_at(unit, U::SLOTS, sub, g.p_slot, g.p_head);
+    while (unit.r * U::SLOTS < hi) {
         uint32_t c[AHEAD][2], p[AHEAD];
-        unsigned char* to[AHEAD];
+        unsigned char* to[AHEAD];                     // null: nothing to do
         #pragma unroll
         for (int k = 0; k < AHEAD; ++k) {
             const int r = unit.r * U::SLOTS + sub;
-            const long long slot = slot0 + r;
-            const bool live = mine && r < n && slot >= 0 && slot < g.total_slots;
-            to[k] = live ? rows + r * g.r_row + unit.h * g.r_head : nullptr;
+            const bool live = mine && r >= lo && r < hi;
+            to[k] = live ? rows + row_at.at : nullptr;
             if (live) {
-                const uint32_t* const from = reinterpret_cast<const uint32_t*>(codes + slot * g.slot_stride + unit.h * g.head_stride);
+                const uint32_t* const from = reinterpret_cast<const uint32_t*>(codes + code_at.at);
                 c[k][0] = __ldcs(from), c[k][1] = __ldcs(from + G);
-                p[k] = params[slot * g.p_slot + unit.h * g.p_head];
+                p[k] = params[word_at.at];
             }
-            unit.step();
+            const bool on = unit.step();
+            row_at.step(on), code_at.step(on), word_at.step(on);
         }
         #pragma unroll
         for (int k = 0; k < AHEAD; ++k) {
             if (to[k] == nullptr) continue;
-            const float s = __uint_as_float(p[k] << 16);
-            const int z = (p[k] >> 16) & 0xf;
+            // c - z from bf16 128 + c and 128 + z, exactly; times s, rounded once
+            const uint32_t s = __byte_perm(p[k], 0u, 0x1010), z = __byte_perm(p[k], 0u, 0x3232) | 0x43004300u;
             #pragma unroll
             for (int w = 0; w < 2; ++w) {
                 uint32_t out[4];
                 #pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    out[j] = pack_values(s * static_cast<float>(static_cast<int>((c[k][w] >> (4 * j)) & 0xf) - z),
-                                         s * static_cast<float>(static_cast<int>((c[k][w] >> (16 + 4 * j)) & 0xf) - z));
+                for (int j = 0; j < 4; ++j) out[j] = mul_bf16x2(sub_bf16x2((c[k][w] >> (4 * j) & 0x000f000fu) | 0x43004300u, z), s);
                 __stcs(reinterpret_cast<uint4*>(to[k]) + w * G, make_uint4(out[0], out[1], out[2], out[3]));
             }
         }
@@ -270,9 +310,9 @@ static int32_t make_geo(const ss_kvq_rows* rows, const ss_kvq_cache* cache, KvqG
 }
 
 // CTAs along x, for the longest run (the lengths are on the device).  The start of a CTA costs as much as several steps, so it gets
-// eight of them before there are more (a user's accepted path into 32 layers and back 6.8 us; with one step each 10.7, with two 8.2);
-// and where runs are long there are up to 32 CTAs per SM, eight times what is resident, so that the shorter runs' end early (up to 8:
-// 570 us for the prompts of four users, up to 32: 480).  Sharing the sum of the runs out evenly was slower, whether each CTA
+// eight of them before there are more (a user's accepted path into 32 layers and back 6.4 us; before, with one step each 10.7, two 8.2, eight 6.8);
+// and where runs are long there are up to 32 CTAs per SM, eight times what is resident, so that the shorter runs' end early (the
+// prompts of four users and back: up to 8 579 us, up to 32 480).  Sharing the sum of the runs out evenly was slower, whether each CTA
 // took a stretch (550) or all went side by side (740): finding one's place and starting anew in every run costs more than it evens out.
 static dim3 grid_for(const KvqGeo& g, int batch, long long max_rows, int head_dim) {
     const long long slots = head_dim == 128 ? Unit<128>::SLOTS : head_dim == 80 ? Unit<80>::SLOTS : Unit<64>::SLOTS, warps = kKvqThreads / 32;
