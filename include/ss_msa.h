@@ -388,7 +388,7 @@ int32_t ss_kvq_read(const ss_kvq_cache* cache, const ss_kvq_rows* rows, const in
  * rows in the workspace, and the last of them to finish joins them in key order: results do not depend on the order of arrival,
  * and no CTA waits for another.  The workspace holds the counters of arrivals, zero between calls, and those rows: calls of
  * different shapes may share one that is large enough for each, in stream order, but it is not one of another entry point's.
- * A sequence with kv_len[b] over its capacity, with slots outside the slab or without nodes is skipped (its outputs are not
+ * A sequence with kv_len[b] over its capacity (or 2^31 - 2^16), with slots outside the slab or without nodes is skipped (its outputs are not
  * written); for the first two the status word is set to SS_ERR_CAPACITY.  SS_ERR_DEVICE_TIMEOUT there means that a wait between the warps of
  * a CTA ran out (about a second): outputs are not written and the workspace is to be zero-filled.
  * Limits: 65535 sequences and heads, SS_MAX_NODES nodes, SS_MAX_GAMMA streams, head_dim 64, 80 or 128.

@@ -418,6 +418,10 @@ def make_kvq_attn_params(*, q_main, o_main, k_tree, v_tree, cache: KvqCache, kv_
     for t, shape in ((lse_main, main[:-1]), (lse_spec, spec[:-1])):
         if t is not None and (t.dtype is not torch.float32 or tuple(t.shape) != shape or not t.is_contiguous()):
             raise ValueError("log-sum-exps are contiguous fp32 tensors [B][Tmax][H] and [B][Tmax][gamma][H]")
+    if cache.device >= 0:
+        for t in (q_main, o_main, k_tree, v_tree, q_spec, k_spec, v_spec, o_spec, lse_main, lse_spec, kv_start, kv_len, kv_capacity, trees, workspace):
+            if t is not None and t.get_device() != cache.device:
+                raise ValueError("the call's tensors lie on the cache's device")
     p = KvqAttnParams()
     p.batch, p.gamma, p.max_nodes, p.layer, p.sm_scale = B, int(gamma), Tmax, int(layer), float(sm_scale)
     p.q_main, p.o_main, p.k_tree, p.v_tree = _ptr(q_main), _ptr(o_main), _ptr(k_tree), _ptr(v_tree)

@@ -395,6 +395,42 @@ def test_attention_skips_sequences_that_cannot_be_run(api):
     assert api.ss_status(ws) == api.SS_ERR_CAPACITY
 
 
+@pytest.mark.parametrize("nodes", [3, 30])
+def test_attention_skips_lengths_at_the_end_of_32_bits(api, nodes):
+    """Lengths from 2^31 - 2^16 on are refused on the device, whatever the slab is said to hold; the sequences beside them run."""
+    x = Layer(api, 3, 2, 64, [40, 70, 100], [nodes] * 3, 0, seed=3)
+    ws = x.workspace()
+    p = x.params(ws)
+    p.cache.total_slots = 1 << 33                            # (a length that is refused reads nothing)
+    x.kv_len[1] = 2 ** 31 - 1
+    api.ss_msa_attention_kvq(p)
+    assert api.ss_status(ws) == api.SS_ERR_CAPACITY
+    x.check([0, 2])
+    assert (x.o_main[1] == 77.0).all() and (x.lse_main[1] == 77.0).all()
+
+
+def test_two_calls_at_once(api):
+    """Calls on two streams, each with a workspace of its own, and a path with the same node twice."""
+    xs = [Layer(api, 4, 4, 128, [900, 30, 2000, 500], [n] * 4, 0, seed=40 + n) for n in (7, 40)]
+    spaces, streams = [x.workspace() for x in xs], [torch.cuda.Stream() for _ in xs]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for x, ws, s in zip(xs, spaces, streams):
+            api.ss_msa_attention_kvq(x.params(ws), s)
+    torch.cuda.synchronize()
+    for x, ws in zip(xs, spaces):
+        assert api.ss_status(ws) == 0
+        x.check()
+    cache = api.empty_kvq_cache(1, 16, 2, 64)
+    k = _rows((1, 1, 5, 2, 64), 3)
+    path = torch.full((1, api.SS_PATH_STRIDE), -1, dtype=torch.int32, device="cuda")
+    path[0, :4] = torch.tensor([0, 3, 3, 1])
+    back = torch.zeros((1, 1, 4, 2, 64), dtype=torch.bfloat16, device="cuda")
+    api.ss_kvq_write(k, k, cache, _i64([2]), _i32([0]), _i32([4]), path, None, None)
+    api.ss_kvq_read(cache, back, torch.empty_like(back), _i64([2]), None, None)
+    assert torch.equal(back[:, :, 1], back[:, :, 2]) and not torch.equal(back[:, :, 0], back[:, :, 1])
+
+
 def test_attention_a_row_that_was_not_finite_stays_within_its_head(api):
     """A value that is not finite makes its head's row NaN, and with it the outputs that see it; other heads and sequences do not."""
     x = Layer(api, 2, 3, 128, [100, 90], [6, 6], 0, seed=6)

@@ -168,6 +168,16 @@ def test_binding_refuses_tensors_of_other_sizes(lib):
             api.make_kvq_attn_params(**dict(ok, **kw))
 
 
+def test_binding_refuses_tensors_of_another_device(lib):
+    cache = api.empty_kvq_cache(1, 10, 3, 64, device="cpu")
+    q, i = torch.zeros((1, 2, 3, 64), dtype=torch.bfloat16), torch.zeros(1, dtype=torch.int32)
+    args = dict(q_main=q, o_main=q, k_tree=q, v_tree=q, cache=cache, kv_start=i, kv_len=i, trees=i, gamma=0, sm_scale=1.0)
+    api.make_kvq_attn_params(**args)
+    cache.device = 1                                         # as if it lay on the second GPU
+    with pytest.raises(ValueError):
+        api.make_kvq_attn_params(**args)
+
+
 def test_struct_sizes_match_the_header(lib):
     assert C.sizeof(api.KvqCache) == 16 + 4 * 8 + 7 * 8
     assert C.sizeof(api.KvqAttnParams) == 24 + 8 * 8 + C.sizeof(api.KvqCache) + 4 * 8 + 3 * 8 + 8
