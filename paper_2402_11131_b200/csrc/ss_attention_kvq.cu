@@ -190,8 +190,8 @@ __device__ __forceinline__ float zero_over_16(uint32_t word) { return __uint_as_
 constexpr float kCode = 5.9604644775390625e-08f;                 // 2^-24: what a code counts in an MMA
 
 // Pieces of a lone sequence's unit.  What joining p pieces takes grows with p, what the steps of one take falls as 1 / p: the best p grows
-// as the root of the steps.  (Two heads with 20,000 keys, one row: 14.1 us, in as many pieces as there are CTAs 22.7, with twice the
-// root as the limit 14.9.)  Two steps are not worth a join at all (7.6 against 8.5 us).
+// as the root of the steps.  (Two heads with 20,000 keys, one row: 14.6 us; in as many pieces as there are CTAs 22.7, with twice the
+// root as the limit 0.8 more.)  Two steps are not worth a join at all (7.6 against 8.5 us).
 __device__ __forceinline__ int most_pieces(int steps) { return steps < 3 ? 1 : static_cast<int>(3.f * sqrtf(static_cast<float>(steps))); }
 
 // The line of steps as one CTA sees it (every thread, or one warp of a role, works it out for itself)
@@ -996,7 +996,7 @@ __global__ void __launch_bounds__(kThreads, NG == 1 ? 3 : 2) msa_attention_kvq_r
             }
             __syncthreads();
             if (joined) {
-                constexpr int kJoinAhead = NG == 1 ? 8 : 4;                   // partial rows that a thread has on their way
+                constexpr int kJoinAhead = 6;        // partial rows that a thread has on their way (12 pieces of 8 rows: 13.4 us, 8 14.0, 4 13.2; 37 of one: 14.6, 14.1, 15.4)
                 #pragma unroll 1
                 for (int item = tid; item < items; item += kThreads) {
                     const int hr = item / (D / 8), d0 = (item - hr * (D / 8)) * 8, hd = hr / rows, r = hr - hd * rows;
@@ -1039,10 +1039,10 @@ struct KvqPlan {
 static KvqPlan kvq_plan(const ss_kvq_attn_params& p) {
     const int rows = q_rows(p);
     // Up to 8 rows the rows are one group: three CTAs per SM, and nothing is spent on the second group's padding (16 users with 512 to 4096
-    // keys, a row each: 43 us, with two groups 50; 32 heads of 50,000 keys, 8 rows: 57 and 64; 2048 keys: 14.4 and 11.9, the other way round).
-    // From 17 rows on tcgen05 is faster at all lengths (32 rows: 16 users 86 us, by two groups of 16 rows 121; 50,000 keys 107 and 125;
-    // 512 keys 12.9 and 14.3), up to 16 it is slower in all but short sequences (12 rows: 84 and 64 us; 105 and 68; 512 keys 12.1 and 12.6).
-    // 32 rows in the kernel for 64 cost a sixth (102 us).
+    // keys, a row each: 43 us, with two groups 51; 32 heads of 50,000 keys, 8 rows: 56 and 63; 512 keys 10.1 and 10.2; 2048 keys 13.4 and
+    // 11.7, the other way round).  From 17 rows on tcgen05 is faster at all lengths (32 rows: 16 users 86 us, by two groups of 16 rows 121;
+    // 50,000 keys 107 and 125; 512 keys 12.9 and 14.3); up to 16 it is slower where it counts (12 rows: 16 users 85 and 65 us; 50,000 keys
+    // 105 and 67; 512 keys 11.5 and 12.4: only the device knows the lengths).  32 rows in the kernel for 64 cost a sixth (102 us).
     KvqPlan k{0, rows <= 8 ? 1 : 2, 0, 0};
     if (rows > 16) k.tile = rows <= 32 ? 32 : 64;
     k.block = k.tile > 0 ? k.tile : 8 * k.groups;
