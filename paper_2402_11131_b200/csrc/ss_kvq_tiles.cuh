@@ -123,6 +123,20 @@ struct TileCtrl {
 __device__ __forceinline__ void tile_wait(uint32_t bar, uint32_t parity, int* abort, int* status) {
     if (!mbar_try(bar, parity)) mbar_wait_slow(bar, parity, abort, status);
 }
+// The planning warp's wait for a whole unit: 2^31 keys take seconds.  A role that is stuck gives up after its own bound and sets `abort`,
+// so this one need not be short.
+static __device__ __noinline__ void wait_for_unit(uint32_t bar, uint32_t parity, volatile int* abort, int* status) {
+    const long long t0 = clock64();
+    while (!mbar_try(bar, parity)) {
+        if (*abort) return;
+        if (clock64() - t0 > 64 * kWaitCycles) {
+            *abort = 1;
+            set_status(status, SS_ERR_DEVICE_TIMEOUT);
+            return;
+        }
+    }
+}
+
 template <int C>
 __device__ __forceinline__ void tmem_load(uint32_t addr, uint32_t (&r)[C]) {
     if constexpr (C == 32) tmem_ld32<0>(addr, r);
@@ -852,7 +866,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) msa_attention_kvq_tiles_kerne
                 if (unit > 0) {                      // (the first unit's plan is there)
                     const bool more = line.next(a);
                     // (a unit's rows are free when all are done with the plan: its last S is complete then)
-                    if (unit >= 2) wait(c.plan_free[unit & 1], ((unit - 2) >> 1) & 1);
+                    if (unit >= 2) wait_for_unit(smem_u32(&c.plan_free[unit & 1]), ((unit - 2) >> 1) & 1, &c.abort, status);
                     make_plan(u, more);
                 }
             }
