@@ -17,8 +17,9 @@
 // What bounds it: each role's chain of latencies per tile (loads, conversion, TMEM round trip, hand-over), some 1800 to 2300 cycles of 128 keys
 // by 64 rows whatever the role, where the MMAs need 300 and the exponentials 512: 16 users with 512 to 4096 keys 104 us for 27.5 of HBM.
 // On the way there: one softmax group per 32 rows 143 us, four 130; weights without a vote on the references 118 (a sum per tile
-// decides) against 112; a unit's start counted in the deal of work 112 for 131; own warps for what comes before a unit 107.  Registers (72 each, all there are) decide too: what is called
-// seldom and spills least is out of line (rows and waits: 104, inline 121; the join, though: 125).
+// decides) against 112; a unit's start counted in the deal of work 112 for 131; own warps for what comes before a unit 107.
+// Registers (72 each, all there are) decide too: what is called seldom is out of line where the loops around it then spill less (rows and
+// the wait for a unit: 104, inline 121; not the join: 125).
 // Rounding: keys and values are whole numbers below 2^8 in bf16, exactly; queries enter as they are; a weight p s_v is rounded once to
 // bf16 (2^-8 of itself), as the bf16 attention rounds p.  The sums of q (128 + c) are larger than those of q (c - z) by some 143 over
 // |c - z|: fp32 accumulators lose 2^-24 of them per step of 16, 10^-4 of a score unit for normal queries and keys, a tenth of what the
