@@ -143,7 +143,8 @@ int32_t ss_tree_build(const int32_t* parent, int32_t n_nodes, int32_t gamma, ss_
  * It does NOT hold for a call that directly follows ss_kv_compact on the same cache when that call writes
  * the kv_len array the attention reads (kv_len_out == kv_len) or when the attention's lengths already
  * include the compacted slots: compaction turns tree slots into prefix and writes the lengths.  Pass
- * flags = 0 to the first attention call after such a compaction, or put any other kernel between them.
+ * flags = 0 to the first attention call after such a compaction, or put any other kernel between them.  The same goes for a call that
+ * directly follows ss_kvq_write where that call's kv_len_out is the attention's kv_len, or ss_kvq_read into its prefix.
  * ss_next_draft and ss_tree_prune let the next kernel of the stream be scheduled only once their descriptors are in
  * memory, so an attention call directly behind one of them may make the promise for these. */
 #define SS_ATTN_PREFIX_STABLE 1u
