@@ -421,14 +421,15 @@ struct WarpState {
     float limit;                                     // V scales from here on raise r; 0: none seen yet
 };
 
-// Moves the references by `by` (log2 units)
+// Moves the references by `by` (log2 units): up, or, a row's first one, to wherever its maximum lies.  That may be far down, where
+// 2^-by is no number any more; there is nothing to scale then.
 template <int D, int NG>
 __device__ __forceinline__ void move_refs(WarpState<D, NG>& w, const float (&by)[NG][2]) {
     #pragma unroll
     for (int n = 0; n < NG; ++n) {
         #pragma unroll
         for (int e = 0; e < 2; ++e) {
-            const float f = exp2_approx(-by[n][e]);
+            const float f = exp2_approx(-fmaxf(by[n][e], 0.f));
             w.ref[n][e] += by[n][e];
             w.sum[n][e] *= f;
             w.zo[n][e] *= f;
