@@ -462,7 +462,8 @@ __device__ __forceinline__ void raise_scale(WarpState<D, NG>& w, float scale) {
 
 // Scores above their references (d, log2 units; -inf: not seen) of H tiles of 16 keys: where one is more than 8 above, references are
 // raised to the maxima and d lowered by as much.  A row that has seen no key so far takes the maximum whatever it is: so the first chunk
-// always comes here, by its V scales (no limit holds yet) or, `first`, because it is not a cached one.  `top`: the largest V scale.
+// always comes here, by its V scales (no limit holds yet; nor does one for NaN) or, `first`, because it is not a cached one.  `top`: the
+// largest V scale.
 template <int D, int NG, int H>
 __device__ __forceinline__ void keep_in_range(WarpState<D, NG>& w, float (&d)[H][NG][4], float top, bool first) {
     float most = d[0][0][0];
@@ -471,7 +472,7 @@ __device__ __forceinline__ void keep_in_range(WarpState<D, NG>& w, float (&d)[H]
         #pragma unroll
         for (int n = 0; n < NG; ++n) most = fmaxf(fmaxf(fmaxf(most, d[j][n][0]), fmaxf(d[j][n][1], d[j][n][2])), d[j][n][3]);
     }
-    if (__any_sync(0xffffffffu, most > 8.f || top >= w.limit || first)) {
+    if (__any_sync(0xffffffffu, most > 8.f || !(top < w.limit) || first)) {
         float by[NG][2];
         #pragma unroll
         for (int n = 0; n < NG; ++n) {

@@ -3,6 +3,7 @@ import pytest
 
 torch = pytest.importorskip("torch")
 
+import kvq_util as U
 from test_gpu_kvq import Layer, _i32, _i64, _rows, api  # noqa: F401  (api is a fixture)
 
 pytestmark = pytest.mark.gpu
@@ -19,6 +20,18 @@ def _put(x, b, k=None, v=None, at=0):
 
 def _normal(shape, seed):
     return torch.randn(shape, generator=torch.Generator().manual_seed(seed))
+
+
+def _check_lse(x, b):
+    """Log-sum-exps of sequence b, which do not depend on the values."""
+    keys, _ = U.cache_values(x.cache, 0, "cuda")
+    n, g, held = x.nodes[b], x.gamma, slice(x.starts[b], x.starts[b] + x.lens[b])
+    spec = (lambda t: t[b, :n] if g else None)
+    none = [torch.zeros_like(t) if t is not None else None for t in (keys[held], x.v_tree[b, :n], spec(x.v_spec))]
+    _, lse, _, tol = U.attention(x.parents[b], g, x.scale, x.q_main[b, :n], spec(x.q_spec), keys[held], none[0], x.k_tree[b, :n], none[1],
+                                 spec(x.k_spec), none[2])
+    got = torch.cat([x.lse_main[b, :n].double()] + ([x.lse_spec[b, :n].double().flatten(0, 1)] if g else []))
+    assert ((got - lse).abs() <= tol).all()
 
 
 @pytest.mark.parametrize("d", [64, 80, 128])
@@ -40,3 +53,25 @@ def test_first_scores_far_below_zero(api, d, nodes, gamma):
         x.fresh()
         x.run()
         x.check()
+
+
+@pytest.mark.parametrize("d", [64, 80, 128])
+@pytest.mark.parametrize("nodes,gamma", SHAPES)
+def test_values_without_a_number_leave_the_log_sum_exps(api, d, nodes, gamma):
+    """A sequence's cached values are all NaN (their keys are not): so are its outputs, while its log-sum-exps, of scores of some 200
+    above or below zero, are numbers; another sequence's outputs are untouched by it."""
+    H, lens = 3, [33, 600]
+    for bad, sign in ((0, 1.0), (1, -1.0), (0, -1.0)):
+        x = Layer(api, 2, H, d, lens, [nodes] * 2, gamma, seed=7 + d)
+        _put(x, bad, sign * (_normal((lens[bad], H, d), 1).abs() * 0.2 + 10.0), torch.full((lens[bad], H, d), float("nan")))
+        for t in (x.q_main, x.q_spec):
+            if t is not None:
+                t.copy_((t.float().abs() * 0.1 + 20.0 * d ** -0.5).to(torch.bfloat16))
+        for t in (x.k_tree, x.k_spec):
+            if t is not None:
+                t.copy_((sign * (t.float().abs() * 0.2 + 10.0)).to(torch.bfloat16))
+        x.run()
+        x.check([1 - bad])
+        for o in (x.o_main, x.o_spec):
+            assert o is None or torch.isnan(o[bad]).all()
+        _check_lse(x, bad)
