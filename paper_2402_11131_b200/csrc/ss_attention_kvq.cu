@@ -445,7 +445,7 @@ __device__ __forceinline__ void move_refs(WarpState<D, NG>& w, const float (&by)
 // Raises r to the exponent of a V scale
 template <int D, int NG>
 __device__ __forceinline__ void raise_scale(WarpState<D, NG>& w, float scale) {
-    const uint32_t r = min(max(__float_as_uint(scale) >> 23, 32u), 240u);
+    const uint32_t r = min(max(__float_as_uint(scale) >> 23, 32u), 252u);       // (2^125: the largest scale there is)
     const float now = __uint_as_float((254u + 6u - r) << 23), f = now * __uint_as_float((254u << 23) - __float_as_uint(w.weight));   // (powers of two)
     w.weight = now;
     w.limit = __uint_as_float((r + 1u) << 23);
@@ -950,7 +950,7 @@ __global__ void __launch_bounds__(kThreads, NG == 1 ? 3 : 2) msa_attention_kvq_r
                 if (g == 0) stats[warp * ROWS + 8 * n + 2 * c + e] = make_float2(w.sum[n][e] == 0.f ? kNoRef : w.ref[n][e], w.sum[n][e]);
             }
         }
-        const float unweigh = 1.f / (kCode * w.weight);
+        const float unweigh = __uint_as_float((254u << 23) - __float_as_uint(w.weight));     // (a power of two; 2^24 apart from it, or it may pass fp32)
         #pragma unroll
         for (int k = 0; k < G::kTiles; ++k) {
             const int dim = tile_dim<D>(k, g);
@@ -960,7 +960,7 @@ __global__ void __launch_bounds__(kThreads, NG == 1 ? 3 : 2) msa_attention_kvq_r
                 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
                     float* dst = parts + (warp * ROWS + 8 * n + 2 * c + e) * PAD + dim;
-                    const float x = fmaf(w.o[k][n][e], f, -w.zo[n][e]) * unweigh, y = fmaf(w.o[k][n][2 + e], f, -w.zo[n][e]) * unweigh;
+                    const float x = fmaf(w.o[k][n][e], f, -w.zo[n][e]) * (1.f / kCode) * unweigh, y = fmaf(w.o[k][n][2 + e], f, -w.zo[n][e]) * (1.f / kCode) * unweigh;
                     if (k < 4 * G::kWordsV) *reinterpret_cast<float2*>(dst) = make_float2(x, y);
                     else dst[0] = x, dst[8] = y;
                 }

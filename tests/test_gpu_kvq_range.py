@@ -75,3 +75,27 @@ def test_values_without_a_number_leave_the_log_sum_exps(api, d, nodes, gamma):
         for o in (x.o_main, x.o_spec):
             assert o is None or torch.isnan(o[bad]).all()
         _check_lse(x, bad)
+
+
+# log2 of the sizes of the cached values: of the first keys, of those from key 100 on; of the nodes' and streams' values
+SIZES = {"cached large": (112, 112, 0), "later ones large": (0, 20, 0), "later ones small": (0, -20, 3), "cached tiny": (-100, -100, 0),
+         "both large": (89, 89, 89), "behind the prefix large": (0, 0, 89), "behind the prefix tiny": (10, 12, -70), "all tiny": (-110, -112, -110)}
+
+
+@pytest.mark.parametrize("d", [64, 80, 128])
+@pytest.mark.parametrize("nodes,gamma", SHAPES)
+@pytest.mark.parametrize("sizes", list(SIZES))
+def test_values_of_very_different_sizes(api, d, nodes, gamma, sizes):
+    H, lens = 3, [20, 133, 900]
+    first, later, behind = SIZES[sizes]
+    x = Layer(api, 3, H, d, lens, [nodes] * 3, gamma, seed=11 + d)
+    for b, n in enumerate(lens):
+        v = _normal((n, H, d), b)
+        v[:100] *= 2.0 ** first
+        v[100:] *= 2.0 ** later
+        _put(x, b, _normal((n, H, d), 20 + b), v)
+    for t in (x.v_tree, x.v_spec):
+        if t is not None:
+            t.copy_((t.float() * 2.0 ** behind).to(torch.bfloat16))
+    x.run()
+    x.check()
