@@ -340,7 +340,7 @@ typedef struct ss_kvq_cache {
     uint32_t* v_params;
     int64_t layer_stride, slot_stride, head_stride;
     int64_t param_layer_stride, param_slot_stride, param_head_stride;
-    int64_t total_slots;
+    int64_t total_slots;             /* at most 2^48 */
 } ss_kvq_cache;
 
 /* bf16 rows outside the cache: layer l, sequence b, row r, head h at k + l * layer_stride + b * batch_stride + r * row_stride +

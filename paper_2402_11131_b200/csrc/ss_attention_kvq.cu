@@ -61,7 +61,7 @@ __device__ __forceinline__ Seq load_seq(const KvqArgs& a, int b) {
     s.L = a.kv_len[b];
     s.start = a.kv_start[b];
     s.T = min(a.trees[b].n_nodes, a.max_nodes);
-    const bool fits = s.L >= 0 && s.L <= kMostKeys && s.start >= 0 && s.start + s.L <= a.total_slots && (a.kv_capacity == nullptr || s.L <= a.kv_capacity[b]);
+    const bool fits = s.L >= 0 && s.L <= kMostKeys && s.start >= 0 && s.start <= a.total_slots - s.L && (a.kv_capacity == nullptr || s.L <= a.kv_capacity[b]);
     if (!fits) set_status(a.ws, SS_ERR_CAPACITY);
     if (!fits || s.T < 1) s.T = s.rows = s.blocks = s.chunks = 0;
     else {

@@ -31,7 +31,7 @@ inline int sm_count() {
 
 // A cache in 4 bits: what the host can see of it.
 inline int32_t kvq_check_cache(const ss_kvq_cache& c) {
-    if (!c.k_codes || !c.v_codes || !c.k_params || !c.v_params || c.n_layers < 1 || c.n_heads < 1 || c.total_slots < 0) return SS_ERR_INVALID_ARG;
+    if (!c.k_codes || !c.v_codes || !c.k_params || !c.v_params || c.n_layers < 1 || c.n_heads < 1 || c.total_slots < 0 || c.total_slots > 1ll << 48) return SS_ERR_INVALID_ARG;
     if ((c.head_dim != 64 && c.head_dim != 80 && c.head_dim != 128) || c.n_heads > 65535) return SS_ERR_UNSUPPORTED;
     const uintptr_t unit = c.head_dim == 80 ? 7u : 15u;
     if (((reinterpret_cast<uintptr_t>(c.k_codes) | reinterpret_cast<uintptr_t>(c.v_codes)) & unit) ||

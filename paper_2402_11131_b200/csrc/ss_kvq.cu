@@ -102,9 +102,10 @@ __device__ __forceinline__ bool write_run(const KvqGeo& g, const int64_t* kv_sta
     const int limit = path != nullptr ? SS_PATH_STRIDE : g.max_rows;
     *L = kv_len_in[b];
     *n = n_rows != nullptr ? max(0, min(n_rows[b], limit)) : min(g.max_rows, limit);
-    *slot0 = kv_start[b] + *L;
-    const bool fits = *L >= 0 && *n <= INT_MAX - *L && *slot0 >= 0 && *slot0 + *n <= g.total_slots &&
+    const long long start = kv_start[b];             // (anything: no sum of it before it is known to be near the slab)
+    const bool fits = *L >= 0 && *n <= INT_MAX - *L && start >= -static_cast<long long>(*L) && start <= g.total_slots - *L - *n &&
                       (kv_capacity == nullptr || *L + *n <= kv_capacity[b]);
+    *slot0 = fits ? start + *L : 0;
     return fits;
 }
 
@@ -253,7 +254,8 @@ kvq_read_kernel(const __grid_constant__ KvqGeo g, const int64_t* __restrict__ kv
     const int layer = blockIdx.y >> 1, b = blockIdx.z;
     const bool is_v = blockIdx.y & 1;
     const int n = n_rows != nullptr ? min(n_rows[b], g.max_rows) : g.max_rows;
-    const long long slot0 = kv_start[b] + (first != nullptr ? first[b] : 0);
+    // (a start so far outside that no row's slot is in the slab may be nearer: no sum overflows)
+    const long long slot0 = min(max(static_cast<long long>(kv_start[b]), -(1ll << 32)), g.total_slots + (1ll << 31)) + (first != nullptr ? first[b] : 0);
     const unsigned char* codes = (is_v ? g.v_codes : g.k_codes) + layer * g.layer_stride + 4 * at;
     const uint32_t* params = (is_v ? g.v_params : g.k_params) + layer * g.p_layer;
     unsigned char* rows = (is_v ? g.v_rows : g.k_rows) + layer * g.r_layer + b * g.r_batch + 16 * at;

@@ -99,3 +99,29 @@ def test_values_of_very_different_sizes(api, d, nodes, gamma, sizes):
             t.copy_((t.float() * 2.0 ** behind).to(torch.bfloat16))
     x.run()
     x.check()
+
+
+def test_starts_at_the_ends_of_64_bits(api):
+    """A start whose sum with the length or the number of rows passes 2^63 is one outside the slab, for all three calls; the sequences
+    beside it are dealt with."""
+    H, d, far = 2, 64, [2 ** 63 - 1, 2 ** 63 - 30, -2 ** 63, -2 ** 63 + 7]
+    for nodes in (3, 30):
+        x = Layer(api, 5, H, d, [40, 50, 60, 70, 80], [nodes] * 5, 0, seed=3)
+        x.kv_start = _i64(far + x.starts[4:])
+        ws = x.workspace()
+        api.ss_msa_attention_kvq(x.params(ws))
+        assert api.ss_status(ws) == api.SS_ERR_CAPACITY
+        x.check([4])
+        assert (x.o_main[:4] == 77.0).all() and (x.lse_main[:4] == 77.0).all()
+    cache = api.empty_kvq_cache(1, 60, H, d)
+    k, v = _rows((1, 5, 6, H, d), 1), _rows((1, 5, 6, H, d), 2)
+    lens, out, status = _i32([40, 29, 0, 0, 3]), _i32([0] * 5), api.workspace(256)
+    api.ss_kvq_write(k, v, cache, _i64(far + [10]), lens, None, None, None, out, status)
+    assert out.tolist() == [40, 29, 0, 0, 9] and api.ss_status(status) == api.SS_ERR_CAPACITY
+    assert (cache.tensors[1][0] != 0).any(1).nonzero().flatten().tolist() == list(range(13, 19))
+    back = torch.full((1, 5, 6, H, d), 9.0, dtype=torch.bfloat16, device="cuda")
+    other = torch.full_like(back, 9.0)
+    api.ss_kvq_read(cache, back, other, _i64(far + [13]), _i32([40, 2 ** 31 - 1, -2 ** 31, -8, 0]))
+    assert (back[:, :4] == 9.0).all() and (other[:, :4] == 9.0).all()
+    step = (k[:, 4].double().amax(-1).clamp(min=0) - k[:, 4].double().amin(-1).clamp(max=0)) / 15 * (1 + 2.0 ** -7)
+    assert ((back[:, 4].double() - k[:, 4].double()).abs() <= (step * (1 + 16 * 2.0 ** -8))[..., None]).all()
