@@ -107,6 +107,11 @@ struct TileLoader {
     }
 };
 
+struct alignas(8) TileWaits {
+    int abort;                                       // a wait has run out
+    int limit;                                       // bound of waits for data, in units of 1024 cycles
+};
+
 template <int C>
 struct TileCtrl {
     unsigned long long k_full[2], s_full[2], s_free[2], v_full[2], p_full[2], pv_done[2], o_free, drain;
@@ -119,21 +124,45 @@ struct TileCtrl {
     float sums[kTileGroups][4][C];
     int hot[kTileGroups][2];                                      // a reference has to go up
     uint32_t tmem;
-    int abort, joined, any;
+    int joined, any;
+    TileWaits waits;
 };
 
-__device__ __forceinline__ void tile_wait(uint32_t bar, uint32_t parity, int* abort, int* status) {
-    if (!mbar_try(bar, parity)) mbar_wait_slow(bar, parity, abort, status);
+// Two kinds of waits.
+// Waits for data (codes, operands, products, buffers) end at their bound, and at once when one of them has ended so: from then on the CTA goes
+// through its tiles without them, on whatever the buffers hold, and nothing of that is used.  The bound is the caller's (workspace word
+// 1), but for the softmax warps a second: they wait for products alone, for whose buffers the others wait as well, and have no registers for
+// more (with the caller's bound there, spills in their loop: 16 users 119 for 103 us).
+// Waits for the other warps' steps, which decide where a warp goes next (units' plans, a group's vote), are never left early: plans are not
+// overwritten under their readers, warps that meet at barriers take the same branches, and addresses are those of the plan.  They end all the
+// same: they wait for arrivals alone, which come as soon as the other warps' waits for data have ended.  That may take as long as the longest
+// unit (2^24 tiles of some 2000 cycles, 3.4 10^10 cycles), so their bound is 1.3 10^11.
+__device__ __forceinline__ uint32_t kilocycles() { return static_cast<uint32_t>(clock64() >> 10); }
+static __device__ __noinline__ void wait_for_warps_slow(uint32_t bar, uint32_t parity, volatile TileWaits* w) {
+    const uint32_t t0 = kilocycles();
+    while (!mbar_try(bar, parity)) {
+        if (kilocycles() - t0 > static_cast<uint32_t>(64 * kWaitCycles >> 10)) {
+            w->abort = 1;
+            return;
+        }
+    }
 }
-// The planning warp's wait for a whole unit: 2^31 keys take seconds.  A role that is stuck gives up after its own bound and sets `abort`,
-// so this one need not be short.
-static __device__ __noinline__ void wait_for_unit(uint32_t bar, uint32_t parity, volatile int* abort, int* status) {
-    const long long t0 = clock64();
+static __device__ __noinline__ void wait_for_data_slow(uint32_t bar, uint32_t parity, volatile TileWaits* w) {
+    const uint32_t t0 = kilocycles();
+    while (!mbar_try(bar, parity)) {
+        if (w->abort) return;
+        if (kilocycles() - t0 > static_cast<uint32_t>(w->limit)) {
+            w->abort = 1;
+            return;
+        }
+    }
+}
+static __device__ __noinline__ void wait_for_product_slow(uint32_t bar, uint32_t parity, volatile int* abort) {
+    const uint32_t t0 = static_cast<uint32_t>(clock());
     while (!mbar_try(bar, parity)) {
         if (*abort) return;
-        if (clock64() - t0 > 64 * kWaitCycles) {
+        if (static_cast<uint32_t>(clock()) - t0 > static_cast<uint32_t>(kWaitCycles)) {
             *abort = 1;
-            set_status(status, SS_ERR_DEVICE_TIMEOUT);
             return;
         }
     }
@@ -288,10 +317,9 @@ __global__ void __launch_bounds__(kTileThreads, 1) msa_attention_kvq_tiles_kerne
     __shared__ __align__(16) TileCtrl<C> c;
     const int tid = threadIdx.x, lane = tid & 31, warp = static_cast<int>(uniform(tid >> 5)), quad = warp & 3;
     const uint32_t smem = smem_u32(smem_raw);
-    int* const status = reinterpret_cast<int*>(a.ws);
     constexpr int kMmaWarp = kTileWarpsOfUnit - 1, kPlanWarp = kMmaWarp + 1;
     if (tid == 0) {
-        c.abort = 0;
+        c.waits.abort = 0, c.waits.limit = static_cast<int>(kWaitCycles >> 10);
         for (int i = 0; i < 2; ++i) {
             mbar_init(smem_u32(&c.k_full[i]), 128), mbar_init(smem_u32(&c.v_full[i]), 128);
             mbar_init(smem_u32(&c.s_free[i]), kTileSoftmax), mbar_init(smem_u32(&c.p_full[i]), kTileSoftmax);
@@ -309,6 +337,10 @@ __global__ void __launch_bounds__(kTileThreads, 1) msa_attention_kvq_tiles_kerne
     }
     wait_for_previous_kernel();
     release_next_kernel();
+    if (tid == 0) {
+        const int lim = reinterpret_cast<const volatile int*>(a.ws)[1];
+        if (lim > 0) c.waits.limit = lim;
+    }
     Line<N, kTileOfKeys, 0, kTileStart> line;                    // (the planning warp's)
     const auto make_plan = [&](TileUnit& u, bool more) {         // of the unit that the line is at
         if (lane != 0) return;
@@ -335,11 +367,18 @@ __global__ void __launch_bounds__(kTileThreads, 1) msa_attention_kvq_tiles_kerne
         return;
     }
     const uint32_t tmem = uniform(c.tmem), lanes = static_cast<uint32_t>(32 * quad) << 16;
-    // (a wait that runs out leaves the roles in step: everyone goes through the same tiles without waiting, and no output is written)
-    const auto wait = [&](unsigned long long& bar, uint32_t parity) { tile_wait(smem_u32(&bar), parity, &c.abort, status); };
+    const auto wait = [&](unsigned long long& bar, uint32_t parity) {
+        if (!mbar_try(smem_u32(&bar), parity)) wait_for_data_slow(smem_u32(&bar), parity, &c.waits);
+    };
+    const auto wait_for_product = [&](unsigned long long& bar, uint32_t parity) {
+        if (!mbar_try(smem_u32(&bar), parity)) wait_for_product_slow(smem_u32(&bar), parity, &c.waits.abort);
+    };
+    const auto wait_for_warps = [&](unsigned long long& bar, uint32_t parity) {
+        if (!mbar_try(smem_u32(&bar), parity)) wait_for_warps_slow(smem_u32(&bar), parity, &c.waits);
+    };
     // units one after another: the plan of unit n, and back to the planning warp when a warp is done with it
     const auto plan_of = [&](uint32_t n) -> const TileUnit& {
-        wait(c.plan_full[n & 1], (n >> 1) & 1);
+        wait_for_warps(c.plan_full[n & 1], (n >> 1) & 1);
         return c.unit[n & 1];
     };
     const auto plan_used = [&](uint32_t n) {
@@ -594,7 +633,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) msa_attention_kvq_tiles_kerne
             #pragma unroll 1
             for (int k = from; k < to; ++k, ++tau) {
                 const uint32_t parity = (tau >> 1) & 1;
-                wait(c.s_full[tau & 1], parity);
+                wait_for_product(c.s_full[tau & 1], parity);
                 tc_fence_after();
                 const uint32_t params = ((tau % G::kParams) * kTileOfKeys + key) * 4;
                 const float sk = scale_of(lds32(smem + G::oKParams + params)) * a.scale, sv = scale_of(lds32(smem + G::oVParams + params));
@@ -645,7 +684,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) msa_attention_kvq_tiles_kerne
                 }
                 #pragma unroll
                 for (int i = 0; i < C; ++i) d[i] = exp2_approx(d[i]);
-                wait(c.vote[group][tau & 1], parity);
+                wait_for_warps(c.vote[group][tau & 1], parity);
                 if (*const_cast<volatile int*>(&c.hot[group][tau & 1])) {
                     // references go up to the maxima (a row's first one: to its maximum, whatever it is)
                     scores();
@@ -674,7 +713,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) msa_attention_kvq_tiles_kerne
                         l[i] *= __shfl_sync(0xffffffffu, f, i);
                     }
                     if (k > from) {                  // and O with them: the products so far are complete, this tile's waits for our weights
-                        wait(c.pv_done[(tau - 1) & 1], ((tau - 1) >> 1) & 1);
+                        wait_for_product(c.pv_done[(tau - 1) & 1], ((tau - 1) >> 1) & 1);
                         tc_fence_after();
                         #pragma unroll
                         for (int i = 0; i < C; i += 8) {
@@ -711,7 +750,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) msa_attention_kvq_tiles_kerne
                 mbar_arrive(smem_u32(&c.p_full[tau & 1]));
             }
             // ---- the unit's end: sums over the keys, O
-            wait(c.pv_done[(tau - 1) & 1], ((tau - 1) >> 1) & 1);
+            wait_for_product(c.pv_done[(tau - 1) & 1], ((tau - 1) >> 1) & 1);
             tc_fence_after();
             #pragma unroll
             for (int w = 16; w >= C; w >>= 1) {      // (fewer rows than lanes: whole sums first)
@@ -737,7 +776,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) msa_attention_kvq_tiles_kerne
             tmem_wait_ld();
             tc_fence_before();
             mbar_arrive(smem_u32(&c.o_free));
-            const bool ok = *const_cast<volatile int*>(&c.abort) == 0;
+            const bool ok = *const_cast<volatile int*>(&c.waits.abort) == 0;
             const int rows = u.real ? u.rows : 0, mains = u.T - u.row0;       // rows, and how many of them are main-stream ones
             if (u.whole) {
                 const float f = 1.f / sum;
@@ -868,7 +907,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) msa_attention_kvq_tiles_kerne
                 if (unit > 0) {                      // (the first unit's plan is there)
                     const bool more = line.next(a);
                     // (a unit's rows are free when all are done with the plan: its last S is complete then)
-                    if (unit >= 2) wait_for_unit(smem_u32(&c.plan_free[unit & 1]), ((unit - 2) >> 1) & 1, &c.abort, status);
+                    if (unit >= 2) wait_for_warps(c.plan_free[unit & 1], ((unit - 2) >> 1) & 1);
                     make_plan(u, more);
                 }
             }
@@ -893,6 +932,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) msa_attention_kvq_tiles_kerne
     __syncthreads();
     tc_fence_after();
     if (warp == kMmaWarp) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem));
+    if (tid == 0 && c.waits.abort != 0) set_status(a.ws, SS_ERR_DEVICE_TIMEOUT);
 }
 
 }  // namespace ss
