@@ -392,8 +392,8 @@ int32_t ss_kvq_read(const ss_kvq_cache* cache, const ss_kvq_rows* rows, const in
  * different shapes may share one that is large enough for each, in stream order, but it is not one of another entry point's.
  * A sequence with kv_len[b] over its capacity (or 2^31 - 2^16), with slots outside the slab or without nodes is skipped (its outputs are not
  * written); for the first two the status word is set to SS_ERR_CAPACITY.  With more than 16 query rows per head the warps of a CTA wait for one
- * another: SS_ERR_DEVICE_TIMEOUT means that a wait for data ran out (about a second, or workspace word 1 as for ss_msa_attention); the
- * workspace is to be zero-filled then.
+ * another: SS_ERR_DEVICE_TIMEOUT means that a wait for data ran out (about a second, or workspace word 1 as for ss_msa_attention): outputs
+ * whose computation that concerns are not written, and the workspace is to be zero-filled.
  * Limits: 65535 sequences and heads, SS_MAX_NODES nodes, SS_MAX_GAMMA streams, head_dim 64, 80 or 128.
  * Errors (nothing launched): SS_ERR_INVALID_ARG, SS_ERR_UNSUPPORTED, SS_ERR_WORKSPACE, SS_ERR_CUDA. */
 typedef struct ss_kvq_attn_params {

@@ -776,11 +776,13 @@ __global__ void __launch_bounds__(kTileThreads, 1) msa_attention_kvq_tiles_kerne
             tmem_wait_ld();
             tc_fence_before();
             mbar_arrive(smem_u32(&c.o_free));
-            const bool ok = *const_cast<volatile int*>(&c.waits.abort) == 0;
+            // Nothing that was computed from a wait that ran out is written or passed on.  Whoever left one early had set or seen `abort` before it came
+            // to the barrier that lies between its results and their use: so it is looked at behind that barrier.
+            const auto good = [&] { return *const_cast<volatile int*>(&c.waits.abort) == 0; };
             const int rows = u.real ? u.rows : 0, mains = u.T - u.row0;       // rows, and how many of them are main-stream ones
             if (u.whole) {
                 const float f = 1.f / sum;
-                if (quad == 0 && lane < C && ok && group * C + lane < rows) {
+                if (quad == 0 && lane < C && group * C + lane < rows && good()) {
                     const int n = group * C + lane;
                     float* lse = n < mains ? a.lse_main : a.lse_spec;
                     if (lse != nullptr) lse[u.out[n] / D] = (ref + log2f(sum)) * 0.6931471805599453f;
@@ -796,6 +798,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) msa_attention_kvq_tiles_kerne
                     st_shared_v4(weights + ((((i >> 3) + group * (C / 8)) ^ (key & 7)) << 4), y[0], y[1], y[2], y[3]);
                 }
                 named_barrier(bar, 128);
+                const bool ok = good();
                 // matrices of 8 dimensions (a word's) by 8 rows, transposed: a lane gets two dimensions of a row
                 #pragma unroll 1
                 for (int m0 = 4 * quad; m0 < D / 8 * (C / 8); m0 += 16) {
@@ -821,7 +824,8 @@ __global__ void __launch_bounds__(kTileThreads, 1) msa_attention_kvq_tiles_kerne
                 }
                 named_barrier(3 + kTileGroups, kTileSoftmax);
                 if (tid == 256) {
-                    c.joined = last_piece(counters + (u.first << u.team) + u.member, u.last - u.first + 1);
+                    // (a piece that is no good is not counted: its unit is never joined)
+                    c.joined = good() && last_piece(counters + (u.first << u.team) + u.member, u.last - u.first + 1);
                 }
                 named_barrier(3 + kTileGroups, kTileSoftmax);
                 if (c.joined) {
@@ -849,7 +853,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) msa_attention_kvq_tiles_kerne
                             for (int q = 0; q < 4; ++q)
                                 if (i + q < n) join_row(o, m, sm, st[q], u[q], v[q]);
                         }
-                        if (ok) store_row<D>(a, r < mains, u.out[r], d0, o, m, sm);
+                        store_row<D>(a, r < mains, u.out[r], d0, o, m, sm);
                     }
                 }
             }

@@ -46,3 +46,28 @@ def test_a_call_whose_waits_run_out_ends_and_says_so(api, name):
         x.run(ws)
         x.cache = near
         x.check([0, x.B - 1])
+
+
+@pytest.mark.parametrize("name", list(CALLS))
+def test_what_a_call_writes_whose_waits_run_out(api, name):
+    """Every row is either as it was or what it should be: nothing that a CTA that gave up has left reaches an output, not through the
+    partial rows of the CTAs that share its heads either."""
+    c = CALLS[name]
+    x = Layer(api, c["B"], c["H"], 128, c["lens"], [c["nodes"]] * c["B"], c["gamma"], seed=9)
+    ws = x.workspace()
+    words = ws.view(torch.int32)
+    x.run(ws)
+    x.check([0, x.B - 1])
+    want = [None if t is None else t.clone() for t in (x.o_main, x.o_spec, x.lse_main, x.lse_spec)]
+    x.cache = _in_host_memory(api, x)
+    for limit in (1, 8, 16, 32, 64, 128):                      # (longer bounds run out in some CTAs only)
+        for _ in range(4):
+            x.fresh()
+            words.zero_()
+            words[1] = limit
+            api.ss_msa_attention_kvq(x.params(ws))
+            torch.cuda.synchronize()
+            assert api.ss_status(ws) in (0, api.SS_ERR_DEVICE_TIMEOUT)
+            for t, w in zip((x.o_main, x.o_spec, x.lse_main, x.lse_spec), want):
+                if t is not None:
+                    assert ((t == w) | (t == 77.0)).all(), (limit, int(((t != w) & (t != 77.0)).sum()))
