@@ -2,8 +2,8 @@
 //
 // S^T = K Q^T and O^T = V^T P^T with 128 keys (dimensions) as the 128 lanes of TMEM and the N <= 64 query rows as columns: what
 // grows with the rows is the cheap side, and codes go from registers to TMEM as A operands, never through shared memory.
-//   K: the thread of a key turns the key's codes into bf16 128 + c (a mask and an or), one TMEM lane; one more step of the product, whose
-//      operands are 128 + z and -sum(q) in three bf16 terms, leaves sum q (c - z); the key's scale multiplies the lane's scores.
+//   K: the thread of a key turns the key's codes into bf16 c - z, exactly (128 + c by a mask and an or, less 128 + z), one TMEM lane; the key's
+//      scale multiplies the lane's scores.
 //   V: transposing loads (ldmatrix, 16 keys by 16 bytes) give a thread four keys' codes of two dimensions; a TMEM lane is a dimension.
 //      The scale is part of the weight that meets it.
 // Lane 32 w + x of V^T and O^T (w < D / 32) holds, for x < 16, the low codes of byte 16 w + x of a row, else the high codes of
@@ -20,10 +20,10 @@
 // decides) against 112; a unit's start counted in the deal of work 112 for 131; own warps for what comes before a unit 107.
 // Registers (72 each, all there are) decide too: what is called seldom is out of line where the loops around it then spill less (rows and
 // the wait for a unit: 104, inline 121; not the join: 125).
-// Rounding: keys and values are whole numbers below 2^8 in bf16, exactly; queries enter as they are; a weight p s_v is rounded once to
-// bf16 (2^-8 of itself), as the bf16 attention rounds p.  The sums of q (128 + c) are larger than those of q (c - z) by some 143 over
-// |c - z|: fp32 accumulators lose 2^-24 of them per step of 16, 10^-4 of a score unit for normal queries and keys, a tenth of what the
-// weights' rounding does.
+// Rounding: keys and values are whole numbers from -15 to 15 in bf16, exactly; queries enter as they are; a weight p s_v is rounded once to
+// bf16 (2^-8 of itself), as the bf16 attention rounds p.  Sums of q (c - z) are as large as the score's own terms, so a score is off by
+// some d / 16 steps of 2^-24 of sum |q k|.  (As sums of q (128 + c) less (128 + z) sum q, which saves a subtraction per two codes, scores of queries
+// with a mean and keys with a large channel were off by 3 10^-3; in time the subtractions and the additional step of the product are the same.)
 #pragma once
 #include "ss_tcgen05.cuh"
 
@@ -46,11 +46,11 @@ struct TileGeo {
     static constexpr int kBoxes = D > 64 ? 2 : 1, kBox = N * 128;
     static constexpr int kRowOfV = 64 * kQuads;                   // bytes of a bf16 row in lane order
     static constexpr int kP = kTileOfKeys * 128;
-    static constexpr int oP = 0, oQ = oP + 2 * kP, oZ = oQ + kBoxes * kBox, kRowsOfUnit = kBoxes * kBox + N * 32, oSums = oQ + 2 * kRowsOfUnit, oK = oSums + N * 64, oV = oK + kStages * kCodes;
+    static constexpr int oP = 0, oQ = oP + 2 * kP, kRowsOfUnit = kBoxes * kBox, oK = oQ + 2 * kRowsOfUnit, oV = oK + kStages * kCodes;
     static constexpr int oRows = oV + kStages * kCodes;           // 64 rows of bf16 values in the order of the lanes
     static constexpr int oKParams = oRows + 64 * kRowOfV, oVParams = oKParams + kParams * kTileOfKeys * 4;
     static constexpr int kBytes = oVParams + kParams * kTileOfKeys * 4;
-    static constexpr uint32_t kTmemK = 0, kTmemV = 144, kTmemS = 272, kTmemO = 272 + 2 * N;          // K: 72 columns a buffer, the last 8 for zero points
+    static constexpr uint32_t kTmemK = 0, kTmemV = 128, kTmemS = 256, kTmemO = 256 + 2 * N;          // K and V: 64 columns a buffer
     // bf16 operands, fp32 sums, 128 lanes, N columns; P^T is MN-major
     static constexpr uint32_t kIdescS = (1u << 4) | (1u << 7) | (1u << 10) | (static_cast<uint32_t>(N >> 3) << 17) | ((128u >> 4) << 24);
     static constexpr uint32_t kIdescPV = kIdescS | (1u << 16);
@@ -210,14 +210,6 @@ __device__ __forceinline__ void load_transposed_bytes(uint32_t addr, uint32_t& r
 __device__ __forceinline__ void load_transposed_halves(uint32_t addr, uint32_t (&r)[4]) {
     asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
 }
-// two columns
-__device__ __forceinline__ void tmem_store2(uint32_t addr, uint32_t x, uint32_t y) {
-    asm volatile("tcgen05.st.sync.aligned.32x32b.x2.b32 [%0], {%1, %2};" ::"r"(addr), "r"(x), "r"(y) : "memory");
-}
-// K-major operand of 16 columns without a swizzle: 8 rows by 16 bytes are 128 bytes in a row, the second 16 bytes of the rows 128 further
-__device__ __forceinline__ uint64_t desc_16_columns(uint32_t addr) {
-    return static_cast<uint64_t>((addr & 0x3FFFFu) >> 4) | (static_cast<uint64_t>(128 >> 4) << 16) | (static_cast<uint64_t>(256 >> 4) << 32) | (1ull << 46);
-}
 // codes to bf16: 128 + c, which 128 + z is taken from
 __device__ __forceinline__ uint32_t code_plus_128(uint32_t x) {
     uint32_t r;
@@ -256,10 +248,10 @@ __device__ __forceinline__ void prefetch_extra(const KvqArgs& a, const Extra& x,
     if (D > 64) prefetch_l2(src + D - 8);
 }
 
-// A unit's query rows as THREADS threads put them into shared memory at `rows_at`, what 128 + z meets, and which rows see which node.
-// BATCH: loads of a thread on their way at once; `sums`: [row][16] partial sums
+// A unit's query rows as THREADS threads put them into shared memory at `rows_at`, where their outputs go, and which rows see which node.
+// BATCH: loads of a thread on their way at once
 template <int D, int N, int THREADS, int BATCH>
-static __device__ __noinline__ void prepare_rows(const KvqArgs& a, TileUnit& u, uint32_t rows_at, float* sums, int t, int bar) {
+static __device__ __noinline__ void prepare_rows(const KvqArgs& a, TileUnit& u, uint32_t rows_at, int t) {
     using G = TileGeo<D, N>;
     constexpr int kItems = (N * (D / 8) + THREADS - 1) / THREADS;
     const int rows = u.rows, T = u.T, row0 = u.row0, h = u.head, b = u.b, lane = t & 31;
@@ -283,30 +275,14 @@ static __device__ __noinline__ void prepare_rows(const KvqArgs& a, TileUnit& u, 
         for (int q = 0; q < BATCH; ++q) {
             const int item = (i + q) * THREADS + t, r = item / (D / 8), at = item - r * (D / 8);
             if (item >= N * (D / 8)) break;
-            const uint32_t pair[4] = {v[q].x, v[q].y, v[q].z, v[q].w};
-            float sum = 0.f;
-            #pragma unroll
-            for (int n = 0; n < 4; ++n) sum += __uint_as_float(pair[n] << 16) + __uint_as_float(pair[n] & 0xffff0000u);
             st_shared_v4(rows_at + (at >> 3) * G::kBox + r * 128 + (((at & 7) ^ (r & 7)) << 4), v[q].x, v[q].y, v[q].z, v[q].w);
-            sums[r * 16 + at] = sum;
         }
     }
     for (int e = t >> 5; e < T; e += THREADS / 32) {
         const uint32_t lo = __ballot_sync(0xffffffffu, see[0] >> e & 1ull), hi = N > 32 ? __ballot_sync(0xffffffffu, see[1] >> e & 1ull) : 0u;
         if (lane == 0) u.see[e] = static_cast<unsigned long long>(hi) << 32 | lo;
     }
-    named_barrier(bar, THREADS);
-    if (t < N) {
-        float x = 0.f;
-        #pragma unroll
-        for (int i = 0; i < D / 8; ++i) x += sums[t * 16 + i];
-        x = -x;
-        const float t0 = round_bf16(x), t1 = round_bf16(x - t0), t2 = (x - t0) - t1;
-        const uint32_t row = rows_at + G::kBoxes * G::kBox + (t >> 3) * 256 + (t & 7) * 16;
-        st_shared_v4(row, pack2_bf16(t0, t1), pack2_bf16(t2, 0.f), 0u, 0u);
-        st_shared_v4(row + 128, 0u, 0u, 0u, 0u);
-        u.out[t] = t < rows ? row_offset(a, D, b, h, row0 + t, T) : 0;
-    }
+    if (t < N) u.out[t] = t < rows ? row_offset(a, D, b, h, row0 + t, T) : 0;
 }
 
 template <int D, int N>
@@ -391,11 +367,6 @@ __global__ void __launch_bounds__(kTileThreads, 1) msa_attention_kvq_tiles_kerne
         // ---- K ------------------------------------------------------------------------------
         const int key = tid;
         uint32_t unit = 0, copied = 0;               // units; tiles of codes copied or on their way
-        #pragma unroll
-        for (int i = 0; i < 2; ++i) {                // the columns of the zero points' step that stay zero
-            const uint32_t none[8] = {};
-            tmem_store<8, 0>(tmem + G::kTmemK + i * 72 + 64 + lanes, none);
-        }
         for (;; ++unit) {
             const TileUnit& u = plan_of(unit);
             if (u.done) break;
@@ -445,7 +416,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) msa_attention_kvq_tiles_kerne
                 }
                 if (tau >= 2) wait(c.s_full[tau & 1], ((tau - 2) >> 1) & 1);
                 tc_fence_after();
-                const uint32_t dst = tmem + G::kTmemK + (tau & 1) * 72 + lanes;
+                const uint32_t dst = tmem + G::kTmemK + (tau & 1) * 64 + lanes;
                 if (k < held) {
                     #pragma unroll
                     for (int i = 0; i < G::kWords; i += 8) {
@@ -454,7 +425,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) msa_attention_kvq_tiles_kerne
                         for (int q = 0; q < 8; ++q) {
                             if (i + q < G::kWords) {
                                 #pragma unroll
-                                for (int n = 0; n < 4; ++n) r[4 * q + n] = code_plus_128(w[i + q] >> (4 * n));
+                                for (int n = 0; n < 4; ++n) r[4 * q + n] = sub_bf16x2(code_plus_128(w[i + q] >> (4 * n)), z);
                             }
                         }
                         if (i + 8 <= G::kWords) tmem_store<32, 0>(dst + 4 * i, r);
@@ -481,7 +452,6 @@ __global__ void __launch_bounds__(kTileThreads, 1) msa_attention_kvq_tiles_kerne
                         else tmem_store<8, 0>(dst + 4 * i, r);
                     }
                 }
-                tmem_store2(dst + 64, z, z & 0xffffu);
                 tmem_wait_st();
                 tc_fence_before();
                 mbar_arrive(smem_u32(&c.k_full[tau & 1]));
@@ -614,8 +584,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) msa_attention_kvq_tiles_kerne
         // TMEM lane to dimension
         const int byte = 16 * quad + (lane & 15), dim = 8 * (byte >> 2) + ((byte & 1) << 2) + ((byte >> 1) & 1) + ((lane >> 4) << 1);
         if (!plan_of(0).done) {
-            // (partial sums where the weights will be)
-            prepare_rows<D, N, kTileSoftmax, 2>(a, c.unit[0], smem + G::oQ, reinterpret_cast<float*>(smem_raw + G::oP), tid - 256, 3 + kTileGroups);
+            prepare_rows<D, N, kTileSoftmax, 2>(a, c.unit[0], smem + G::oQ, tid - 256);
             fence_async_smem();
             named_barrier(3 + kTileGroups, kTileSoftmax);
             if (tid == 256) mbar_arrive(smem_u32(&c.rows_full[0]));
@@ -862,7 +831,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) msa_attention_kvq_tiles_kerne
     } else if (warp == kMmaWarp) {
         // ---- MMAs ---------------------------------------------------------------------------
         const uint32_t base = uniform(smem);
-        const uint64_t dq = desc_k_major(base + G::oQ), dz = desc_16_columns(base + G::oZ), dp = desc_mn_major(base + G::oP, 0);
+        const uint64_t dq = desc_k_major(base + G::oQ), dp = desc_mn_major(base + G::oP, 0);
         uint32_t unit = 0;
         const auto product = [&](uint32_t t, bool first) {       // O^T (+)= V^T P^T of tile t
             if (first && unit > 0) wait(c.o_free, (unit - 1) & 1);
@@ -886,11 +855,10 @@ __global__ void __launch_bounds__(kTileThreads, 1) msa_attention_kvq_tiles_kerne
                 wait(c.k_full[tau & 1], (tau >> 1) & 1);
                 if (tau >= 2) wait(c.s_free[tau & 1], ((tau - 2) >> 1) & 1);
                 tc_fence_after();
-                const uint32_t ka = tmem + G::kTmemK + (tau & 1) * 72, sd = tmem + G::kTmemS + (tau & 1) * N;
+                const uint32_t ka = tmem + G::kTmemK + (tau & 1) * 64, sd = tmem + G::kTmemS + (tau & 1) * N;
                 tile_mma<4>(sd, ka, dq + rows, G::kIdescS, 0u);
                 if constexpr (D == 128) tile_mma<4>(sd, ka + 32, dq + rows + (G::kBox >> 4), G::kIdescS, 1u);
                 if constexpr (D == 80) tile_mma<1>(sd, ka + 32, dq + rows + (G::kBox >> 4), G::kIdescS, 1u);
-                tile_mma<1>(sd, ka + 64, dz + rows, G::kIdescS, 1u);
                 tc_commit_e(smem_u32(&c.s_full[tau & 1]));
                 if (lane == 0) mbar_arrive(smem_u32(&c.s_full[tau & 1]));            // (passes on what the K warps have written: the keys' scales)
                 if (i > 0) product(tau - 1, i == 1);
@@ -903,7 +871,6 @@ __global__ void __launch_bounds__(kTileThreads, 1) msa_attention_kvq_tiles_kerne
     } else {
         // ---- preparing ----------------------------------------------------------------------
         const int t = tid - 32 * kPlanWarp, place = warp - kPlanWarp;
-        float* const sums = reinterpret_cast<float*>(smem_raw + G::oSums);           // [row][16] of partial sums of x
         for (uint32_t unit = 0;; ++unit) {
             TileUnit& u = c.unit[unit & 1];
             const uint32_t rows_at = smem + G::oQ + (unit & 1) * G::kRowsOfUnit;
@@ -926,7 +893,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) msa_attention_kvq_tiles_kerne
                 }
             }
             if (unit == 0) continue;                 // (the softmax warps, idle then, fetch the first unit's rows in a third of the time)
-            prepare_rows<D, N, kTilePrepare, 6>(a, u, rows_at, sums, t, 4 + kTileGroups);
+            prepare_rows<D, N, kTilePrepare, 6>(a, u, rows_at, t);
             fence_async_smem();
             named_barrier(4 + kTileGroups, kTilePrepare);
             if (t == 0) mbar_arrive(smem_u32(&c.rows_full[unit & 1]));           // (the query rows, and with them `out` and `see`)

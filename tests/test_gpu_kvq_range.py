@@ -125,3 +125,74 @@ def test_starts_at_the_ends_of_64_bits(api):
     assert (back[:, :4] == 9.0).all() and (other[:, :4] == 9.0).all()
     step = (k[:, 4].double().amax(-1).clamp(min=0) - k[:, 4].double().amin(-1).clamp(max=0)) / 15 * (1 + 2.0 ** -7)
     assert ((back[:, 4].double() - k[:, 4].double()).abs() <= (step * (1 + 16 * 2.0 ** -8))[..., None]).all()
+
+
+def _leaning(case, n, H, d, seed):
+    """Queries' lean, and keys [n][H][d], of models whose queries and keys are not centred."""
+    k = _normal((n, H, d), seed)
+    if case == "one channel":                                  # a key channel far larger than the others, queries with a mean
+        k[..., 7] = 60.0 * (1.0 - 2.0 * (torch.arange(H) % 2))
+        return 4.0, k
+    if case == "two channels":
+        k[..., 3], k[..., d - 2] = 45.0, -30.0
+        return -3.0, k
+    if case == "keys with a mean":
+        return 2.0, 0.1 * k + 5.0
+    k[:, :, 11] += 20.0                                        # "both in one channel"
+    return None, k
+
+
+@pytest.mark.parametrize("d", [64, 80, 128])
+@pytest.mark.parametrize("nodes,gamma", SHAPES)
+@pytest.mark.parametrize("case", ["one channel", "two channels", "keys with a mean", "both in one channel"])
+def test_queries_and_keys_that_are_not_centred(api, d, nodes, gamma, case):
+    """Scores are sums of q s (c - z), whose size bounds their error (see attention()): large sums of q alone, or of codes, must not
+    enter them.  Log-sum-exps show it."""
+    H, lens = 4, [40, 700]
+    x = Layer(api, 2, H, d, lens, [nodes] * 2, gamma, seed=17 + d)
+    for b, n in enumerate(lens):
+        lean, k = _leaning(case, n, H, d, 30 + b)
+        _put(x, b, k, _normal((n, H, d), 40 + b))
+    for t in (x.q_main, x.q_spec):
+        if t is not None and lean is not None:
+            t.copy_((t.float() + lean).to(torch.bfloat16))
+        elif t is not None:
+            t[..., 11] += 50.0
+    x.run()
+    x.check()
+
+
+def _single_scores(api, d, rows, case):
+    """A row that sees one cached key, its own and the root's lying far below, has that key's score as its log-sum-exp.  Its bound is that
+    of attention() for this key alone: (d + 16) 2^-23 sum |q| |k| scale for the products, and what exp and log lose."""
+    B, H = 32, 8
+    cache = api.empty_kvq_cache(1, 4 * B, H, d)
+    lean, k = _leaning(case, B, H, d, 50)
+    k = k.to(torch.bfloat16).cuda()[None, :, None]             # [1][B][1][H][d]
+    q = _normal((B, rows, H, d), 60)
+    if lean is None:
+        q[..., 11] += 50.0
+    q = (q + (lean or 0.0)).to(torch.bfloat16).cuda()
+    start, length = _i64([4 * b for b in range(B)]), _i32([1] * B)
+    api.ss_kvq_write(k, k, cache, start, _i32([0] * B), None, None, None, None)
+    below = (-200.0 * torch.sign(q.float())).to(torch.bfloat16)
+    lse = torch.zeros((B, rows, H), device="cuda")
+    kw = dict(q_main=q, o_main=torch.zeros_like(q), k_tree=below, v_tree=below, cache=cache, kv_start=start, kv_len=length, gamma=0, sm_scale=d ** -0.5,
+              trees=api.trees_to_device([api.ss_tree_build([-1] + [0] * (rows - 1), 0)] * B), lse_main=lse)
+    ws = api.workspace(api.ss_msa_attention_kvq_workspace_bytes(api.make_kvq_attn_params(**kw)))
+    api.ss_msa_attention_kvq(api.make_kvq_attn_params(workspace=ws, **kw))
+    assert api.ss_status(ws) == 0
+    keys = U.cache_values(cache, 0, "cuda")[0][::4]
+    score = torch.einsum("brhd,bhd->brh", q.double(), keys) * d ** -0.5
+    size = torch.einsum("brhd,bhd->brh", q.double().abs(), keys.abs()) * d ** -0.5
+    assert (score > -100.0).all()
+    bound = (d + 16) * 2.0 ** -23 * size + 2.0 ** -20 + 65 * 2.0 ** -24 + 2.0 ** -22 * score.abs() + 2.0 ** -20
+    err = (lse.double() - score).abs()
+    assert (err <= bound).all(), float((err / bound).max())
+
+
+@pytest.mark.parametrize("d", [64, 80, 128])
+@pytest.mark.parametrize("rows", [24, 64])
+@pytest.mark.parametrize("case", ["one channel", "two channels", "keys with a mean", "both in one channel"])
+def test_single_scores_of_blocks_that_are_not_centred(api, d, rows, case):
+    _single_scores(api, d, rows, case)
