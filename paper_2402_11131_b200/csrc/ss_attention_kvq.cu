@@ -163,11 +163,24 @@ __device__ __forceinline__ void mma_bf16(float (&d)[4], uint32_t a0, uint32_t a1
         : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
-// Codes as fp16 operands without any arithmetic: a code in the last four mantissa bits of a half word is the subnormal number c 2^-24,
-// one in the four bits above them 16 c 2^-24, exactly, and MMAs take subnormal numbers at full value.  So a mask is all it takes, and a
-// shift by 8 for the other two codes of a half word; the powers of two, and the zero points, are dealt with where sums begin and end.
+// Codes as fp16 operands: a code in the last four mantissa bits of a half word is the subnormal number c 2^-24, one in the four bits above
+// them 16 c 2^-24, exactly, and MMAs take subnormal numbers at full value.  So a mask is all it takes, and a shift by 8 for the other two
+// codes of a half word; the powers of two are dealt with where sums end.  V's zero points are too: the weights' sums of codes are at most
+// some 15 / |c - z| larger than those of values.  Not so K's: they are subtracted here, exactly again, so that scores are sums of q (c - z), no
+// larger than the score's own terms.  (With zero points applied to the sums of q, scores of queries with a mean and keys with a large
+// channel were off by up to 4 10^-4.  The subtractions cost 2 %: 64 users 236 -> 242 us, 100,000 keys and 5 rows 92.5 -> 94.7.)
 __device__ __forceinline__ uint32_t low_codes(uint32_t w) { return w & 0x000f000fu; }
 __device__ __forceinline__ uint32_t high_codes(uint32_t w) { return w & 0x00f000f0u; }
+__device__ __forceinline__ uint32_t sub_f16x2(uint32_t a, uint32_t b) {
+    uint32_t r;
+    asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+__device__ __forceinline__ uint32_t less_16_times(uint32_t a, uint32_t b) {
+    uint32_t r;
+    asm("{.reg .b32 m;\n\tmov.b32 m, 0xcc00cc00;\n\tfma.rn.f16x2 %0, %1, m, %2;}" : "=r"(r) : "r"(b), "r"(a));      // (-16 twice)
+    return r;
+}
 __device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
     asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
         : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
@@ -185,7 +198,7 @@ __device__ __forceinline__ uint32_t times16_bf16x2(uint32_t x) {
 }
 __device__ __forceinline__ uint32_t zero_pair(uint32_t a, uint32_t b) { return low_codes(__byte_perm(a, b, 0x7632)); }     // of two keys
 __device__ __forceinline__ float scale_of(uint32_t word) { return __uint_as_float(word << 16); }
-__device__ __forceinline__ float zero_over_16(uint32_t word) { return __uint_as_float(((word & 0xf0000u) << 3) | 0x3f800000u); }     // 1 + z / 16
+__device__ __forceinline__ uint32_t zero_of(uint32_t word) { return __byte_perm(word, 0u, 0x3232); }                            // twice
 constexpr float kCode = 5.9604644775390625e-08f;                 // 2^-24: what a code counts in an MMA
 
 // Pieces of a lone sequence's unit.  What joining p pieces takes grows with p, what the steps of one take falls as 1 / p: the best p grows
@@ -415,7 +428,7 @@ struct WarpState {
     float o[D / 16][NG][4], zo[NG][4];
     float ref[NG][2], sum[NG][2];
     uint32_t q[D / 16][NG][2];
-    float start[NG][2], factor[NG][2];               // of the lane's two rows: 16 sum(x) 2^-24; 2^24 2^e scale
+    float factor[NG][2];                             // of the lane's two rows: 2^24 2^e scale
     float weight;                                    // 2^(6 - r)
     float limit;                                     // V scales from here on raise r; 0: none seen yet
 };
@@ -507,13 +520,13 @@ __device__ __forceinline__ void prefix_chunk(WarpState<D, NG>& w, uint32_t stage
     constexpr uint32_t kWordsOfV = 4 * kChunk;
     uint32_t pa[2], pb[2];
     float d[2][NG][4];
-    // Scores.  With X = sum(x), sum x (c - z) = sum x c + 16 X - (1 + z / 16) 16 X: the second term is what the accumulators start
-    // from, and 1 + z / 16 is the zero point or'd into a float.
+    // Scores: sums of x (c - z)
     #pragma unroll
     for (int j = 0; j < 2; ++j) {
         pa[j] = lds32(stage + pl + 64 * j), pb[j] = lds32(stage + pl + 64 * j + 32);
         #pragma unroll
-        for (int n = 0; n < NG; ++n) d[j][n][0] = d[j][n][2] = w.start[n][0], d[j][n][1] = d[j][n][3] = w.start[n][1];
+        for (int n = 0; n < NG; ++n) d[j][n][0] = d[j][n][1] = d[j][n][2] = d[j][n][3] = 0.f;
+        const uint32_t za = zero_of(pa[j]), zb = zero_of(pb[j]);
         const uint32_t row = stage + kl + j * 16 * G::kRowBytes;
         uint32_t wa[4], wb[4];
         if constexpr (G::kWordsK == 4) {
@@ -529,28 +542,29 @@ __device__ __forceinline__ void prefix_chunk(WarpState<D, NG>& w, uint32_t stage
             #pragma unroll
             for (int s = 0; s < 2; ++s) {
                 const uint32_t u = wa[i] >> (8 * s), v = wb[i] >> (8 * s);
+                const uint32_t a0 = sub_f16x2(low_codes(u), za), a1 = sub_f16x2(low_codes(v), zb);
+                const uint32_t a2 = less_16_times(high_codes(u), za), a3 = less_16_times(high_codes(v), zb);
                 #pragma unroll
-                for (int n = 0; n < NG; ++n)
-                    mma_f16(d[j][n], low_codes(u), low_codes(v), high_codes(u), high_codes(v), w.q[2 * i + s][n][0], w.q[2 * i + s][n][1]);
+                for (int n = 0; n < NG; ++n) mma_f16(d[j][n], a0, a1, a2, a3, w.q[2 * i + s][n][0], w.q[2 * i + s][n][1]);
             }
         }
         if constexpr (D == 80) {
             const uint32_t tail = stage + kl - c * (4 * G::kWordsK) + j * 16 * G::kRowBytes + 32;
             const uint2 x = lds64(tail), y = lds64(tail + 8 * G::kRowBytes);
+            const uint32_t a0 = sub_f16x2(low_codes(x.x >> (4 * c)), za), a1 = sub_f16x2(low_codes(y.x >> (4 * c)), zb);
+            const uint32_t a2 = sub_f16x2(low_codes(x.y >> (4 * c)), za), a3 = sub_f16x2(low_codes(y.y >> (4 * c)), zb);
             #pragma unroll
-            for (int n = 0; n < NG; ++n)
-                mma_f16(d[j][n], low_codes(x.x >> (4 * c)), low_codes(y.x >> (4 * c)), low_codes(x.y >> (4 * c)), low_codes(y.y >> (4 * c)), w.q[4][n][0], w.q[4][n][1]);
+            for (int n = 0; n < NG; ++n) mma_f16(d[j][n], a0, a1, a2, a3, w.q[4][n][0], w.q[4][n][1]);
         }
     }
     #pragma unroll
     for (int j = 0; j < 2; ++j) {
-        const float sa = scale_of(pa[j]), sb = scale_of(pb[j]), za = zero_over_16(pa[j]), zb = zero_over_16(pb[j]);
+        const float sa = scale_of(pa[j]), sb = scale_of(pb[j]);
         #pragma unroll
         for (int n = 0; n < NG; ++n) {
             #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const float u = fmaf(i < 2 ? za : zb, -w.start[n][i & 1], d[j][n][i]) * (i < 2 ? sa : sb);
-                d[j][n][i] = fmaf(u, w.factor[n][i & 1], -w.ref[n][i & 1]);
+                d[j][n][i] = fmaf(d[j][n][i] * (i < 2 ? sa : sb), w.factor[n][i & 1], -w.ref[n][i & 1]);
             }
         }
         pa[j] = lds32(stage + pl + kWordsOfV + 64 * j), pb[j] = lds32(stage + pl + kWordsOfV + 64 * j + 32);
@@ -873,7 +887,6 @@ __global__ void __launch_bounds__(kThreads, NG == 1 ? 3 : 2) msa_attention_kvq_r
             // 2^e with the largest |q| 2^-e in [2^14, 2^15), kept where 2^e and 2^-e are normal numbers
             const uint32_t eb = min(max(max(top & 0xffffu, top >> 16) >> 7, 24u), 247u) - 14u;
             const float up = __uint_as_float(eb << 23), down = __uint_as_float((254u - eb) << 23);
-            float total = 0.f;
             #pragma unroll
             for (int i = 0; i < D / 16; ++i) {
                 #pragma unroll
@@ -881,17 +894,11 @@ __global__ void __launch_bounds__(kThreads, NG == 1 ? 3 : 2) msa_attention_kvq_r
                     const float x = __uint_as_float(v[i][k] << 16) * down, y = __uint_as_float(v[i][k] & 0xffff0000u) * down;
                     const float f = k && i < 2 * G::kWordsK ? 0.0625f : 1.f;         // (these meet high codes)
                     w.q[i][n][k] = pack2_f16(x * f, y * f);
-                    total += x + y;
                 }
             }
-            total += __shfl_xor_sync(0xffffffffu, total, 1);
-            total += __shfl_xor_sync(0xffffffffu, total, 2);
-            // a row's sum and factor go to the lanes that hold its scores: rows 2c and 2c + 1 of the group
+            // a row's factor goes to the lanes that hold its scores: rows 2c and 2c + 1 of the group
             #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                w.start[n][e] = __shfl_sync(0xffffffffu, total, 4 * (2 * c + e)) * (16.f * kCode);
-                w.factor[n][e] = __shfl_sync(0xffffffffu, up, 4 * (2 * c + e)) * (a.scale * (1.f / kCode));
-            }
+            for (int e = 0; e < 2; ++e) w.factor[n][e] = __shfl_sync(0xffffffffu, up, 4 * (2 * c + e)) * (a.scale * (1.f / kCode));
         }
         uint32_t stage = ring;
         int k = from * KS + slice;

@@ -196,3 +196,10 @@ def _single_scores(api, d, rows, case):
 @pytest.mark.parametrize("case", ["one channel", "two channels", "keys with a mean", "both in one channel"])
 def test_single_scores_of_blocks_that_are_not_centred(api, d, rows, case):
     _single_scores(api, d, rows, case)
+
+
+@pytest.mark.parametrize("d", [64, 80, 128])
+@pytest.mark.parametrize("rows", [1, 8, 12])
+@pytest.mark.parametrize("case", ["one channel", "two channels", "keys with a mean", "both in one channel"])
+def test_single_scores_of_few_rows_that_are_not_centred(api, d, rows, case):
+    _single_scores(api, d, rows, case)
