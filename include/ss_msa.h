@@ -333,7 +333,7 @@ int32_t ss_kv_compact(void* k_cache_all, void* v_cache_all, const ss_cache_layou
  * The attention reads a head's words slot after slot: param_slot_stride = 1 is the fast layout. */
 typedef struct ss_kvq_cache {
     int32_t n_layers, n_heads, head_dim;
-    int32_t device;                  /* the device that holds the cache: a call with another current device is refused; -1: not checked */
+    int32_t device;                  /* the device that holds the cache: a call with another current device is refused; -1: not checked; less: none, refused */
     void* k_codes;
     void* v_codes;
     uint32_t* k_params;

@@ -173,7 +173,7 @@ def native():
             torch.cuda.current_stream()                   # initialises CUDA if nothing has yet
         addresses = tuple(C.cast(getattr(lib(), name), C.c_void_p).value for name in _NATIVE_CALLS)
         _pycall.setup(SsError, torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice, AttnParams, CacheLayout, C.byref,
-                      C.ArgumentError, addresses, KvqAttnParams, KvqCache)
+                      C.ArgumentError, addresses, KvqAttnParams, KvqCache, torch.int32, torch.int64, torch.bfloat16)
         _native = _pycall
     return _native
 
@@ -365,7 +365,7 @@ def make_kvq_cache(k_codes: torch.Tensor, k_params: torch.Tensor, v_codes: torch
         raise ValueError("the parts of a cache lie on one device")
     c = KvqCache()
     c.n_layers, c.total_slots, c.n_heads, c.head_dim = k_codes.shape[0], k_codes.shape[1], k_codes.shape[2], 2 * k_codes.shape[3]
-    c.device = k_codes.device.index if k_codes.is_cuda else -1
+    c.device = k_codes.device.index if k_codes.is_cuda else -2          # (host memory: no call takes it)
     c.k_codes, c.v_codes, c.k_params, c.v_params = _ptr(k_codes), _ptr(v_codes), _ptr(k_params), _ptr(v_params)
     c.layer_stride, c.slot_stride, c.head_stride = k_codes.stride()[:3]
     c.param_layer_stride, c.param_slot_stride, c.param_head_stride = k_params.stride()
@@ -380,26 +380,17 @@ def empty_kvq_cache(n_layers: int, slots: int, n_heads: int, head_dim: int, devi
     return make_kvq_cache(codes[0], params[0], codes[1], params[1])
 
 
-def _check_rows(k, v, cache):
-    if k.dtype is not torch.bfloat16 or v.dtype is not torch.bfloat16 or k.device != v.device:
-        raise ValueError("rows are bf16 tensors on one device")
-    if isinstance(cache, KvqCache) and cache.device >= 0 and k.get_device() != cache.device:
-        raise ValueError("rows and cache lie on one device")
-
-
 def ss_kvq_write(k_rows, v_rows, cache: KvqCache, kv_start, kv_len_in, n_rows=None, path=None, kv_capacity=None, kv_len_out=None,
                  status=None, stream=None) -> None:
     """Quantises rows into the cache, in every layer (asynchronous on `stream`).  k_rows, v_rows: bf16 [n_layers][B][rows][H][d] (d
     contiguous); row r < n_rows[b] (int32 [B], None: all) goes to slot kv_start[b] + kv_len_in[b] + r, taken from row path[b][r]
     where a path (int32 [B][SS_PATH_STRIDE], a verification's accept_path) is given; kv_len_out[b] = kv_len_in[b] + n_rows[b].
     Sequences that do not fit are skipped; word 0 of `status` (a workspace) then says so."""
-    _check_rows(k_rows, v_rows, cache)
     (_native or native()).kvq_write(k_rows, v_rows, cache, kv_start, kv_len_in, n_rows, path, kv_capacity, kv_len_out, status, stream)
 
 
 def ss_kvq_read(cache: KvqCache, k_rows, v_rows, kv_start, first=None, n_rows=None, stream=None) -> None:
     """Rows of the cache as bf16, in every layer: k_rows[:, b, r] for r < n_rows[b] receives slot kv_start[b] + first[b] + r."""
-    _check_rows(k_rows, v_rows, cache)
     (_native or native()).kvq_read(cache, k_rows, v_rows, kv_start, first, n_rows, stream)
 
 
@@ -422,6 +413,11 @@ def make_kvq_attn_params(*, q_main, o_main, k_tree, v_tree, cache: KvqCache, kv_
         for t in (q_main, o_main, k_tree, v_tree, q_spec, k_spec, v_spec, o_spec, lse_main, lse_spec, kv_start, kv_len, kv_capacity, trees, workspace):
             if t is not None and t.get_device() != cache.device:
                 raise ValueError("the call's tensors lie on the cache's device")
+        for t, dtype in ((kv_start, torch.int64), (kv_len, torch.int32), (kv_capacity, torch.int32)):
+            if t is not None and (t.dtype is not dtype or t.numel() < B or not t.is_contiguous()):
+                raise ValueError("kv_start is a contiguous int64 tensor of [B], kv_len and kv_capacity are int32 ones")
+        if trees.numel() * trees.element_size() < B * C.sizeof(TreeDesc) or not trees.is_contiguous():
+            raise ValueError("trees holds a descriptor per sequence")
     p = KvqAttnParams()
     p.batch, p.gamma, p.max_nodes, p.layer, p.sm_scale = B, int(gamma), Tmax, int(layer), float(sm_scale)
     p.q_main, p.o_main, p.k_tree, p.v_tree = _ptr(q_main), _ptr(o_main), _ptr(k_tree), _ptr(v_tree)

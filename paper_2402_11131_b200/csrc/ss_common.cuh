@@ -38,6 +38,7 @@ inline int32_t kvq_check_cache(const ss_kvq_cache& c) {
         ((reinterpret_cast<uintptr_t>(c.k_params) | reinterpret_cast<uintptr_t>(c.v_params)) & 3u))
         return SS_ERR_INVALID_ARG;
     if (static_cast<uintptr_t>(c.layer_stride | c.slot_stride | c.head_stride) & unit) return SS_ERR_UNSUPPORTED;
+    if (c.device < -1) return SS_ERR_INVALID_ARG;
     int dev = -1;
     if (c.device >= 0 && (cudaGetDevice(&dev) != cudaSuccess || dev != c.device)) return SS_ERR_INVALID_ARG;
     return SS_OK;

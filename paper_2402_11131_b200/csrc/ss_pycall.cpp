@@ -4,7 +4,7 @@
 // A decode step of a small model is a handful of calls of 3 to 8 us of GPU time each, so the host has to spend less than that
 // on a call.  Through ctypes, with the pointers collected in Python, a verification call took 5.6 us, of which the launch is
 // 2.6; here it takes 3.5 us.  Only the CPython API is used: a tensor is any object with `data_ptr()`, `shape` and
-// `nbytes`.
+// `nbytes` (and, for the cache in 4 bits, `stride()`, `dtype`, `is_contiguous()` and `get_device()`).
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 
@@ -12,10 +12,12 @@
 
 namespace {
 
-PyObject *s_data_ptr, *s_shape, *s_stride, *s_nbytes, *s_cuda_stream;      // interned attribute names
+// interned attribute names
+PyObject *s_data_ptr, *s_shape, *s_stride, *s_nbytes, *s_cuda_stream, *s_dtype, *s_is_contiguous, *s_get_device;
 PyObject *g_error, *g_raw_stream, *g_device;                    // SsError; torch's raw current stream and current device
 PyObject *g_attn_params, *g_cache_layout;                       // the ctypes structures of ss_attn_params and ss_cache_layout,
 PyObject *g_kvq_params, *g_kvq_cache;                           // of ss_kvq_attn_params and ss_kvq_cache
+PyObject *g_int32, *g_int64, *g_bfloat16;                       // torch's types
 // the entry points, in the order in which setup() takes them
 #define SS_FUNCTIONS(F)                                                                                                 \
     F(ss_msa_attention) F(ss_tree_verify) F(ss_tree_verify_soft) F(ss_tree_verify_sampled) F(ss_tree_prune)             \
@@ -74,6 +76,11 @@ struct Args {
         strides(v, 5, y);
         r.k = ptr(k), r.v = ptr(v);
         if (!ok) return r;
+        if (!is_of(k, g_bfloat16) || !is_of(v, g_bfloat16) || !on_device(k, cache) || !on_device(v, cache)) {
+            if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "rows are bf16 tensors on the cache's device");
+            ok = false;
+            return r;
+        }
         bool same = x[4] == 1 || n[4] <= 1;
         for (int i = 0; i < 5; ++i) same = same && n[i] == m[i] && (x[i] == y[i] || n[i] <= 1);
         if (!same || n[0] != cache->n_layers || n[3] != cache->n_heads || n[4] != cache->head_dim || n[1] > INT32_MAX || n[2] > INT32_MAX) {
@@ -85,6 +92,35 @@ struct Args {
         r.layer_stride = n[0] > 1 ? x[0] : 0, r.batch_stride = n[1] > 1 ? x[1] : 0, r.row_stride = n[2] > 1 ? x[2] : 0, r.head_stride = n[3] > 1 ? x[3] : 0;
         r.batch = static_cast<int32_t>(n[1]), r.max_rows = static_cast<int32_t>(n[2]);
         return r;
+    }
+    // `count` whole numbers of type T next to each other on the cache's device, or None (which the library refuses where it has to)
+    template <typename T>
+    T* numbers(int i, long long count, const ss_kvq_cache* cache, const char* what) {
+        if (!ok || a[i] == Py_None) return nullptr;
+        if (!is_of(i, sizeof(T) == 8 ? g_int64 : g_int32) || static_cast<long long>(nbytes(i)) < count * static_cast<long long>(sizeof(T)) ||
+            (count > 1 && !truth(i, s_is_contiguous)) || !on_device(i, cache)) {
+            if (!PyErr_Occurred())
+                PyErr_Format(PyExc_ValueError, "%s: expected %lld contiguous int%d numbers on the cache's device", what, count, static_cast<int>(8 * sizeof(T)));
+            ok = false;
+        }
+        return as<T>(i);
+    }
+    bool is_of(int i, PyObject* type) {
+        PyObject* const dtype = PyObject_GetAttr(a[i], s_dtype);
+        Py_XDECREF(dtype);                           // (the type itself is kept by torch)
+        return dtype == type;
+    }
+    bool truth(int i, PyObject* method) {
+        PyObject* const r = PyObject_CallMethodNoArgs(a[i], method);
+        const bool yes = r == Py_True;
+        Py_XDECREF(r);
+        return yes;
+    }
+    bool on_device(int i, const ss_kvq_cache* cache) {
+        PyObject* const r = PyObject_CallMethodNoArgs(a[i], s_get_device);
+        const long d = r ? PyLong_AsLong(r) : -1;
+        Py_XDECREF(r);
+        return cache->device >= 0 ? d == cache->device : d >= 0;
     }
     size_t nbytes(int i) {
         if (!ok) return 0;
@@ -300,13 +336,18 @@ SS_ENTRY(msa_attention_kvq, 2)
 
 SS_ENTRY(kvq_write, 11)
     Py_buffer view;
-    const int64_t* ks = a.as<int64_t>(3);
-    const int32_t *kl = a.as<int32_t>(4), *nr = a.as<int32_t>(5), *pa = a.as<int32_t>(6), *kc = a.as<int32_t>(7);
-    int32_t* ko = a.as<int32_t>(8);
-    void* const status = a.ptr(9);
     void* const s = a.stream(10);
     const ss_kvq_cache* const ca = a.structure<ss_kvq_cache>(2, g_kvq_cache, &view);
     const ss_kvq_rows r = a.rows(0, 1, ca);
+    const int64_t* ks = a.numbers<int64_t>(3, r.batch, ca, "kv_start");
+    const int32_t *kl = a.numbers<int32_t>(4, r.batch, ca, "kv_len_in"), *nr = a.numbers<int32_t>(5, r.batch, ca, "n_rows");
+    const int32_t *pa = a.numbers<int32_t>(6, static_cast<long long>(r.batch) * SS_PATH_STRIDE, ca, "path"), *kc = a.numbers<int32_t>(7, r.batch, ca, "kv_capacity");
+    int32_t* ko = a.numbers<int32_t>(8, r.batch, ca, "kv_len_out");
+    void* const status = a.ptr(9);
+    if (a.ok && status && (a.nbytes(9) < sizeof(int32_t) || !a.on_device(9, ca))) {
+        if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "status: expected a workspace on the cache's device");
+        a.ok = false;
+    }
     if (!a.ok && view.obj) PyBuffer_Release(&view);
     SS_CALL(g_lib.ss_kvq_write(&r, ca, ks, kl, nr, pa, kc, ko, status, s))
     PyBuffer_Release(&view);
@@ -315,11 +356,11 @@ SS_ENTRY(kvq_write, 11)
 
 SS_ENTRY(kvq_read, 7)
     Py_buffer view;
-    const int64_t* ks = a.as<int64_t>(3);
-    const int32_t *fi = a.as<int32_t>(4), *nr = a.as<int32_t>(5);
     void* const s = a.stream(6);
     const ss_kvq_cache* const ca = a.structure<ss_kvq_cache>(0, g_kvq_cache, &view);
     const ss_kvq_rows r = a.rows(1, 2, ca);
+    const int64_t* ks = a.numbers<int64_t>(3, r.batch, ca, "kv_start");
+    const int32_t *fi = a.numbers<int32_t>(4, r.batch, ca, "first"), *nr = a.numbers<int32_t>(5, r.batch, ca, "n_rows");
     if (!a.ok && view.obj) PyBuffer_Release(&view);
     SS_CALL(g_lib.ss_kvq_read(ca, &r, ks, fi, nr, s))
     PyBuffer_Release(&view);
@@ -327,8 +368,8 @@ SS_ENTRY(kvq_read, 7)
 }
 
 // setup(SsError, raw_stream(device) -> int, device() -> int, AttnParams, CacheLayout, ctypes.byref, ctypes.ArgumentError,
-//       addresses of SS_FUNCTIONS: a tuple of int, KvqAttnParams, KvqCache)
-SS_ENTRY(setup, 10)
+//       addresses of SS_FUNCTIONS: a tuple of int, KvqAttnParams, KvqCache, torch.int32, torch.int64, torch.bfloat16)
+SS_ENTRY(setup, 13)
     (void)a; (void)st;
     PyObject* const at = argv[7];
     Py_ssize_t n = 0;
@@ -339,9 +380,9 @@ SS_ENTRY(setup, 10)
     ++n;
     SS_FUNCTIONS(SS_TAKE)
     g_lib = lib;
-    PyObject** const kept[10] = {&g_error, &g_raw_stream, &g_device, &g_attn_params, &g_cache_layout, &g_byref, &g_argument_error, nullptr, &g_kvq_params,
-                                 &g_kvq_cache};
-    for (int i = 0; i < 10; ++i)
+    PyObject** const kept[13] = {&g_error, &g_raw_stream, &g_device, &g_attn_params, &g_cache_layout, &g_byref, &g_argument_error, nullptr, &g_kvq_params,
+                                 &g_kvq_cache, &g_int32, &g_int64, &g_bfloat16};
+    for (int i = 0; i < 13; ++i)
         if (kept[i]) Py_XSETREF(*kept[i], Py_NewRef(argv[i]));
     Py_RETURN_NONE;
 }
@@ -361,5 +402,8 @@ PyMODINIT_FUNC PyInit__pycall() {
     s_stride = PyUnicode_InternFromString("stride");
     s_nbytes = PyUnicode_InternFromString("nbytes");
     s_cuda_stream = PyUnicode_InternFromString("cuda_stream");
+    s_dtype = PyUnicode_InternFromString("dtype");
+    s_is_contiguous = PyUnicode_InternFromString("is_contiguous");
+    s_get_device = PyUnicode_InternFromString("get_device");
     return PyModule_Create(&module);
 }
