@@ -398,7 +398,8 @@ def make_kvq_attn_params(*, q_main, o_main, k_tree, v_tree, cache: KvqCache, kv_
                          k_spec=None, v_spec=None, o_spec=None, kv_capacity=None, lse_main=None, lse_spec=None,
                          workspace=None) -> KvqAttnParams:
     """Fills ss_kvq_attn_params from tensors.  q_main, o_main, k_tree, v_tree: bf16 [B][Tmax][H][d]; *_spec: bf16
-    [B][Tmax][gamma][H][d]; contiguous, on the cache's device."""
+    [B][Tmax][gamma][H][d]; contiguous, on the cache's device.  The parameters keep the cache's tensors, as the cache does, not the
+    others."""
     B, Tmax, H, d = q_main.shape
     if (H, d) != (cache.n_heads, cache.head_dim):
         raise ValueError("the cache holds %d heads of %d, the queries have %d of %d" % (cache.n_heads, cache.head_dim, H, d))
@@ -423,6 +424,7 @@ def make_kvq_attn_params(*, q_main, o_main, k_tree, v_tree, cache: KvqCache, kv_
     p.q_main, p.o_main, p.k_tree, p.v_tree = _ptr(q_main), _ptr(o_main), _ptr(k_tree), _ptr(v_tree)
     p.q_spec, p.k_spec, p.v_spec, p.o_spec = _ptr(q_spec), _ptr(k_spec), _ptr(v_spec), _ptr(o_spec)
     p.cache = cache
+    p.cache_tensors = getattr(cache, "tensors", None)     # (the copy above has the pointers only)
     p.kv_start, p.kv_len, p.kv_capacity, p.trees = _ptr(kv_start), _ptr(kv_len), _ptr(kv_capacity), _ptr(trees)
     p.lse_main, p.lse_spec = _ptr(lse_main), _ptr(lse_spec)
     p.workspace = _ptr(workspace)

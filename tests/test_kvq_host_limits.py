@@ -1,5 +1,7 @@
 """Host-side checks of the cache in 4 bits: what its calls refuse before any launch, sizes and tensors at the edge of what they take."""
 import ctypes as C
+import gc
+import weakref
 
 import pytest
 
@@ -106,3 +108,18 @@ def test_attention_parameters_refuse_whole_numbers_of_other_types_and_sizes(lib)
         for b in bad:
             with pytest.raises(ValueError):
                 api.make_kvq_attn_params(**dict(ok, **gpu(**{name: b})))
+
+
+def test_attention_parameters_keep_the_cache(lib):
+    """A cache that only its parameters know is not freed under them."""
+    q, i = torch.zeros((1, 2, 3, 64), dtype=torch.bfloat16), torch.zeros(1, dtype=torch.int64)
+    cache = api.empty_kvq_cache(1, 10, 3, 64, device="cpu")
+    parts = [weakref.ref(t) for t in cache.tensors]
+    p = api.make_kvq_attn_params(q_main=q, o_main=q, k_tree=q, v_tree=q, cache=cache, kv_start=i, kv_len=i.int(), trees=i, gamma=0, sm_scale=1.0)
+    del cache
+    gc.collect()
+    assert all(r() is not None for r in parts)
+    assert p.cache.k_codes == parts[0]().data_ptr()
+    del p
+    gc.collect()
+    assert all(r() is None for r in parts)
