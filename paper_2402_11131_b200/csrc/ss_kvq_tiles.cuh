@@ -170,21 +170,20 @@ static __device__ __noinline__ void wait_for_product_slow(uint32_t bar, uint32_t
 
 template <int C>
 __device__ __forceinline__ void tmem_load(uint32_t addr, uint32_t (&r)[C]) {
-    if constexpr (C == 32) tmem_ld32<0>(addr, r);
-    else if constexpr (C == 16) tmem_ld16<0>(addr, r);
+    static_assert(C == 8 || C == 16, "columns");
+    if constexpr (C == 16) tmem_ld16<0>(addr, r);
     else
         asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
                      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]) : "r"(addr) : "memory");
 }
-template <int C, int O, int M>
+// 8 or 32 columns
+template <int C, int M>
 __device__ __forceinline__ void tmem_store(uint32_t addr, const uint32_t (&r)[M]) {
-    if constexpr (C == 32)
-        asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
-                     "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31};" ::SS_W16(r, O), SS_W16(r, O + 16), "r"(addr) : "memory");
-    else if constexpr (C == 16) tmem_st16<O>(addr, r);
+    static_assert(C == 8 || (C == 32 && M == 32), "columns");
+    if constexpr (C == 32) tmem_st32(addr, r);
     else
         asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%8], {%0,%1,%2,%3,%4,%5,%6,%7};"
-                     ::"r"(r[O]), "r"(r[O + 1]), "r"(r[O + 2]), "r"(r[O + 3]), "r"(r[O + 4]), "r"(r[O + 5]), "r"(r[O + 6]), "r"(r[O + 7]), "r"(addr) : "memory");
+                     ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(addr) : "memory");
 }
 // 16 lanes by 32 columns: r[2 k + e] is column 4 k + lane % 4 of TMEM lane lane / 4 + 8 e
 __device__ __forceinline__ void tmem_store_lanes16(uint32_t addr, const uint32_t (&r)[16]) {
@@ -428,8 +427,8 @@ __global__ void __launch_bounds__(kTileThreads, 1) msa_attention_kvq_tiles_kerne
                                 for (int n = 0; n < 4; ++n) r[4 * q + n] = sub_bf16x2(code_plus_128(w[i + q] >> (4 * n)), z);
                             }
                         }
-                        if (i + 8 <= G::kWords) tmem_store<32, 0>(dst + 4 * i, r);
-                        else tmem_store<8, 0>(dst + 4 * i, r);       // (80: the last two words)
+                        if (i + 8 <= G::kWords) tmem_store<32>(dst + 4 * i, r);
+                        else tmem_store<8>(dst + 4 * i, r);       // (80: the last two words)
                     }
                 } else {
                     const __nv_bfloat16* src = nullptr;
@@ -448,8 +447,8 @@ __global__ void __launch_bounds__(kTileThreads, 1) msa_attention_kvq_tiles_kerne
                             if (src && i + q < G::kWords) v = *reinterpret_cast<const uint4*>(src + 8 * (i + q));
                             r[4 * q] = v.x, r[4 * q + 1] = v.y, r[4 * q + 2] = v.z, r[4 * q + 3] = v.w;
                         }
-                        if (i + 8 <= G::kWords) tmem_store<32, 0>(dst + 4 * i, r);
-                        else tmem_store<8, 0>(dst + 4 * i, r);
+                        if (i + 8 <= G::kWords) tmem_store<32>(dst + 4 * i, r);
+                        else tmem_store<8>(dst + 4 * i, r);
                     }
                 }
                 tmem_wait_st();
@@ -575,7 +574,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) msa_attention_kvq_tiles_kerne
     } else if (warp < kMmaWarp) {
         // ---- softmax ------------------------------------------------------------------------
         const int group = (warp - 8) >> 2, key = 32 * quad + lane, bar = 3 + group;
-        constexpr uint32_t all = C == 32 ? 0xffffffffu : (1u << C) - 1u;
+        constexpr uint32_t all = (1u << C) - 1u;
         uint32_t unit = 0;
         int* const counters = reinterpret_cast<int*>(a.ws + kWsHeaderBytes);
         float* const partial = reinterpret_cast<float*>(a.ws + kWsHeaderBytes + kCounterBytes);
@@ -691,7 +690,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) msa_attention_kvq_tiles_kerne
                             tmem_wait_ld();
                             #pragma unroll
                             for (int q = 0; q < 8; ++q) o[q] = __float_as_uint(__uint_as_float(o[q]) * __shfl_sync(0xffffffffu, f, i + q));
-                            tmem_store<8, 0>(tmem + G::kTmemO + group * C + i + lanes, o);
+                            tmem_store<8>(tmem + G::kTmemO + group * C + i + lanes, o);
                         }
                         tmem_wait_st();
                         tc_fence_before();
