@@ -168,7 +168,8 @@ __device__ __forceinline__ void mma_bf16(float (&d)[4], uint32_t a0, uint32_t a1
 // codes of a half word; the powers of two are dealt with where sums end.  V's zero points are too: the weights' sums of codes are at most
 // some 15 / |c - z| larger than those of values.  Not so K's: they are subtracted here, exactly again, so that scores are sums of q (c - z), no
 // larger than the score's own terms.  (With zero points applied to the sums of q, scores of queries with a mean and keys with a large
-// channel were off by up to 4 10^-4.  The subtractions cost 2 %: 64 users 236 -> 242 us, 100,000 keys and 5 rows 92.5 -> 94.7.)
+// channel were off by up to 4 10^-4.  The subtractions cost 1.5 to 2 %: 100,000 keys and 5 rows 93.2 -> 94.6 us, 16 users' tokens 42.7 -> 43.5;
+// nothing that shows where memory bounds: 64 users.)
 __device__ __forceinline__ uint32_t low_codes(uint32_t w) { return w & 0x000f000fu; }
 __device__ __forceinline__ uint32_t high_codes(uint32_t w) { return w & 0x00f000f0u; }
 __device__ __forceinline__ uint32_t sub_f16x2(uint32_t a, uint32_t b) {
@@ -202,8 +203,10 @@ __device__ __forceinline__ uint32_t zero_of(uint32_t word) { return __byte_perm(
 constexpr float kCode = 5.9604644775390625e-08f;                 // 2^-24: what a code counts in an MMA
 
 // Pieces of a lone sequence's unit.  What joining p pieces takes grows with p, what the steps of one take falls as 1 / p: the best p grows
-// as the root of the steps.  (Two heads with 20,000 keys, one row: 14.6 us; in as many pieces as there are CTAs 22.7, with twice the
+// as the root of the steps.  (Two heads of 64 with 20,000 keys, one row: 14.6 us; in as many pieces as there are CTAs 22.7, with twice the
 // root as the limit 0.8 more.)  Two steps are not worth a join at all (7.6 against 8.5 us).
+// Not the fewest pieces for their longest one: 2048 keys are 17 steps in 12 pieces of one or two, which nine would be as well (8 rows: 13.4 us;
+// by the kernel for 16, whose grid allows nine, 11.6).  And equal pieces for all units leave CTAs over: 28 of 444 with 32 heads, 20 of 148 on tcgen05.
 __device__ __forceinline__ int most_pieces(int steps) { return steps < 3 ? 1 : static_cast<int>(3.f * sqrtf(static_cast<float>(steps))); }
 
 // The line of steps as one CTA sees it (every thread, or one warp of a role, works it out for itself)
@@ -378,7 +381,7 @@ __device__ __forceinline__ void join_row(float (&o)[8], float& m, float& l, cons
 // S^T = K Q^T and O^T = V^T P^T on mma.sync m16n8k16 with the keys (the dimensions) as the 16 rows of A and NG groups of 8 query
 // rows as N: a CTA of 4 warps, each with an online softmax of its own over its chunks of the CTA's piece of a unit, its codes on their way
 // through a ring of its own in shared memory.
-// What bounds it: with one row the bytes (64 users with up to 8191 keys: 229 us for 178 of HBM), from some eight rows on, and in long
+// What bounds it: with one row the bytes (64 users with up to 8191 keys: 224 to 231 us for 178 of HBM), from some eight rows on, and in long
 // sequences, the instructions that make fragments of codes and weights of scores, which is why codes are taken as they lie
 // (below: a mask, no conversion) and why keys are the wide side of the products.  Short calls are a chain of latencies: lengths, codes,
 // a few steps, partial rows and their join.
@@ -1047,10 +1050,11 @@ struct KvqPlan {
 static KvqPlan kvq_plan(const ss_kvq_attn_params& p) {
     const int rows = q_rows(p);
     // Up to 8 rows the rows are one group: three CTAs per SM, and nothing is spent on the second group's padding (16 users with 512 to 4096
-    // keys, a row each: 43 us, with two groups 51; 32 heads of 50,000 keys, 8 rows: 56 and 63; 512 keys 10.1 and 10.2; 2048 keys 13.4 and
-    // 11.7, the other way round).  From 17 rows on tcgen05 is faster at all lengths (32 rows: 16 users 86 us, by two groups of 16 rows 121;
-    // 50,000 keys 107 and 125; 512 keys 12.9 and 14.3); up to 16 it is slower where it counts (12 rows: 16 users 85 and 65 us; 50,000 keys
-    // 105 and 67; 512 keys 11.5 and 12.4: only the device knows the lengths).  32 rows in the kernel for 64 cost a sixth (102 us).
+    // keys, a row each: 43 us, with two groups 52; 32 heads of 50,000 keys, 8 rows: 57 and 65; 512 keys 9.8 and 10.0; 2048 keys 13.4 and
+    // 11.6, the other way round for want of fewer pieces, see most_pieces).  From 17 rows on tcgen05 is faster at all lengths (32 rows: 16 users
+    // 84 us, by two groups of 16 rows 124; 50,000 keys 103 and 126; 512 keys 12.1 and 14.8); up to 16 it is slower where it counts (12 rows: 16
+    // users 83 and 63 us; 50,000 keys 101 and 68; 512 keys 11.5 and 11.9: only the device knows the lengths).  32 rows in the kernel for 64
+    // cost a sixth (100 us).
     KvqPlan k{0, rows <= 8 ? 1 : 2, 0, 0};
     if (rows > 16) k.tile = rows <= 32 ? 32 : 64;
     k.block = k.tile > 0 ? k.tile : 8 * k.groups;

@@ -1,8 +1,8 @@
 // Rows into and out of a cache held in 4 bits (format and layout: ss_msa.h).  Compiled without fast-math: scales and codes are
 // defined bit by bit.
 //
-// Both kernels stream: HBM bounds them, with the instructions per value (13 of a write, 78 % of the issue slots) close behind.  Four
-// users' prompts into eight layers, 8240 rows of 32 x 128 each: written in 252 us (1.32 GB, 5.2 TB/s), read back in 220 (1.31 GB, 6.0 TB/s).
+// Both kernels stream: HBM bounds them, with the instructions per value (12 of a write, 73 % of the issue slots) close behind.  Four
+// users' prompts into eight layers, 8240 rows of 32 x 128 each: written in 243 us (1.31 GB, 5.4 TB/s), read back in 222 (1.31 GB, 5.9 TB/s).
 // One layer of 2048 slots is read in 7.9 us, 4 of them the launch and one trip to memory.  A thread holds 16 values, 8 at dimension 8 at and 8 at D / 2 + 8 at: a row of a head is 4, 5
 // or 8 neighbouring lanes that read (or write) runs of 16 bytes next to each other, and find the row's extremes with three exchanges.
 //

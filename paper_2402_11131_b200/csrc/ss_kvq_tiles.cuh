@@ -15,7 +15,7 @@
 // the roles work on different tiles and units.
 //
 // What bounds it: each role's chain of latencies per tile (loads, conversion, TMEM round trip, hand-over), some 1800 to 2300 cycles of 128 keys
-// by 64 rows whatever the role, where the MMAs need 300 and the exponentials 512: 16 users with 512 to 4096 keys 104 us for 27.5 of HBM.
+// by 64 rows whatever the role, where the MMAs need 300 and the exponentials 512: 16 users with 512 to 4096 keys 103 us for 27.5 of HBM.
 // On the way there: one softmax group per 32 rows 143 us, four 130; weights without a vote on the references 118 (a sum per tile
 // decides) against 112; a unit's start counted in the deal of work 112 for 131; own warps for what comes before a unit 107.
 // Registers (72 each, all there are) decide too: what is called seldom is out of line where the loops around it then spill less (rows and
