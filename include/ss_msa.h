@@ -386,6 +386,8 @@ int32_t ss_kvq_read(const ss_kvq_cache* cache, const ss_kvq_rows* rows, const in
  * per head (max_nodes * (1 + gamma)) to fp16 under a power of two that follows the largest s_v (11 bits, down to 2^-31 of it), with more to bf16, as
  * ss_msa_attention rounds p.  Sums, statistics and both products accumulate in fp32.  That holds for values below 2^90 and queries below
  * 2^120 in magnitude; beyond that the weights of the keys behind the prefix lose bits, and sums or queries may pass the range of their types.
+ * Keys of nodes and streams that a row does not see may hold anything; their values have to be finite, since a weight of zero times a value that is not a
+ * number is none either.
  * The keys of all heads are dealt out evenly over the GPU, whatever the lengths; a head that several CTAs share leaves partial
  * rows in the workspace, and the last of them to finish joins them in key order: results do not depend on the order of arrival,
  * and no CTA waits for another.  The workspace holds the counters of arrivals, zero between calls, and those rows: calls of

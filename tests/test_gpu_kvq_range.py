@@ -203,3 +203,41 @@ def test_single_scores_of_blocks_that_are_not_centred(api, d, rows, case):
 @pytest.mark.parametrize("case", ["one channel", "two channels", "keys with a mean", "both in one channel"])
 def test_single_scores_of_few_rows_that_are_not_centred(api, d, rows, case):
     _single_scores(api, d, rows, case)
+
+
+@pytest.mark.parametrize("d", [64, 80, 128])
+@pytest.mark.parametrize("nodes,gamma", SHAPES)
+@pytest.mark.parametrize("q_scale,k_scale", [(2.0 ** -10, 1.0), (300.0, 1.0), (1.0, 10.0), (2.0 ** -100, 2.0 ** 90), (2.0 ** 100, 2.0 ** -97)])
+def test_queries_and_keys_of_other_sizes(api, d, nodes, gamma, q_scale, k_scale):
+    """Queries enter the few-rows kernel under a power of two of their own; scores from nothing to hundreds."""
+    x = Layer(api, 2, 3, d, [50, 700], [nodes] * 2, gamma, seed=19 + d, q_scale=q_scale, k_scale=k_scale)
+    for t in (x.k_tree, x.k_spec):
+        if t is not None and k_scale != 1.0:
+            t.copy_((t.float() * k_scale).to(torch.bfloat16))
+    x.run()
+    x.check()
+
+
+@pytest.mark.parametrize("d", [64, 80, 128])
+@pytest.mark.parametrize("nodes,gamma", [s for s in SHAPES if s[0] > 1])
+@pytest.mark.parametrize("what", [float("nan"), float("inf")])
+def test_keys_that_a_row_does_not_see_may_hold_anything(api, d, nodes, gamma, what):
+    """The last node's key, which only its own rows see, and the last stream's key of the first node are not numbers: the other rows'
+    outputs are what they are without."""
+    x = Layer(api, 2, 3, d, [0, 300], [nodes] * 2, gamma, seed=23 + d)
+    x.run()
+    x.check()
+    want = [None if t is None else t.clone() for t in (x.o_main, x.lse_main, x.o_spec, x.lse_spec)]
+    x.k_tree[:, nodes - 1] = what
+    if gamma:
+        x.k_spec[:, 0, gamma - 1] = what
+    x.fresh()
+    x.run()
+    last = nodes - 1
+    for t, w in zip((x.o_main, x.lse_main), want[:2]):
+        assert torch.equal(t[:, :last], w[:, :last])
+        assert not torch.isfinite(t[:, last]).any()
+    if gamma:
+        for t, w in zip((x.o_spec, x.lse_spec), want[2:]):
+            assert torch.equal(t[:, 1:last], w[:, 1:last]) and torch.equal(t[:, 0, :gamma - 1], w[:, 0, :gamma - 1])
+            assert not torch.isfinite(t[:, last]).any() and not torch.isfinite(t[:, 0, gamma - 1]).any()
